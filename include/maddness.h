@@ -300,6 +300,144 @@ int maddness_learn_prototypes(const uint8_t *train_codes, const float *A_train, 
                               void *stream);
 
 /*
+ * The exact product at 8 bits, and layers of experts made of such products.
+ *
+ * Layers that are not replaced by tables keep their product.  It is computed here on the same
+ * kind of numbers as the tables hold: 8 bits beside a power of two, chosen as in Appendix A, but in
+ * floating point (E4M3: sign, 4 exponent bits with bias 7, 3 mantissa bits, largest value 448, no
+ * infinity, one NaN) and with a power of two for every block of 128 values along the sum.
+ *
+ * A block matrix is an 8-bit matrix [rows][cols] with exponents, one byte each (E8M0: byte b stands for
+ * 2^(b - 127), 255 for NaN).  The byte at scale[(r / tile) lds + c / 128] belongs to the value at
+ * data[r ld + c]; tile is 1 (blocks of 1 x 128) or 128 (tiles of 128 x 128).  Matrices of several experts
+ * lie `stride` values and `scale_stride` bytes apart.
+ *   data   16-byte aligned, ld and stride multiples of 16; what lies between cols and ld does not matter.
+ *   scale  4-byte aligned, lds and scale_stride multiples of 4, lds >= ceil(cols / 128); likewise.
+ */
+typedef enum { MADDNESS_E4M3 = 16 } maddness_block_dtype;
+#define MADDNESS_BLOCK 128
+
+typedef struct {
+    const void *data;
+    int32_t dtype;        /* MADDNESS_E4M3 (or MADDNESS_F32 / F16 / BF16 where the call says so) */
+    int32_t tile;         /* rows that share an exponent: 1 or 128 */
+    int64_t rows, cols;   /* of one matrix */
+    int64_t ld;           /* row stride in elements */
+    int64_t stride;       /* from one expert's matrix to the next, in elements */
+    const uint8_t *scale;
+    int64_t lds;          /* row stride of scale in bytes */
+    int64_t scale_stride; /* from one expert's exponents to the next, in bytes */
+} maddness_block_matrix;
+
+/*
+ * x to a block matrix (q, scale), to its transpose (qt, scale_t), or to both from one pass over x.
+ * For every block: t = the largest |x| among its finite values; e = the least integer with t <= 448 2^e, kept in
+ * [-126, 126]; 0 where t = 0.  scale = e + 127; q = x 2^-e rounded to the nearest E4M3 number, ties to even; a NaN or an
+ * infinity becomes NaN and leaves the rest of its block as it is.
+ *
+ * x       [count][rows][ldx] of `dtype` (F32, F16 or BF16), stride_x elements from one matrix to the next.
+ * tile    1: q has blocks of 1 x 128 and qt, the transpose, has blocks of 128 rows of x by one column, which are
+ *         blocks of 1 x 128 of qt.  128: tiles of 128 x 128; qt holds the same values as q.
+ * source  NULL, or [rows]: row r is factors[source[r]] * x[source[r] / repeat], the product rounded to fp32; a source
+ *         outside [0, source_rows repeat) makes a row of zeros.  x then has source_rows rows, and count is 1.
+ * factors NULL (1), or [source_rows repeat] fp32.  Only with source.
+ * q       [count][rows][ldq], scale [count][ceil(rows / tile)][lds], or both NULL.
+ * qt      [count][cols][ldqt], scale_t [count][ceil(cols / tile)][ldst], or both NULL.
+ * The outputs of one matrix follow those of the one before without a gap; alignment as for a block matrix.  Bytes from
+ * the last value of a row up to the next multiple of 16 are set to 0, exponents up to the next multiple of 4 to 127.
+ */
+int maddness_quantise_blocks(const void *x, int32_t dtype, int64_t count, int64_t rows, int64_t cols, int64_t ldx,
+                             int64_t stride_x, int32_t tile, const int32_t *source, int64_t source_rows,
+                             int32_t repeat, const float *factors, uint8_t *q, int64_t ldq, uint8_t *scale,
+                             int64_t lds, uint8_t *qt, int64_t ldqt, uint8_t *scale_t, int64_t ldst, void *stream);
+
+/*
+ * out[m][n] = sum_k A[m][k] B[n][k] of two block matrices, every 8-bit value times its power of two, rounded once to
+ * out_dtype (F32, F16 or BF16).  Products and sums are those of fp32 where out_dtype is F32 or the rows are few; for results
+ * of 16 bits the 128 products of a block may be cut off at 2^-11 of the largest of them before they are added up in fp32.
+ * The order of the sum depends on the sizes only.
+ *
+ * by      MADDNESS_DENSE: A is [M][K], B [N][K], out [M][ldo].
+ *         MADDNESS_BY_ROWS: rows offsets[e] .. offsets[e + 1] - 1 of A are multiplied with the e-th of `groups` matrices
+ *         of B.  Rows of out that no expert has are not written.
+ *         MADDNESS_BY_DEPTH: out is [groups][M][ldo], the e-th from the columns offsets[e] .. offsets[e + 1] - 1 of A and of B
+ *         (0 where there are none); both have tile 1.  For whole blocks, the offsets are multiples of 128.
+ * offsets NULL, or [groups + 1] on the device, not decreasing.  One outside the matrix is cut back to it, and for
+ *         MADDNESS_BY_DEPTH one that is no multiple of 128 is rounded down to one, so a wrong array gives wrong sums
+ *         but no bad access.
+ * A       MADDNESS_E4M3, or F32 / F16 / BF16 (not for MADDNESS_BY_DEPTH): then its rows are rounded as
+ *         maddness_quantise_blocks does with tile 1; data aligned to its element, scale ignored.
+ * workspace  maddness_block_product_workspace(M, N, K, groups, by, dtype of A) bytes, 16-byte aligned (NULL where
+ *         that is 0); contents undefined afterwards.
+ * M = 0 and N = 0 are valid; K = 0 gives zeros.  M, N, K < 2^31.
+ */
+typedef enum { MADDNESS_DENSE = 0, MADDNESS_BY_ROWS = 1, MADDNESS_BY_DEPTH = 2 } maddness_product_groups;
+
+size_t maddness_block_product_workspace(int64_t M, int64_t N, int64_t K, int32_t groups, int32_t by, int32_t a_dtype);
+int maddness_block_product(const maddness_block_matrix *A, const maddness_block_matrix *B, int32_t by, int32_t groups,
+                           const int32_t *offsets, void *out, int32_t out_dtype, int64_t ldo, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/*
+ * Which k of E experts a token goes to, and with which weights.
+ * A logit of minus infinity or NaN takes its expert out of the token's choice; one of plus infinity counts as the largest
+ * fp32 number.  Over the experts that are left (all in fp32; the softmax's sum in fp64, rounded once, so that it does not depend
+ * on an order):
+ *   s     = softmax(logits) or sigmoid(logits)
+ *   key   = s + bias  (bias NULL: 0; one that is minus infinity or NaN takes the expert out of the choice, not
+ *           out of the softmax)
+ *   group g of E / groups experts in a row: the sum of its two largest keys; kept_groups of the groups with an expert
+ *           left are kept, the largest first, the lower index among equals
+ *   ids   = the k largest keys among the kept, largest first, the lower index among equals; -1 once there are no more
+ *   w     = s of those (0 for -1), divided by their sum where renormalise is set and the sum is not 0; times factor
+ *
+ * logits  [T][ldl] of `dtype` (F32, F16, BF16).   bias [E] fp32 or NULL.
+ * ids     [T][k] int32.   weights [T][k] fp32.
+ * 1 <= E <= MADDNESS_MAX_EXPERTS, 1 <= k <= min(E, MADDNESS_MAX_CHOICE), groups divides E and is at most 64.
+ *
+ * maddness_route_gradient: the gradient of the logits [T][ldd] of `dtype`, from that of the weights.  The choice itself has
+ * none; a row's ids may be any (those outside [0, E) have no weight).  renormalise, scores and factor as in the call before.
+ */
+#define MADDNESS_MAX_EXPERTS 1024
+#define MADDNESS_MAX_CHOICE 32
+typedef enum { MADDNESS_SOFTMAX = 0, MADDNESS_SIGMOID = 1 } maddness_scores;
+
+int maddness_route(const void *logits, int32_t dtype, int64_t T, int32_t E, int64_t ldl, const float *bias,
+                   int32_t scores, int32_t groups, int32_t kept_groups, int32_t k, int32_t renormalise, float factor,
+                   int32_t *ids, float *weights, void *stream);
+int maddness_route_gradient(const void *logits, int32_t dtype, int64_t T, int32_t E, int64_t ldl, int32_t scores,
+                            int32_t k, int32_t renormalise, float factor, const int32_t *ids,
+                            const float *weights_gradient, void *gradient, int64_t ldd, void *stream);
+
+/*
+ * The slots 0 .. slots - 1 (slot t k + j is the j-th choice of token t) in the order of their experts, and in their own order
+ * for one expert.  An id outside [0, E) has no place.
+ * offsets [E + 1]: expert e has the places offsets[e] .. offsets[e + 1] - 1, a multiple of `align` of them; counts [E]
+ *         (or NULL): how many are taken, the first ones.
+ * source  [capacity]: the slot at each place, -1 where there is none.
+ * place   [slots]: the place of each slot, -1 where it has none.
+ * capacity >= maddness_order_capacity(slots, E, align), which is enough for any ids; < 2^31.
+ * workspace  maddness_order_workspace(slots, E) bytes, 4-byte aligned.
+ */
+int64_t maddness_order_capacity(int64_t slots, int32_t E, int32_t align);
+size_t maddness_order_workspace(int64_t slots, int32_t E);
+int maddness_order(const int32_t *ids, int64_t slots, int32_t E, int32_t align, int32_t *offsets, int32_t *counts,
+                   int32_t *source, int64_t capacity, int32_t *place, void *workspace, size_t workspace_bytes,
+                   void *stream);
+
+/*
+ * out[t] = sum_j weights[t][j] y[place[t][j]], j = 0 .. k - 1 in this order, in fp32 and rounded once to out_dtype; a place outside
+ * [0, rows) adds nothing.  y [rows][ldy] of y_dtype, place [T][k], weights [T][k] fp32 or NULL (1), out [T][ldo]; F32, F16 or BF16.
+ * maddness_combine_gradient: weights_gradient[t][j] = sum_n gradient[t][n] y[place[t][j]][n], 0 without a place.  (The
+ * gradient of y is the gradient's rows times the weights: source and factors of maddness_quantise_blocks.)
+ */
+int maddness_combine(const void *y, int32_t y_dtype, int64_t rows, int64_t N, int64_t ldy, const int32_t *place,
+                     const float *weights, int64_t T, int32_t k, void *out, int32_t out_dtype, int64_t ldo, void *stream);
+int maddness_combine_gradient(const void *gradient, int32_t dtype, int64_t ldg, const void *y, int32_t y_dtype,
+                              int64_t rows, int64_t N, int64_t ldy, const int32_t *place, int64_t T, int32_t k,
+                              float *weights_gradient, void *stream);
+
+/*
  * Process-wide switches for tests and measurements (Section 4.4 describes f as table
  * lookups and integer additions; MADDNESS_OPT_KERNELS = 1 keeps the library to kernels
  * of exactly that form).  Normal use needs none of them: every switch starts at 0, "the

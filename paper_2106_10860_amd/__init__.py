@@ -40,6 +40,16 @@ EXPORTS = (
     "maddness_learn_trees",
     "maddness_learn_prototypes_workspace",
     "maddness_learn_prototypes",
+    "maddness_quantise_blocks",
+    "maddness_block_product_workspace",
+    "maddness_block_product",
+    "maddness_route",
+    "maddness_route_gradient",
+    "maddness_order_capacity",
+    "maddness_order_workspace",
+    "maddness_order",
+    "maddness_combine",
+    "maddness_combine_gradient",
     "maddness_set_option",
     "maddness_get_option",
     "maddness_last_error",
@@ -56,6 +66,11 @@ class MaddnessError(RuntimeError):
 class _Params(C.Structure):
     _fields_ = [("D", C.c_int32), ("C", C.c_int32), ("split_dims", C.c_void_p),
                 ("thresholds", C.c_void_p), ("prototypes", C.c_void_p)]
+
+
+class _BlockMatrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("tile", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("ld", C.c_int64), ("stride", C.c_int64), ("scale", C.c_void_p), ("lds", C.c_int64), ("scale_stride", C.c_int64)]
 
 
 _lib = None
@@ -91,6 +106,20 @@ def lib() -> C.CDLL:
         L.maddness_learn_prototypes_workspace.argtypes = [i32, i32]
         L.maddness_learn_prototypes_workspace.restype = sz
         L.maddness_learn_prototypes.argtypes = [vp, vp, i64, i64, i32, i32, vp, i32, C.c_double, vp, vp, sz, vp]
+        L.maddness_quantise_blocks.argtypes = [vp, i32, i64, i64, i64, i64, i64, i32, vp, i64, i32, vp, vp, i64, vp, i64, vp, i64,
+                                               vp, i64, vp]
+        L.maddness_block_product_workspace.argtypes = [i64, i64, i64, i32, i32, i32]
+        L.maddness_block_product_workspace.restype = sz
+        L.maddness_block_product.argtypes = [C.POINTER(_BlockMatrix), C.POINTER(_BlockMatrix), i32, i32, vp, vp, i32, i64, vp, sz, vp]
+        L.maddness_route.argtypes = [vp, i32, i64, i32, i64, vp, i32, i32, i32, i32, i32, C.c_float, vp, vp, vp]
+        L.maddness_route_gradient.argtypes = [vp, i32, i64, i32, i64, i32, i32, i32, C.c_float, vp, vp, vp, i64, vp]
+        L.maddness_order_capacity.argtypes = [i64, i32, i32]
+        L.maddness_order_capacity.restype = i64
+        L.maddness_order_workspace.argtypes = [i64, i32]
+        L.maddness_order_workspace.restype = sz
+        L.maddness_order.argtypes = [vp, i64, i32, i32, vp, vp, vp, i64, vp, vp, sz, vp]
+        L.maddness_combine.argtypes = [vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, i32, i64, vp]
+        L.maddness_combine_gradient.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, vp, i64, i32, vp, vp]
         L.maddness_set_option.argtypes = [i32, i32]
         L.maddness_get_option.argtypes = [i32]
         L.maddness_get_option.restype = i32
@@ -501,3 +530,17 @@ def maddness_get_option(option: int) -> int:
 def maddness_last_kernel() -> str:
     """Which kernel the last call on this thread launched (diagnostic; "" if none)."""
     return lib().maddness_last_kernel().decode()
+
+
+# The exact product at 8 bits and layers of experts (the calls' own module, their names here).
+from .blocks import (  # noqa: E402
+    BLOCK,
+    BlockMatrix,
+    maddness_block_product,
+    maddness_combine,
+    maddness_combine_gradient,
+    maddness_order,
+    maddness_quantise_blocks,
+    maddness_route,
+    maddness_route_gradient,
+)

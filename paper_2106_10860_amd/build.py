@@ -15,7 +15,7 @@ LIB = os.path.join(HERE, "libmaddness.so")
 CALIB_LIB = os.path.join(HERE, "libmaddness_calib.so")
 CALIB_SOURCE = os.path.join("calib", "stream_copy.hip")
 SOURCES = ["api.hip", "encode_scan.hip", "fused_rows.hip", "encode_cols.hip", "mfma_scan.hip", "fused_mfma.hip", "fused_blocks.hip", "build_luts.hip",
-           "learn.hip"]
+           "learn.hip", "api_blocks.hip", "block_quantise.hip", "block_product.hip", "route.hip"]
 # the Python calls' argument marshalling: host code against torch's headers, a library of its own
 BINDING_LIB = os.path.join(HERE, "maddness_binding.so")
 BINDING_SOURCE = "binding.cpp"

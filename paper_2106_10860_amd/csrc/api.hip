@@ -32,8 +32,7 @@ void note_kernel(const char *family, const char *instance)
     g_kernel_instance = instance;
 }
 
-// every launching entry point starts with this
-static void begin_call() { g_kernel_family = g_kernel_instance = nullptr; }
+void begin_call() { g_kernel_family = g_kernel_instance = nullptr; }
 
 int check_hip(hipError_t e, const char *what)
 {

@@ -1,0 +1,183 @@
+// What the kernels on 8-bit block matrices share: the number format, its conversions and the search for an expert's rows.
+#pragma once
+
+#include "common.h"
+#include "device_common.h"
+
+namespace maddness {
+
+constexpr int kE4M3 = MADDNESS_E4M3;
+constexpr int kBlock = MADDNESS_BLOCK;
+
+using i32x4 = __attribute__((ext_vector_type(4))) int;
+using i32x8 = __attribute__((ext_vector_type(8))) int;
+using f32x4 = __attribute__((ext_vector_type(4))) float;
+
+template <typename T>
+__host__ __device__ constexpr T ceil_div(T a, T b) { return (a + b - 1) / b; }
+template <typename T>
+__host__ __device__ constexpr T round_up(T a, T b) { return ceil_div(a, b) * b; }
+
+// Eight consecutive elements (any alignment to the element), widened; those from `n` on are 0.
+template <int DT>
+__device__ __forceinline__ void load8(const void *base, int64_t at, int n, float (&v)[8])
+{
+    if (n >= 8) {
+        struct __attribute__((packed, aligned(elem_size(DT)))) Piece { uint32_t w[2 * elem_size(DT)]; };
+        const Piece p = *reinterpret_cast<const Piece *>(static_cast<const char *>(base) + at * elem_size(DT));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (DT == kF32) v[i] = __uint_as_float(p.w[i]);
+            else if constexpr (DT == kBF16) v[i] = __uint_as_float(i & 1 ? p.w[i / 2] & 0xffff0000u : p.w[i / 2] << 16);
+            else v[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(p.w[i / 2] >> (i & 1 ? 16 : 0)));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? widen_at<DT>(base, at + i) : 0.0f;
+    }
+}
+
+// |x| of a finite x as bits (they order as the numbers do), 0 for NaN and the infinities.
+__device__ __forceinline__ uint32_t finite_magnitude(float x)
+{
+    const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
+    return b < 0x7f800000u ? b : 0u;
+}
+
+// The exponent byte of a block whose largest magnitude has these bits.  A number m 2^E, 1 <= m < 2, is at most
+// 448 2^e = 1.75 2^(8 + e) from e = E - 8 on where m <= 1.75, from E - 7 on where it is larger: the addition carries into the
+// exponent just then.
+__device__ __forceinline__ uint32_t exponent_byte(uint32_t top)
+{
+    if (top == 0) return 127;
+    const int e = (int)((top + 0x1fffffu) >> 23) - 8;      // biased
+    return (uint32_t)max(e, 1);
+}
+
+// 2^-e for a byte of 1 .. 253, exactly
+__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// Four values (scaled; at most 448 where finite) to E4M3, nearest, ties to even.
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d)
+{
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// Scaled for pack4: infinities become NaN (the format has none, and the conversion would make 448 of them).
+__device__ __forceinline__ float scaled(float x, float inverse)
+{
+    const float y = x * inverse;
+    return fabsf(x) == __builtin_inff() ? __builtin_nanf("") : y;
+}
+
+// Largest value of the 16 lanes of a row of lanes, in all of them (rotations within the row).
+__device__ __forceinline__ uint32_t row16_max(uint32_t x)
+{
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x124, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x122, 0xf, 0xf, true));
+    return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x121, 0xf, 0xf, true));
+}
+
+// fp32 to a result's type, nearest even, NaN kept.
+__device__ __forceinline__ uint16_t to_bf16(float x)
+{
+    const uint32_t b = __float_as_uint(x);
+    if ((b & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((b >> 16) | 0x40u);
+    return (uint16_t)((b + 0x7fffu + ((b >> 16) & 1u)) >> 16);
+}
+
+template <int DT>
+__device__ __forceinline__ void store_as(void *base, int64_t at, float x)
+{
+    if constexpr (DT == kF32) static_cast<float *>(base)[at] = x;
+    else if constexpr (DT == kF16) static_cast<_Float16 *>(base)[at] = (_Float16)x;
+    else static_cast<uint16_t *>(base)[at] = to_bf16(x);
+}
+
+// Two results as one word of a narrow type.
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    if constexpr (DT == kF16) {
+        const uint16_t x = __builtin_bit_cast(uint16_t, (_Float16)a), y = __builtin_bit_cast(uint16_t, (_Float16)b);
+        return x | ((uint32_t)y << 16);
+    } else {
+        return to_bf16(a) | ((uint32_t)to_bf16(b) << 16);
+    }
+}
+
+// Entry e of an array of offsets, cut back to 0 .. limit.
+__device__ __forceinline__ int64_t offset_at(const int32_t *offsets, int e, int64_t limit)
+{
+    return min(max((int64_t)offsets[e], (int64_t)0), limit);
+}
+
+// The piece of `rows` rows with index `piece` when every expert's rows are cut into pieces of their own: the expert, or -1 where
+// there are fewer pieces; first and one-past-last row.  Every lane of a wavefront calls it with the same piece.
+__device__ __forceinline__ int find_piece(const int32_t *offsets, int groups, int64_t limit, int rows, int64_t piece, int64_t &first, int64_t &last)
+{
+    const int lane = threadIdx.x & 63;
+    int64_t before = 0;
+    for (int e0 = 0; e0 < groups; e0 += 64) {
+        const int e = e0 + lane;
+        const int64_t lo = e < groups ? offset_at(offsets, e, limit) : 0, hi = e < groups ? offset_at(offsets, e + 1, limit) : 0;
+        const int mine = hi > lo ? (int)ceil_div(hi - lo, (int64_t)rows) : 0;      // (limit < 2^31)
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        const int64_t at = piece - before;
+        const uint64_t has = __ballot(at < upto && at >= upto - mine);
+        if (has) {
+            const int l = __ffsll((unsigned long long)has) - 1;
+            const int begin = __shfl(upto - mine, l);
+            const int64_t low = (int64_t)__shfl((int)lo, l), high = (int64_t)__shfl((int)hi, l);
+            first = low + (at - begin) * rows;
+            last = min(first + rows, high);
+            return e0 + l;
+        }
+        before += __shfl(upto, 63);
+    }
+    return -1;
+}
+
+// Arguments of a product, as the launchers hand them on.
+struct ProductArgs {
+    const uint8_t *a, *b;              // 8-bit values (a: elements of a_dtype)
+    const uint8_t *scale_a, *scale_b;
+    int64_t lda, ldb, lds_a, lds_b;
+    int64_t stride_b, scale_stride_b;  // between experts
+    int shift_a, shift_b;              // row -> row of exponents: 0 or 7
+    int64_t M, N, K;
+    int by, groups;
+    const int32_t *offsets;
+    void *out;
+    int64_t ldo, out_stride;
+};
+
+int launch_quantise_blocks(const void *x, int dtype, int64_t count, int64_t rows, int64_t cols, int64_t ldx, int64_t stride_x, int tile,
+                           const int32_t *source, int64_t source_rows, int repeat, const float *factors, uint8_t *q, int64_t ldq,
+                           uint8_t *scale, int64_t lds, uint8_t *qt, int64_t ldqt, uint8_t *scale_t, int64_t ldst, hipStream_t stream);
+
+// a_dtype: kE4M3, or a floating type that the kernel rounds by itself (rounds_inside).
+int launch_block_product(const ProductArgs &p, int a_dtype, int out_dtype, hipStream_t stream);
+// Whether a product of this size rounds a floating A inside its kernel; otherwise A is rounded into the workspace before.
+bool rounds_inside(int64_t M, int64_t N, int64_t K, int groups, int by);
+
+int launch_route(const void *logits, int dtype, int64_t T, int E, int64_t ldl, const float *bias, int scores, int groups, int kept, int k,
+                 bool renormalise, float factor, int32_t *ids, float *weights, hipStream_t stream);
+int launch_route_gradient(const void *logits, int dtype, int64_t T, int E, int64_t ldl, int scores, int k, bool renormalise, float factor,
+                          const int32_t *ids, const float *dweights, void *gradient, int64_t ldd, hipStream_t stream);
+size_t order_workspace_bytes(int64_t slots, int E);
+int launch_order(const int32_t *ids, int64_t slots, int E, int align, int32_t *offsets, int32_t *counts, int32_t *source, int64_t capacity,
+                 int32_t *place, void *workspace, hipStream_t stream);
+int launch_combine(const void *y, int y_dtype, int64_t rows, int64_t N, int64_t ldy, const int32_t *place, const float *weights, int64_t T,
+                   int k, void *out, int out_dtype, int64_t ldo, hipStream_t stream);
+int launch_combine_gradient(const void *gradient, int dtype, int64_t ldg, const void *y, int y_dtype, int64_t rows, int64_t N, int64_t ldy,
+                            const int32_t *place, int64_t T, int k, float *dweights, hipStream_t stream);
+
+}  // namespace maddness

@@ -20,6 +20,9 @@ int fail(int code, const char *fmt, ...);
 // template arguments) or nullptr.  The first kernel noted in a call is the one kept.
 void note_kernel(const char *family, const char *instance);
 
+// Every launching entry point starts with this.
+void begin_call();
+
 // Turns a hipError_t into MADDNESS_E_HIP (with message) or MADDNESS_OK.
 int check_hip(hipError_t e, const char *what);
 
