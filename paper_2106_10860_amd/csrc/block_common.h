@@ -114,33 +114,52 @@ __device__ __forceinline__ int64_t offset_at(const int32_t *offsets, int e, int6
     return min(max((int64_t)offsets[e], (int64_t)0), limit);
 }
 
-// The piece of `rows` rows with index `piece` when every expert's rows are cut into pieces of their own: the expert, or -1 where
-// there are fewer pieces; first and one-past-last row.  Every lane of a wavefront calls it with the same piece.
+// Every expert's rows are cut into pieces of their own, `rows` rows each: lane l gets the bounds lo, hi of expert e0 + l's rows, the
+// number of its pieces and that of the pieces up to and with them.
+__device__ __forceinline__ void pieces_of(const int32_t *offsets, int groups, int64_t limit, int rows, int e0, int &lo, int &hi, int &mine, int &upto)
+{
+    const int lane = threadIdx.x & 63, e = e0 + lane;
+    lo = e < groups ? (int)offset_at(offsets, e, limit) : 0;              // (limit < 2^31)
+    hi = e < groups ? (int)offset_at(offsets, e + 1, limit) : 0;
+    mine = hi > lo ? ceil_div((int64_t)hi - lo, (int64_t)rows) : 0;
+    upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+}
+
+__device__ __forceinline__ int64_t count_pieces(const int32_t *offsets, int groups, int64_t limit, int rows)
+{
+    int64_t all = 0;
+    for (int e0 = 0; e0 < groups; e0 += 64) {
+        int lo, hi, mine, upto;
+        pieces_of(offsets, groups, limit, rows, e0, lo, hi, mine, upto);
+        all += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return all;
+}
+
+// The piece with index `piece`: its expert, or -1 where there are fewer; first and one-past-last row.  Every lane of a wavefront calls
+// it with the same piece.
 __device__ __forceinline__ int find_piece(const int32_t *offsets, int groups, int64_t limit, int rows, int64_t piece, int64_t &first, int64_t &last)
 {
-    const int lane = threadIdx.x & 63;
     int64_t before = 0;
     for (int e0 = 0; e0 < groups; e0 += 64) {
-        const int e = e0 + lane;
-        const int64_t lo = e < groups ? offset_at(offsets, e, limit) : 0, hi = e < groups ? offset_at(offsets, e + 1, limit) : 0;
-        const int mine = hi > lo ? (int)ceil_div(hi - lo, (int64_t)rows) : 0;      // (limit < 2^31)
-        int upto = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
-        }
+        int lo, hi, mine, upto;
+        pieces_of(offsets, groups, limit, rows, e0, lo, hi, mine, upto);
         const int64_t at = piece - before;
         const uint64_t has = __ballot(at < upto && at >= upto - mine);
         if (has) {
             const int l = __ffsll((unsigned long long)has) - 1;
-            const int begin = __shfl(upto - mine, l);
-            const int64_t low = (int64_t)__shfl((int)lo, l), high = (int64_t)__shfl((int)hi, l);
+            const int begin = __builtin_amdgcn_readlane(upto - mine, l);
+            const int64_t low = __builtin_amdgcn_readlane(lo, l), high = __builtin_amdgcn_readlane(hi, l);
             first = low + (at - begin) * rows;
             last = min(first + rows, high);
             return e0 + l;
         }
-        before += __shfl(upto, 63);
+        before += __builtin_amdgcn_readlane(upto, 63);
     }
     return -1;
 }

@@ -10,6 +10,8 @@
 // B's rows (the columns of out) are the instruction's first operand and A's rows its second, so that a lane's four results are
 // four neighbours in a row of out.  Lane l holds row l % 16, values 32 (l / 16) .. + 31 of an operand's block, and results
 // n = 4 (l / 16) + i of row m = l % 16.
+#include <type_traits>
+
 #include "block_common.h"
 
 namespace maddness {
@@ -210,6 +212,181 @@ __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, 
     }
 }
 
+// Buffers of plain bytes, and the longest row of 8-bit values that 256 of stay below 2^32 bytes.
+constexpr int kBufferFlags = 0x00027000;
+constexpr int64_t kMostStride = (int64_t)1 << 23;
+constexpr int kExpBlocks = 64;          // blocks whose exponents are in LDS at a time
+
+// Four neighbours of a row of out.
+template <int OUT>
+__device__ __forceinline__ void store4(void *out, int64_t at, f32x4 v, int64_t n, int64_t N, bool wide)
+{
+    if (wide && n + 3 < N) {
+        if constexpr (OUT == kF32) *reinterpret_cast<f32x4 *>(static_cast<float *>(out) + at) = v;
+        else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + at) = make_uint2(pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < N) store_as<OUT>(out, at + i, v[i]);
+    }
+}
+
+// The index among a launch's workgroups that work, such that each of the 8 dies (workgroups go to them in turn) gets neighbours.
+__device__ __forceinline__ uint32_t by_die(uint32_t id, uint32_t total)
+{
+    const uint32_t die = id % 8, each = total / 8, more = total % 8;
+    return die * each + min(die, more) + id / 8;
+}
+
+// Many rows: BM x BN results to a workgroup of WM x WN wavefronts, each with (BM / WM) x (BN / WN) of them in registers.  Blocks of 128 values
+// of the BM + BN rows go to LDS without passing registers, the next one while this one is multiplied.  A row's eight pieces of 16 bytes lie
+// exchanged by half its index, so that the 16 rows that a read of the lanes goes to fall on all banks.  WIDE: the 16-bit instruction.
+template <int BM, int BN, int WM, int WN, bool WIDE, int OUT>
+__global__ __launch_bounds__(WM * WN * 64, 2) void product_tiles_kernel(ProductArgs p, uint32_t col_tiles)
+{
+    constexpr int WAVES = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16, LOADS_A = BM / 8 / WAVES, LOADS_B = BN / 8 / WAVES;
+    static_assert(WAVES % 2 == 0 && LOADS_A * 8 * WAVES == BM && LOADS_B * 8 * WAVES == BN, "a wavefront loads whole groups of 8 rows, all at even or all at odd places");
+    __shared__ __attribute__((aligned(128))) uint8_t tiles[2][(BM + BN) * kBlock];
+    __shared__ uint32_t exps[kExpBlocks / 4][BM + BN];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r16 = lane % 16, g = lane / 16;
+
+    const uint32_t pieces = p.by == MADDNESS_BY_ROWS ? (uint32_t)count_pieces(p.offsets, p.groups, p.M, BM) : (uint32_t)ceil_div(p.M, (int64_t)BM);
+    if (blockIdx.x >= pieces * col_tiles) return;
+    // four pieces by all columns, then the next four: what a die works on at a time shares rows of both operands
+    const uint32_t at = by_die(blockIdx.x, pieces * col_tiles), band = at / (4 * col_tiles), in_band = at % (4 * col_tiles);
+    const uint32_t height = min(4u, pieces - band * 4);
+    const int64_t n0 = (int64_t)(in_band / height) * BN;
+    Part w;
+    if (!find_part(p, BM, band * 4 + in_band % height, blockIdx.y, w)) return;
+
+    // Rows are addressed by 32-bit offsets within the tile (the launcher keeps row strides to kMostStride).  What lies beyond the tile's last
+    // row is out of the buffers' range; what lies beyond column K is cut off in LDS.
+    const uint32_t lda = (uint32_t)p.lda, ldb = (uint32_t)p.ldb, blocks = (uint32_t)ceil_div(w.K, (int64_t)kBlock);
+    const uint32_t rows = (uint32_t)(w.last - w.first), cols = (uint32_t)min((int64_t)BN, p.N - n0), width = round_up((uint32_t)w.K, 16u);
+    const auto mem_a = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a + w.first * p.lda), 0, (rows - 1) * lda + width, kBufferFlags);
+    const auto mem_b = __builtin_amdgcn_make_buffer_rsrc((void *)(w.b + n0 * p.ldb), 0, (cols - 1) * ldb + width, kBufferFlags);
+    const uint32_t chunk = (uint32_t)((lane % 8) ^ ((wave % 2) * 4 + lane / 16)) * 16, row0 = wave * 8 + lane / 8;
+    const uint32_t at_a = row0 * lda + chunk, at_b = row0 * ldb + chunk;
+    // (keeps the compiler from holding every sum of this and a multiple of a stride in a register of its own)
+    auto again = [](uint32_t x) INLINE_LAMBDA { asm volatile("" : "+v"(x)); return x; };
+    auto load = [&](uint8_t *tile, uint32_t kb) INLINE_LAMBDA {
+        const uint32_t lane_a = again(at_a), lane_b = again(at_b);
+#pragma unroll
+        for (int i = 0; i < LOADS_A; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(mem_a, (__attribute__((address_space(3))) void *)(tile + (wave + i * WAVES) * 1024), 16,
+                                                     lane_a + ((i * WAVES * 8) * lda + kb * kBlock), 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < LOADS_B; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(mem_b, (__attribute__((address_space(3))) void *)(tile + BM * kBlock + (wave + i * WAVES) * 1024), 16,
+                                                     lane_b + ((i * WAVES * 8) * ldb + kb * kBlock), 0, 0, 0);
+    };
+    const int wm = wave / WN, wn = wave % WN;
+    // The exponents of kExpBlocks blocks, four to a word, by rows.
+    auto load_exps = [&](uint32_t kb) INLINE_LAMBDA {
+        const uint32_t some = min((uint32_t)kExpBlocks, blocks - kb);
+        for (int row = threadIdx.x; row < BM + BN; row += WAVES * 64) {
+            const uint8_t *from = row < BM ? p.scale_a + (min(w.first + row, w.last - 1) >> p.shift_a) * p.lds_a
+                                           : w.scale_b + (min(n0 + row - BM, p.N - 1) >> p.shift_b) * p.lds_b;
+            for (uint32_t q = 0; q * 4 < some; ++q) exps[q][row] = *reinterpret_cast<const uint32_t *>(from + kb + q * 4);
+        }
+    };
+    f32x4 acc[MT][NT] = {};
+    const int half0 = r16 * kBlock + (((2 * g) ^ (r16 / 2)) * 16), half1 = r16 * kBlock + (((2 * g + 1) ^ (r16 / 2)) * 16);
+    auto fragment = [&](const uint8_t *tile, int row) INLINE_LAMBDA {
+        const i32x4 lo = *reinterpret_cast<const i32x4 *>(tile + row * kBlock + half0), hi = *reinterpret_cast<const i32x4 *>(tile + row * kBlock + half1);
+        return i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    // The columns from K on of the last block, in both operands, to zeros.
+    auto cut_off = [&](uint8_t *tile) INLINE_LAMBDA {
+        for (int row = threadIdx.x; row < BM + BN; row += WAVES * 64)
+            for (int k = (int)(w.K % kBlock); k < kBlock; ++k) tile[row * kBlock + (((k / 16) ^ (row / 2 % 8)) * 16 + k % 16)] = 0;
+        __syncthreads();
+    };
+    const uint32_t kb0 = (uint32_t)w.kb0, kb1 = (uint32_t)w.kb1;
+    if (kb0 < kb1) {
+        uint8_t *tile = tiles[0], *next = tiles[1];
+        load(tile, kb0);
+        load_exps(kb0 / kExpBlocks * kExpBlocks);
+        uint32_t ea[MT], eb[NT];                             // this block's in the lowest byte
+        __syncthreads();
+        for (uint32_t kb = kb0;; ++kb) {
+            if (kb + 1 == kb1 && w.K % kBlock) cut_off(tile);
+            if (kb % 4 == 0 || kb == kb0) {
+                const uint32_t *from = exps[kb % kExpBlocks / 4] + r16;
+#pragma unroll
+                for (int t = 0; t < MT; ++t) ea[t] = from[(wm * MT + t) * 16] >> (kb % 4 * 8);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) eb[t] = from[BM + (wn * NT + t) * 16] >> (kb % 4 * 8);
+            }
+            // All fragments are asked for before the next block is: the compiler lets no read of LDS pass a load into it.
+            i32x8 b[NT], a[MT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) b[j] = fragment(tile, BM + (wn * NT + j) * 16);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) a[i] = fragment(tile, (wm * MT + i) * 16);
+            __builtin_amdgcn_sched_barrier(0);
+            if (kb + 1 < kb1) load(next, kb + 1);
+            if constexpr (!WIDE) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], 0, 0, 0, (int)eb[j], 0, (int)ea[i]);
+            } else {
+                bf16x8 wb[NT][4];
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) wb[j][q] = widen8(b[j][2 * q], b[j][2 * q + 1], as_scale(eb[j] & 255));
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const bf16x8 wa = widen8(a[i][2 * q], a[i][2 * q + 1], as_scale(ea[i] & 255));
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][q], wa, acc[i][j], 0, 0, 0);
+                    }
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t) ea[t] >>= 8;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) eb[t] >>= 8;
+            if (kb + 1 >= kb1) break;
+            __syncthreads();
+            if ((kb + 1) % kExpBlocks == 0) {
+                load_exps(kb + 1);
+                __syncthreads();
+            }
+            uint8_t *t = tile;
+            tile = next;
+            next = t;
+        }
+    }
+    constexpr int64_t bytes = OUT == kF32 ? 4 : 2;
+    const bool wide = (reinterpret_cast<uintptr_t>(p.out) | (uint64_t)(p.ldo * bytes) | (uint64_t)(w.out_at * bytes)) % (4 * bytes) == 0;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t m = w.first + (wm * MT + i) * 16 + r16;
+        if (m >= w.last) continue;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int64_t n = n0 + (wn * NT + j) * 16 + 4 * g;
+            store4<OUT>(p.out, w.out_at + m * p.ldo + n, acc[i][j], n, p.N, wide);
+        }
+    }
+}
+
+template <int BM, int BN, int WM, int WN, int OUT>
+int launch_tiles(const ProductArgs &p, hipStream_t stream)
+{
+    const int64_t col_tiles = ceil_div(p.N, (int64_t)BN), pieces = ceil_div(p.M, (int64_t)BM) + (p.by == MADDNESS_BY_ROWS ? p.groups : 0);
+    if (col_tiles * pieces >= (int64_t)1 << 31) return fail(MADDNESS_E_UNSUPPORTED, "block product: %lld x %lld results are too many", (long long)p.M, (long long)p.N);
+    const dim3 grid((unsigned)(col_tiles * pieces), p.by == MADDNESS_BY_DEPTH ? (unsigned)p.groups : 1u);
+    note_kernel("product_tiles_kernel", __PRETTY_FUNCTION__);
+    hipLaunchKernelGGL((product_tiles_kernel<BM, BN, WM, WN, OUT == kF32, OUT>), grid, dim3(WM * WN * 64), 0, stream, p, (uint32_t)col_tiles);
+    return check_hip(hipGetLastError(), "launch product_tiles_kernel");
+}
+
 template <int AT, int OUT>
 int launch_few(const ProductArgs &p, hipStream_t stream)
 {
@@ -233,7 +410,12 @@ int launch_to(const ProductArgs &p, int a_dtype, hipStream_t stream)
     if (a_dtype == MADDNESS_F32) return launch_few<kF32, OUT>(p, stream);
     if (a_dtype == MADDNESS_F16) return launch_few<kF16, OUT>(p, stream);
     if (a_dtype == MADDNESS_BF16) return launch_few<kBF16, OUT>(p, stream);
-    return launch_few<kE4M3, OUT>(p, stream);
+    const int64_t groups = p.by == MADDNESS_DENSE ? 1 : p.groups, rows = p.by == MADDNESS_BY_ROWS ? ceil_div(p.M, groups) : p.M;
+    if (rows <= 64 || std::max(p.lda, p.ldb) > kMostStride) return launch_few<kE4M3, OUT>(p, stream);
+    const int64_t large = ceil_div(rows, (int64_t)256) * ceil_div(p.N, (int64_t)256) * groups;
+    if constexpr (OUT != kF32)
+        if (large >= device_info().cus && rows >= 1024) return launch_tiles<256, 256, 2, 4, OUT>(p, stream);
+    return launch_tiles<128, 128, 2, 2, OUT>(p, stream);
 }
 
 }  // namespace
