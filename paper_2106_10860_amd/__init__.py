@@ -146,6 +146,7 @@ class _NotBuilt:
         return NotImplemented
 
     encode = scan = build_luts = encode_scan
+    quantise_blocks = block_product = route = route_gradient = order = combine = combine_gradient = encode_scan
 
 
 class _NotLoaded:

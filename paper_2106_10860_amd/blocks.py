@@ -67,7 +67,7 @@ class BlockMatrix:
     """8-bit values ``q`` [rows, cols] (or [experts, rows, cols]) of dtype float8_e4m3fn with unit column stride, and their exponents
     ``scale``, uint8 [rows / tile, cols / 128] each rounded up, the byte b for 2^(b - 127)."""
 
-    __slots__ = ("q", "scale", "tile", "shape", "_struct")
+    __slots__ = ("q", "scale", "tile")
 
     def __init__(self, q, scale, tile: int = 1):
         torch = _m._torch or _m._torch_module()
@@ -84,17 +84,31 @@ class BlockMatrix:
         if tuple(scale.shape[:-1]) != need[:-1] or scale.shape[-1] < need[-1]:
             raise ValueError(f"scale must have shape {need} (or wider rows) for q of shape {tuple(q.shape)}, has {tuple(scale.shape)}")
         _same_device(q, scale)
-        self.q, self.scale, self.tile, self.shape = q, scale, tile, tuple(q.shape)
-        ld, stride = self._strides(q, 16, "q")
-        lds, scale_stride = self._strides(scale, 4, "scale")
-        self._struct = _m._BlockMatrix(q.data_ptr(), MADDNESS_E4M3, tile, rows, cols, ld, stride, scale.data_ptr(), lds, scale_stride)
+        for t, name in ((q, "q"), (scale, "scale")):
+            if t.shape[-1] > 1 and t.stride(-1) != 1:
+                raise ValueError(f"{name} must have unit column stride")
+        self.q, self.scale, self.tile = q, scale, tile
 
-    @staticmethod
-    def _strides(t, unit: int, name: str):
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError(f"{name} must have unit column stride")
-        ld = t.stride(-2) if t.shape[-2] > 1 else _up(max(t.shape[-1], t.stride(-2)), unit)
-        return ld, (t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else 0)
+    @classmethod
+    def _made(cls, q, scale, tile: int) -> "BlockMatrix":
+        """Of tensors that this package made."""
+        b = cls.__new__(cls)
+        b.q, b.scale, b.tile = q, scale, tile
+        return b
+
+    @property
+    def shape(self):
+        return tuple(self.q.shape)
+
+    @property
+    def _struct(self):
+        def strides(t, unit):
+            ld = t.stride(-2) if t.shape[-2] > 1 else _up(max(t.shape[-1], t.stride(-2)), unit)
+            return ld, (t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else 0)
+
+        (ld, stride), (lds, scale_stride) = strides(self.q, 16), strides(self.scale, 4)
+        rows, cols = self.q.shape[-2:]
+        return _m._BlockMatrix(self.q.data_ptr(), MADDNESS_E4M3, self.tile, rows, cols, ld, stride, self.scale.data_ptr(), lds, scale_stride)
 
     @property
     def device(self):
@@ -125,6 +139,10 @@ def maddness_quantise_blocks(x, tile: int = 1, transposed: bool = False, both: b
 
     ``source`` (int32 [rows']): row r of the result is x[source[r] // repeat] (times factors[source[r]] where ``factors``, fp32, is
     given), zeros where source[r] is negative; x is 2-D then."""
+    r = _m._native.quantise_blocks(x, tile, transposed, both, source, repeat, factors, stream)
+    if r is not NotImplemented:
+        r = _m._done(r)
+        return (BlockMatrix._made(r[0], r[1], tile), BlockMatrix._made(r[2], r[3], tile)) if both else BlockMatrix._made(r[0], r[1], tile)
     torch = _m._torch or _m._torch_module()
     code = _code(x, "x")
     if x.dim() == 2:
@@ -164,11 +182,14 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", ou
     With ``offsets`` (int32 [experts + 1]) by experts: by="rows" multiplies rows offsets[e] .. offsets[e + 1] - 1 of A with B[e]
     (B [experts, N, K]) into out [M, N], rows that no expert has are left as they are; by="depth" gives out [experts, M, N] from the
     columns offsets[e] .. offsets[e + 1] - 1 of A [M, K] and B [N, K] (multiples of 128)."""
-    torch = _m._torch or _m._torch_module()
     if not isinstance(B, BlockMatrix):
         raise TypeError("B must be a BlockMatrix")
-    if by not in ("rows", "depth"):
+    if by != "rows" and by != "depth":
         raise ValueError(f"by must be 'rows' or 'depth', is {by!r}")
+    r = _m._native.block_product(isinstance(A, BlockMatrix), A, B, offsets, by == "depth", out_dtype, out, workspace, stream)
+    if r is not NotImplemented:
+        return _m._done(r)
+    torch = _m._torch or _m._torch_module()
     if isinstance(A, BlockMatrix):
         if len(A.shape) != 2:
             raise ValueError("A must be 2-D")
@@ -219,6 +240,9 @@ def _scores(scores: str) -> int:
 def maddness_route(logits, k: int, scores: str = "softmax", bias=None, groups: int = 1, kept_groups: int = 1, renormalise: bool = True,
                    factor: float = 1.0, stream=None):
     """Which k experts each token goes to, and with which weights: (ids int32 [T, k], -1 where there is none; weights fp32 [T, k])."""
+    r = _m._native.route(logits, k, _scores(scores) == 1, bias, groups, kept_groups, renormalise, factor, stream)
+    if r is not NotImplemented:
+        return _m._done(r)
     torch = _m._torch or _m._torch_module()
     code = _code(logits, "logits")
     T, E, ldl = _m._rows(logits, "logits")
@@ -235,6 +259,9 @@ def maddness_route(logits, k: int, scores: str = "softmax", bias=None, groups: i
 
 def maddness_route_gradient(logits, ids, weights_gradient, scores: str = "softmax", renormalise: bool = True, factor: float = 1.0, stream=None):
     """The gradient of the logits (their dtype, [T, E]) from that of the weights that maddness_route gave with these ids."""
+    r = _m._native.route_gradient(logits, ids, weights_gradient, _scores(scores) == 1, renormalise, factor, stream)
+    if r is not NotImplemented:
+        return _m._done(r)
     torch = _m._torch or _m._torch_module()
     code = _code(logits, "logits")
     T, E, ldl = _m._rows(logits, "logits")
@@ -253,6 +280,9 @@ def maddness_route_gradient(logits, ids, weights_gradient, scores: str = "softma
 def maddness_order(ids, experts: int, align: int = 1, stream=None):
     """The slots (choice j of token t is slot t * k + j) in the order of their experts: (offsets int32 [experts + 1], each expert's places
     a multiple of ``align``; counts int32 [experts]; source int32 [places], the slot at each place or -1; place int32 of ids' shape, or -1)."""
+    r = _m._native.order(ids, experts, align, stream)
+    if r is not NotImplemented:
+        return _m._done(r)
     torch = _m._torch or _m._torch_module()
     ids_p = _flat(ids, torch.int32, ids.shape, "ids")
     slots, dev, L = ids.numel(), ids.device, _m.lib()
@@ -270,6 +300,9 @@ def maddness_order(ids, experts: int, align: int = 1, stream=None):
 
 def maddness_combine(y, place, weights=None, out_dtype=None, out=None, stream=None):
     """out[t] = sum over j of weights[t, j] * y[place[t, j]]; a negative place adds nothing, weights None are 1."""
+    r = _m._native.combine(y, place, weights, out_dtype, out, stream)
+    if r is not NotImplemented:
+        return _m._done(r)
     torch = _m._torch or _m._torch_module()
     code = _code(y, "y")
     rows, N, ldy = _m._rows(y, "y")
@@ -290,6 +323,9 @@ def maddness_combine(y, place, weights=None, out_dtype=None, out=None, stream=No
 def maddness_combine_gradient(gradient, y, place, stream=None):
     """The gradient of maddness_combine's weights, fp32 [T, k].  (That of y: maddness_quantise_blocks of the gradient with ``source``
     and ``factors``, or the gradient's rows times the weights.)"""
+    r = _m._native.combine_gradient(gradient, y, place, stream)
+    if r is not NotImplemented:
+        return _m._done(r)
     torch = _m._torch or _m._torch_module()
     code, y_code = _code(gradient, "gradient"), _code(y, "y")
     rows, N, ldy = _m._rows(y, "y")

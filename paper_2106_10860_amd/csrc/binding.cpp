@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdio>
@@ -20,7 +21,7 @@ namespace {
 
 struct NotUsual {};
 
-PyObject *s_split_dims, *s_thresholds, *s_prototypes, *s_C, *s_D, *s_cuda_stream;
+PyObject *s_split_dims, *s_thresholds, *s_prototypes, *s_C, *s_D, *s_cuda_stream, *s_q, *s_scale, *s_tile;
 PyObject *get_stream, *get_device;     // torch._C._cuda_getCurrentRawStream, _cuda_getDevice
 PyObject *int_status(int rc) { return PyLong_FromLong(rc); }
 
@@ -332,6 +333,358 @@ PyObject *build_luts(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ------------------------------------------------------------------------------------- 8-bit block matrices and experts
+
+// The dtype code of a floating type.
+int float_code(at::ScalarType t)
+{
+    if (t == at::kBFloat16) return MADDNESS_BF16;
+    if (t == at::kFloat) return MADDNESS_F32;
+    if (t == at::kHalf) return MADDNESS_F16;
+    throw NotUsual();
+}
+
+at::ScalarType dtype_or(PyObject *o, at::ScalarType otherwise)
+{
+    if (o == Py_None) return otherwise;
+    if (!THPDtype_Check(o)) throw NotUsual();
+    return reinterpret_cast<THPDtype *>(o)->scalar_type;
+}
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// A contiguous tensor of this type and these sizes.
+const at::Tensor &flat(PyObject *o, at::ScalarType type, at::IntArrayRef sizes, const at::Device &device)
+{
+    const at::Tensor &t = tensor(o);
+    if (t.scalar_type() != type || t.sizes() != sizes || !t.is_contiguous() || t.device() != device) throw NotUsual();
+    return t;
+}
+
+template <typename T>
+T *flat_or_null(PyObject *o, at::ScalarType type, at::IntArrayRef sizes, const at::Device &device)
+{
+    return o == Py_None ? nullptr : static_cast<T *>(flat(o, type, sizes, device).data_ptr());
+}
+
+// A BlockMatrix, as its constructor checked it.
+maddness_block_matrix block_matrix(PyObject *o, const at::Device *device, int64_t *experts, at::Device *own = nullptr)
+{
+    Ref q_ref(PyObject_GetAttr(o, s_q)), scale_ref(PyObject_GetAttr(o, s_scale)), tile(PyObject_GetAttr(o, s_tile));
+    const at::Tensor &q = tensor(q_ref.p), &scale = tensor(scale_ref.p);
+    const int64_t n = q.dim();
+    if (n != scale.dim() || (n != 2 && n != 3) || q.scalar_type() != at::kFloat8_e4m3fn || (device && q.device() != *device)) throw NotUsual();
+    maddness_block_matrix m{};
+    m.data = q.data_ptr();
+    m.dtype = MADDNESS_E4M3;
+    m.tile = narrow(whole(tile.p));
+    m.rows = q.size(n - 2);
+    m.cols = q.size(n - 1);
+    m.ld = m.rows > 1 ? q.stride(n - 2) : up(std::max(m.cols, q.stride(n - 2)), 16);
+    m.scale = static_cast<const uint8_t *>(scale.data_ptr());
+    m.lds = scale.size(n - 2) > 1 ? scale.stride(n - 2) : up(std::max(scale.size(n - 1), scale.stride(n - 2)), 4);
+    *experts = n == 3 ? q.size(0) : -1;
+    if (n == 3 && q.size(0) > 1) {
+        m.stride = q.stride(0);
+        m.scale_stride = scale.stride(0);
+    }
+    if (own) *own = q.device();
+    return m;
+}
+
+struct NewBlocks {
+    at::Tensor q, scale;
+    int64_t ld, lds;
+};
+
+NewBlocks new_blocks(int64_t count, int64_t rows, int64_t cols, int64_t tile, const at::Device &device)
+{
+    NewBlocks b;
+    b.ld = up(cols, 16);
+    b.lds = up((cols + MADDNESS_BLOCK - 1) / MADDNESS_BLOCK, 4);
+    const auto bytes = at::TensorOptions().dtype(at::kByte).device(device), e4m3 = bytes.dtype(at::kFloat8_e4m3fn);
+    const int64_t exp_rows = (rows + tile - 1) / tile;
+    b.q = count < 0 ? at::empty({rows, b.ld}, e4m3) : at::empty({count, rows, b.ld}, e4m3);
+    b.scale = count < 0 ? at::empty({exp_rows, b.lds}, bytes) : at::empty({count, exp_rows, b.lds}, bytes);
+    if (b.ld != cols) b.q = b.q.narrow(-1, 0, cols);
+    return b;
+}
+
+// (x, tile, transposed, both, source, repeat, factors, stream) -> (q, scale) or (q, scale, qt, scale_t)
+PyObject *quantise_blocks(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 8) throw NotUsual();
+        const at::Tensor &x = tensor(a[0]);
+        const int code = float_code(x.scalar_type());
+        const int64_t tile = whole(a[1]);
+        const bool transposed = truth(a[2]), both = truth(a[3]);
+        const int64_t repeat = whole(a[5]);
+        if (x.dim() != 2 || (tile != 1 && tile != MADDNESS_BLOCK) || repeat < 1) throw NotUsual();
+        const Rows rx = rows_of(x);
+        int64_t rows = rx.rows;
+        const int32_t *source = nullptr;
+        const float *factors = nullptr;
+        if (a[4] != Py_None) {
+            const at::Tensor &s = tensor(a[4]);
+            if (s.dim() != 1 || s.scalar_type() != at::kInt || !s.is_contiguous() || s.device() != x.device()) throw NotUsual();
+            rows = s.size(0);
+            source = static_cast<const int32_t *>(s.data_ptr());
+            if (a[6] != Py_None) {
+                const at::Tensor &f = tensor(a[6]);
+                if (f.scalar_type() != at::kFloat || !f.is_contiguous() || f.numel() != rx.rows * repeat || f.device() != x.device()) throw NotUsual();
+                factors = static_cast<const float *>(f.data_ptr());
+            }
+        } else if (a[6] != Py_None) {
+            throw NotUsual();
+        }
+        void *stream = stream_of(a[7]);
+        NewBlocks straight, turned;
+        if (both || !transposed) straight = new_blocks(-1, rows, rx.cols, tile, x.device());
+        if (both || transposed) turned = new_blocks(-1, rx.cols, rows, tile, x.device());
+        auto bytes = [](const at::Tensor &t) { return t.defined() ? static_cast<uint8_t *>(t.data_ptr()) : nullptr; };
+        const void *x_p = x.data_ptr();
+        uint8_t *q = bytes(straight.q), *s = bytes(straight.scale), *qt = bytes(turned.q), *st = bytes(turned.scale);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_quantise_blocks(x_p, code, 1, rows, rx.cols, rx.ld, 0, (int32_t)tile, source, rx.rows, (int32_t)repeat, factors, q,
+                                      q ? straight.ld : 0, s, q ? straight.lds : 0, qt, qt ? turned.ld : 0, st, qt ? turned.lds : 0, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        PyObject *tuple = PyTuple_New(both ? 4 : 2);
+        Py_ssize_t at = 0;
+        for (const NewBlocks *b : {&straight, &turned}) {
+            if (!b->q.defined()) continue;
+            PyTuple_SET_ITEM(tuple, at++, THPVariable_Wrap(b->q));
+            PyTuple_SET_ITEM(tuple, at++, THPVariable_Wrap(b->scale));
+        }
+        return tuple;
+    });
+}
+
+// (a_is_blocks, A, B, offsets, by_depth, out_dtype, out, workspace, stream) -> out
+PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 9) throw NotUsual();
+        at::Device device(at::kCPU);
+        maddness_block_matrix A{}, B{};
+        int64_t experts = -1;
+        if (truth(a[0])) {
+            A = block_matrix(a[1], nullptr, &experts, &device);
+            if (experts != -1) throw NotUsual();
+        } else {
+            const at::Tensor &x = tensor(a[1]);
+            const Rows r = rows_of(x);
+            A.data = x.data_ptr();
+            A.dtype = float_code(x.scalar_type());
+            A.tile = 1;
+            A.rows = r.rows;
+            A.cols = r.cols;
+            A.ld = r.ld;
+            device = x.device();
+        }
+        B = block_matrix(a[2], &device, &experts);
+        if (A.cols != B.cols) throw NotUsual();
+        int32_t by = MADDNESS_DENSE, groups = 1;
+        const int32_t *offsets = nullptr;
+        if (a[3] != Py_None) {
+            const at::Tensor &o = tensor(a[3]);
+            if (o.dim() != 1 || o.scalar_type() != at::kInt || !o.is_contiguous() || o.device() != device || o.size(0) < 2) throw NotUsual();
+            groups = narrow(o.size(0) - 1);
+            offsets = static_cast<const int32_t *>(o.data_ptr());
+            by = truth(a[4]) ? MADDNESS_BY_DEPTH : MADDNESS_BY_ROWS;
+            if (by == MADDNESS_BY_ROWS ? experts != groups : experts != -1) throw NotUsual();
+        } else if (experts != -1) {
+            throw NotUsual();
+        }
+        void *stream = stream_of(a[8]);
+        at::Tensor made, work;
+        const at::ScalarType type = dtype_or(a[5], at::kBFloat16);
+        void *out;
+        int64_t ldo;
+        int code;
+        if (a[6] == Py_None) {
+            code = float_code(type);
+            const auto opt = at::TensorOptions().dtype(type).device(device);
+            made = by == MADDNESS_BY_DEPTH ? at::empty({groups, A.rows, B.rows}, opt) : at::empty({A.rows, B.rows}, opt);
+            out = made.data_ptr();
+            ldo = std::max(B.rows, (int64_t)1);
+        } else {
+            const at::Tensor &o = tensor(a[6]);
+            if (by == MADDNESS_BY_DEPTH || o.device() != device || (a[5] != Py_None && o.scalar_type() != type)) throw NotUsual();
+            const Rows r = rows_of(o);
+            if (r.rows != A.rows || r.cols != B.rows) throw NotUsual();
+            code = float_code(o.scalar_type());
+            out = o.data_ptr();
+            ldo = r.ld;
+        }
+        void *work_p = nullptr;
+        size_t work_bytes = 0;
+        if (a[7] != Py_None) {
+            const at::Tensor &w = tensor(a[7]);
+            if (w.scalar_type() != at::kByte || w.device() != device) throw NotUsual();
+            work_p = w.data_ptr();
+            work_bytes = (size_t)w.numel();
+        } else if ((work_bytes = maddness_block_product_workspace(A.rows, B.rows, A.cols, groups, by, A.dtype))) {
+            work = at::empty({(int64_t)work_bytes}, at::TensorOptions().dtype(at::kByte).device(device));
+            work_p = work.data_ptr();
+        }
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_block_product(&A, &B, by, groups, offsets, out, code, ldo, work_p, work_bytes, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        if (made.defined()) return THPVariable_Wrap(std::move(made));
+        Py_INCREF(a[6]);
+        return a[6];
+    });
+}
+
+// (logits, k, sigmoid, bias, groups, kept, renormalise, factor, stream) -> (ids, weights)
+PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 9 || !PyFloat_CheckExact(a[7])) throw NotUsual();
+        const at::Tensor &x = tensor(a[0]);
+        const int code = float_code(x.scalar_type());
+        const Rows r = rows_of(x);
+        const int32_t k = narrow(whole(a[1])), groups = narrow(whole(a[4])), kept = narrow(whole(a[5]));
+        const bool sigmoid = truth(a[2]), renormalise = truth(a[6]);
+        if (k < 1 || r.cols > MADDNESS_MAX_EXPERTS) throw NotUsual();
+        const float *bias = flat_or_null<const float>(a[3], at::kFloat, {r.cols}, x.device());
+        void *stream = stream_of(a[8]);
+        const auto opt = at::TensorOptions().device(x.device());
+        at::Tensor ids = at::empty({r.rows, k}, opt.dtype(at::kInt)), weights = at::empty({r.rows, k}, opt.dtype(at::kFloat));
+        int32_t *ids_p = static_cast<int32_t *>(ids.data_ptr());
+        float *weights_p = static_cast<float *>(weights.data_ptr());
+        const void *x_p = x.data_ptr();
+        const float factor = (float)PyFloat_AS_DOUBLE(a[7]);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_route(x_p, code, r.rows, (int32_t)r.cols, r.ld, bias, sigmoid ? MADDNESS_SIGMOID : MADDNESS_SOFTMAX, groups, kept, k,
+                            renormalise, factor, ids_p, weights_p, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        PyObject *tuple = PyTuple_New(2);
+        PyTuple_SET_ITEM(tuple, 0, THPVariable_Wrap(std::move(ids)));
+        PyTuple_SET_ITEM(tuple, 1, THPVariable_Wrap(std::move(weights)));
+        return tuple;
+    });
+}
+
+// (logits, ids, weights_gradient, sigmoid, renormalise, factor, stream) -> gradient
+PyObject *route_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 7 || !PyFloat_CheckExact(a[5])) throw NotUsual();
+        const at::Tensor &x = tensor(a[0]), &ids = tensor(a[1]);
+        const int code = float_code(x.scalar_type());
+        const Rows r = rows_of(x);
+        if (ids.dim() != 2 || r.cols > MADDNESS_MAX_EXPERTS) throw NotUsual();
+        const int32_t k = narrow(ids.size(1));
+        const int32_t *ids_p = flat_or_null<const int32_t>(a[1], at::kInt, {r.rows, k}, x.device());
+        const float *dw = flat_or_null<const float>(a[2], at::kFloat, {r.rows, k}, x.device());
+        const bool sigmoid = truth(a[3]), renormalise = truth(a[4]);
+        void *stream = stream_of(a[6]);
+        at::Tensor out = at::empty({r.rows, r.cols}, x.options());
+        const void *x_p = x.data_ptr();
+        void *out_p = out.data_ptr();
+        const float factor = (float)PyFloat_AS_DOUBLE(a[5]);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_route_gradient(x_p, code, r.rows, (int32_t)r.cols, r.ld, sigmoid ? MADDNESS_SIGMOID : MADDNESS_SOFTMAX, k, renormalise, factor,
+                                     ids_p, dw, out_p, r.cols, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        return THPVariable_Wrap(std::move(out));
+    });
+}
+
+// (ids, experts, align, stream) -> (offsets, counts, source, place)
+PyObject *order(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 4) throw NotUsual();
+        const at::Tensor &ids = tensor(a[0]);
+        if (ids.scalar_type() != at::kInt || !ids.is_contiguous()) throw NotUsual();
+        const int32_t E = narrow(whole(a[1])), align = narrow(whole(a[2]));
+        if (E < 1 || E > MADDNESS_MAX_EXPERTS || align < 1) throw NotUsual();
+        const int64_t slots = ids.numel(), capacity = maddness_order_capacity(slots, E, align);
+        const int64_t work = ((int64_t)maddness_order_workspace(slots, E) + 3) / 4;
+        void *stream = stream_of(a[3]);
+        const auto opt = ids.options();
+        // one piece of memory: source first, for its alignment
+        at::Tensor all = at::empty({capacity + E + 1 + E + work}, opt), place = at::empty(ids.sizes(), opt);
+        int32_t *base = static_cast<int32_t *>(all.data_ptr()), *place_p = static_cast<int32_t *>(place.data_ptr());
+        const int32_t *ids_p = static_cast<const int32_t *>(ids.data_ptr());
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_order(ids_p, slots, E, align, base + capacity, base + capacity + E + 1, base, capacity, place_p, base + capacity + 2 * E + 1,
+                            (size_t)work * 4, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        PyObject *tuple = PyTuple_New(4);
+        PyTuple_SET_ITEM(tuple, 0, THPVariable_Wrap(all.narrow(0, capacity, E + 1)));
+        PyTuple_SET_ITEM(tuple, 1, THPVariable_Wrap(all.narrow(0, capacity + E + 1, E)));
+        PyTuple_SET_ITEM(tuple, 2, THPVariable_Wrap(all.narrow(0, 0, capacity)));
+        PyTuple_SET_ITEM(tuple, 3, THPVariable_Wrap(std::move(place)));
+        return tuple;
+    });
+}
+
+// (y, place, weights, out_dtype, out, stream) -> out
+PyObject *combine(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 6) throw NotUsual();
+        const at::Tensor &y = tensor(a[0]), &place = tensor(a[1]);
+        const int code = float_code(y.scalar_type());
+        const Rows r = rows_of(y);
+        if (place.dim() != 2 || a[4] != Py_None) throw NotUsual();
+        const int64_t T = place.size(0);
+        const int32_t k = narrow(place.size(1));
+        const int32_t *place_p = flat_or_null<const int32_t>(a[1], at::kInt, {T, k}, y.device());
+        const float *weights = flat_or_null<const float>(a[2], at::kFloat, {T, k}, y.device());
+        const at::ScalarType type = dtype_or(a[3], y.scalar_type());
+        const int out_code = float_code(type);
+        void *stream = stream_of(a[5]);
+        at::Tensor out = at::empty({T, r.cols}, y.options().dtype(type));
+        const void *y_p = y.data_ptr();
+        void *out_p = out.data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_combine(y_p, code, r.rows, r.cols, r.ld, place_p, weights, T, k, out_p, out_code, r.cols, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        return THPVariable_Wrap(std::move(out));
+    });
+}
+
+// (gradient, y, place, stream) -> weights_gradient
+PyObject *combine_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 4) throw NotUsual();
+        const at::Tensor &g = tensor(a[0]), &y = tensor(a[1]), &place = tensor(a[2]);
+        const int code = float_code(g.scalar_type()), y_code = float_code(y.scalar_type());
+        const Rows rg = rows_of(g), ry = rows_of(y);
+        if (place.dim() != 2 || rg.cols != ry.cols || g.device() != y.device()) throw NotUsual();
+        const int32_t k = narrow(place.size(1));
+        const int32_t *place_p = flat_or_null<const int32_t>(a[2], at::kInt, {rg.rows, k}, y.device());
+        void *stream = stream_of(a[3]);
+        at::Tensor out = at::empty({rg.rows, k}, y.options().dtype(at::kFloat));
+        const void *g_p = g.data_ptr(), *y_p = y.data_ptr();
+        float *out_p = static_cast<float *>(out.data_ptr());
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_combine_gradient(g_p, code, rg.ld, y_p, y_code, ry.rows, ry.cols, ry.ld, place_p, rg.rows, k, out_p, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        return THPVariable_Wrap(std::move(out));
+    });
+}
+
 // Tensors are read by the layout of the torch, and objects by that of the Python, that this was built with: with others it is an
 // ImportError, also where every symbol is found.
 bool built_for_these()
@@ -355,6 +708,13 @@ PyMethodDef methods[] = {
     {"encode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(encode)), METH_FASTCALL, nullptr},
     {"scan", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(scan)), METH_FASTCALL, nullptr},
     {"build_luts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(build_luts)), METH_FASTCALL, nullptr},
+    {"quantise_blocks", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(quantise_blocks)), METH_FASTCALL, nullptr},
+    {"block_product", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(block_product)), METH_FASTCALL, nullptr},
+    {"route", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(route)), METH_FASTCALL, nullptr},
+    {"route_gradient", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(route_gradient)), METH_FASTCALL, nullptr},
+    {"order", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(order)), METH_FASTCALL, nullptr},
+    {"combine", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(combine)), METH_FASTCALL, nullptr},
+    {"combine_gradient", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(combine_gradient)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 
@@ -370,6 +730,9 @@ PyMODINIT_FUNC PyInit_maddness_binding()
     s_C = PyUnicode_InternFromString("C");
     s_D = PyUnicode_InternFromString("D");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+    s_q = PyUnicode_InternFromString("q");
+    s_scale = PyUnicode_InternFromString("scale");
+    s_tile = PyUnicode_InternFromString("tile");
     if (!built_for_these()) return nullptr;
     PyObject *torch_c = PyImport_ImportModule("torch._C");
     if (!torch_c) return nullptr;

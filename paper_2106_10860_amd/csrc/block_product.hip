@@ -65,21 +65,66 @@ __device__ __forceinline__ void cut(Piece &p, int64_t kb, int group, int64_t K)
     p.hi = first_bytes(p.hi, K - k - 16);
 }
 
-// The same of a floating A, rounded here: the block's maximum is that of the four lanes that hold the row.
+// A lane's 32 elements of a floating row's block as they are in memory, in pieces of 8.  Pieces that would pass column K are read from K - 8
+// on instead (K >= 8), and moved into their place by round_piece.
 template <int DT>
-__device__ __forceinline__ Piece round_piece(const void *a, int64_t row_at, int64_t kb, int group, int64_t K)
+struct Raw {
+    uint32_t w[4][2 * elem_size(DT)];
+};
+
+template <int DT>
+__device__ __forceinline__ Raw<DT> load_raw(const void *a, int64_t row_at, int64_t kb, int group, int64_t K)
 {
+    struct __attribute__((packed, aligned(elem_size(DT)))) Words { uint32_t w[2 * elem_size(DT)]; };
+    Raw<DT> r;
     const int64_t k = kb * kBlock + group * 32;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const Words p = *reinterpret_cast<const Words *>(static_cast<const char *>(a) + (row_at + min(k + 8 * j, K - 8)) * elem_size(DT));
+#pragma unroll
+        for (int i = 0; i < 2 * elem_size(DT); ++i) r.w[j][i] = p.w[i];
+    }
+    return r;
+}
+
+// Rounds them; the block's maximum is that of the four lanes that hold the row.
+template <int DT>
+__device__ __forceinline__ Piece round_piece(const Raw<DT> &r, int64_t kb, int group, int64_t K)
+{
     float v[4][8];
     uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        load8<DT>(a, row_at + k + 8 * j, (int)max(min(K - k - 8 * j, (int64_t)8), (int64_t)0), v[j]);
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (DT == kF32) v[j][i] = __uint_as_float(r.w[j][i]);
+            else if constexpr (DT == kBF16) v[j][i] = __uint_as_float(i & 1 ? r.w[j][i / 2] & 0xffff0000u : r.w[j][i / 2] << 16);
+            else v[j][i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(r.w[j][i / 2] >> (i & 1 ? 16 : 0)));
+        }
+    if ((kb + 1) * kBlock > K) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t moved = kb * kBlock + group * 32 + 8 * j - (K - 8);      // the piece's first element is at this place of the 8
+            float in[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) in[i] = v[j][i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (moved > 0) v[j][i] = 0.0f;
+#pragma unroll
+                for (int from = i + 1; from < 8; ++from)
+                    if (from - i == moved) v[j][i] = in[from];
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = max(top, finite_magnitude(v[j][i]));
-    }
-    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    const auto rows = __builtin_amdgcn_permlane16_swap(top, top, false, false);
+    top = max(rows[0], rows[1]);
+    const auto halves = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+    top = max(halves[0], halves[1]);
     Piece p;
     p.byte = exponent_byte(top);
     const float inv = inverse_scale(p.byte);
@@ -133,7 +178,7 @@ template <int AT, int MT, int NT, int WAVES, int DEPTH, int OUT>
 __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, uint32_t col_tiles)
 {
     __shared__ f32x4 sums[WAVES][MT * NT][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r16 = lane % 16, g = lane / 16;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r16 = lane % 16, g = lane / 16;
     const int64_t n0 = (int64_t)(blockIdx.x % col_tiles) * (16 * NT);
     Part w;
     if (!find_part(p, 16 * MT, blockIdx.x / col_tiles, blockIdx.y, w)) return;
@@ -155,6 +200,7 @@ __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, 
     f32x4 acc[MT][NT] = {};
     for (int64_t kb0 = w.kb0 + wave; kb0 < w.kb1; kb0 += DEPTH * WAVES) {
         Piece b[DEPTH][NT], a[DEPTH][MT];
+        Raw<AT == kE4M3 ? kF32 : AT> raw[DEPTH][MT];
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
             const int64_t kb = min(kb0 + d * WAVES, w.kb1 - 1);
@@ -163,18 +209,22 @@ __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, 
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 if constexpr (AT == kE4M3) a[d][t] = load_piece(row_a[t], scale_a[t], kb, g, w.K);
-                else a[d][t] = round_piece<AT>(p.a, at_a[t], kb, g, w.K);
+                else raw[d][t] = load_raw<AT>(p.a, at_a[t], kb, g, w.K);
             }
         }
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
             const int64_t kb = kb0 + d * WAVES;
             if (kb >= w.kb1) break;
+            if constexpr (AT != kE4M3)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) a[d][t] = round_piece<AT>(raw[d][t], kb, g, w.K);
             if ((kb + 1) * kBlock > w.K) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) cut(b[d][t], kb, g, w.K);
+                if constexpr (AT == kE4M3)
 #pragma unroll
-                for (int t = 0; t < MT; ++t) cut(a[d][t], kb, g, w.K);
+                    for (int t = 0; t < MT; ++t) cut(a[d][t], kb, g, w.K);
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -400,7 +450,7 @@ int launch_few(const ProductArgs &p, hipStream_t stream)
     note_kernel("product_few_kernel", __PRETTY_FUNCTION__);
     if (small) hipLaunchKernelGGL((product_few_kernel<AT, 1, 1, WAVES, AT == kF32 ? 2 : 4, OUT>), grid, dim3(WAVES * 64), 0, stream, p, (uint32_t)col_tiles);
     else if constexpr (AT == kE4M3)
-        hipLaunchKernelGGL((product_few_kernel<AT, 4, 2, WAVES, 1, OUT>), grid, dim3(WAVES * 64), 0, stream, p, (uint32_t)col_tiles);
+        hipLaunchKernelGGL((product_few_kernel<AT, 4, 2, WAVES, 2, OUT>), grid, dim3(WAVES * 64), 0, stream, p, (uint32_t)col_tiles);
     return check_hip(hipGetLastError(), "launch product_few_kernel");
 }
 
@@ -420,7 +470,7 @@ int launch_to(const ProductArgs &p, int a_dtype, hipStream_t stream)
 
 }  // namespace
 
-bool rounds_inside(int64_t M, int64_t N, int64_t K, int groups, int by) { return by == MADDNESS_DENSE && M <= 16; }
+bool rounds_inside(int64_t M, int64_t N, int64_t K, int groups, int by) { return by == MADDNESS_DENSE && M <= 16 && K >= 8; }
 
 int launch_block_product(const ProductArgs &p, int a_dtype, int out_dtype, hipStream_t stream)
 {

@@ -239,3 +239,41 @@ def test_example_learns(mad):
     losses = train_example()
     print("losses", losses[::10], flush=True)
     assert losses[-1] < 0.5 * losses[0]
+
+
+def test_calls_without_the_native_marshalling_give_the_same(mad, monkeypatch):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(3)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda")      # noqa: E731
+    x, logits, bias, weight, grad = r(50, 200).bfloat16(), r(50, 24), 0.1 * r(24), r(24, 70, 200), r(50, 70).bfloat16()
+    side = torch.cuda.Stream()
+
+    def all_calls():
+        seen = []
+        W, Wt = mad.maddness_quantise_blocks(weight, 128, both=True)
+        for stream in (None, side):
+            torch.cuda.synchronize()
+            ids, w = mad.maddness_route(logits, 3, "sigmoid", bias, 4, 2, True, 2.0, stream=stream)
+            offsets, counts, source, place = mad.maddness_order(ids, 24, 128, stream=stream)
+            a, at = mad.maddness_quantise_blocks(x, both=True, source=source, repeat=3, factors=w, stream=stream)
+            one = mad.maddness_quantise_blocks(x, transposed=True, stream=stream)
+            y = mad.maddness_block_product(a, W, offsets, out_dtype=torch.float32, stream=stream)
+            torch.cuda.synchronize()
+            y = torch.where((source >= 0)[:, None], y, 0)      # (rows that no expert has are not written)
+            torch.cuda.synchronize()
+            d = mad.maddness_block_product(at, at, offsets, by="depth", stream=stream)
+            few = mad.maddness_block_product(x[:3], mad.BlockMatrix(W.q[0], W.scale[0], 128), stream=stream)
+            many = mad.maddness_block_product(x, mad.BlockMatrix(W.q[0], W.scale[0], 128), out=torch.zeros(50, 70, device="cuda"), stream=stream)
+            out = mad.maddness_combine(y, place, w, out_dtype=torch.bfloat16, stream=stream)
+            dw = mad.maddness_combine_gradient(grad, y, place, stream=stream)
+            dl = mad.maddness_route_gradient(logits, ids, dw, "sigmoid", True, 2.0, stream=stream)
+            torch.cuda.synchronize()
+            seen += [ids, w, offsets, counts, source, place, a.values(), at.values(), one.values(), y, d, few, many, out, dw, dl]
+        return seen
+
+    native = all_calls()
+    assert mad._native.__name__ == "maddness_binding"
+    monkeypatch.setattr(mad, "_native", mad._NotBuilt)
+    plain = all_calls()
+    for i, (a, b) in enumerate(zip(native, plain)):
+        assert a.dtype is b.dtype and torch.equal(a, b), i
