@@ -365,17 +365,19 @@ int maddness_quantise_blocks(const void *x, int32_t dtype, int64_t count, int64_
  * offsets NULL, or [groups + 1] on the device, not decreasing.  One outside the matrix is cut back to it, and for
  *         MADDNESS_BY_DEPTH one that is no multiple of 128 is rounded down to one, so a wrong array gives wrong sums
  *         but no bad access.
+ * source  NULL, or [slots] on the device (MADDNESS_BY_ROWS only): out has `slots` rows, and row r is that of A's row
+ *         source[r] / repeat; rows whose source is outside [0, A's rows times repeat) are not written.
  * A       MADDNESS_E4M3, or F32 / F16 / BF16 (not for MADDNESS_BY_DEPTH): then its rows are rounded as
  *         maddness_quantise_blocks does with tile 1; data aligned to its element, scale ignored.
- * workspace  maddness_block_product_workspace(M, N, K, groups, by, dtype of A) bytes, 16-byte aligned (NULL where
+ * workspace  maddness_block_product_workspace(A's rows, K, by, dtype of A) bytes, 16-byte aligned (NULL where
  *         that is 0); contents undefined afterwards.
  * M = 0 and N = 0 are valid; K = 0 gives zeros.  M, N, K < 2^31.
  */
 typedef enum { MADDNESS_DENSE = 0, MADDNESS_BY_ROWS = 1, MADDNESS_BY_DEPTH = 2 } maddness_product_groups;
 
-size_t maddness_block_product_workspace(int64_t M, int64_t N, int64_t K, int32_t groups, int32_t by, int32_t a_dtype);
+size_t maddness_block_product_workspace(int64_t a_rows, int64_t K, int32_t by, int32_t a_dtype);
 int maddness_block_product(const maddness_block_matrix *A, const maddness_block_matrix *B, int32_t by, int32_t groups,
-                           const int32_t *offsets, void *out, int32_t out_dtype, int64_t ldo, void *workspace,
+                           const int32_t *offsets, const int32_t *source, int64_t slots, int32_t repeat, void *out, int32_t out_dtype, int64_t ldo, void *workspace,
                            size_t workspace_bytes, void *stream);
 
 /*

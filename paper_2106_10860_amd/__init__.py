@@ -108,9 +108,9 @@ def lib() -> C.CDLL:
         L.maddness_learn_prototypes.argtypes = [vp, vp, i64, i64, i32, i32, vp, i32, C.c_double, vp, vp, sz, vp]
         L.maddness_quantise_blocks.argtypes = [vp, i32, i64, i64, i64, i64, i64, i32, vp, i64, i32, vp, vp, i64, vp, i64, vp, i64,
                                                vp, i64, vp]
-        L.maddness_block_product_workspace.argtypes = [i64, i64, i64, i32, i32, i32]
+        L.maddness_block_product_workspace.argtypes = [i64, i64, i32, i32]
         L.maddness_block_product_workspace.restype = sz
-        L.maddness_block_product.argtypes = [C.POINTER(_BlockMatrix), C.POINTER(_BlockMatrix), i32, i32, vp, vp, i32, i64, vp, sz, vp]
+        L.maddness_block_product.argtypes = [C.POINTER(_BlockMatrix), C.POINTER(_BlockMatrix), i32, i32, vp, vp, i64, i32, vp, i32, i64, vp, sz, vp]
         L.maddness_route.argtypes = [vp, i32, i64, i32, i64, vp, i32, i32, i32, i32, i32, C.c_float, vp, vp, vp]
         L.maddness_route_gradient.argtypes = [vp, i32, i64, i32, i64, i32, i32, i32, C.c_float, vp, vp, vp, i64, vp]
         L.maddness_order_capacity.argtypes = [i64, i32, i32]

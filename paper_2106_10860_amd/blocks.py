@@ -176,17 +176,20 @@ def maddness_quantise_blocks(x, tile: int = 1, transposed: bool = False, both: b
     return (a, b) if both else (b if transposed else a)
 
 
-def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", out_dtype=None, out=None, workspace=None, stream=None):
+def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", source=None, repeat: int = 1, out_dtype=None, out=None, workspace=None, stream=None):
     """A @ B.T.  A: a BlockMatrix or a float tensor [M, K]; B: a BlockMatrix [N, K].
 
     With ``offsets`` (int32 [experts + 1]) by experts: by="rows" multiplies rows offsets[e] .. offsets[e + 1] - 1 of A with B[e]
     (B [experts, N, K]) into out [M, N], rows that no expert has are left as they are; by="depth" gives out [experts, M, N] from the
-    columns offsets[e] .. offsets[e + 1] - 1 of A [M, K] and B [N, K] (multiples of 128)."""
+    columns offsets[e] .. offsets[e + 1] - 1 of A [M, K] and B [N, K] (multiples of 128).
+
+    With ``source`` (int32 [slots], by="rows") out is [slots, N] and its row r that of A's row source[r] // repeat; rows whose source is
+    negative are left as they are."""
     if not isinstance(B, BlockMatrix):
         raise TypeError("B must be a BlockMatrix")
     if by != "rows" and by != "depth":
         raise ValueError(f"by must be 'rows' or 'depth', is {by!r}")
-    r = _m._native.block_product(isinstance(A, BlockMatrix), A, B, offsets, by == "depth", out_dtype, out, workspace, stream)
+    r = _m._native.block_product(isinstance(A, BlockMatrix), A, B, offsets, by == "depth", source, repeat, out_dtype, out, workspace, stream)
     if r is not NotImplemented:
         return _m._done(r)
     torch = _m._torch or _m._torch_module()
@@ -198,7 +201,12 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", ou
         a_dtype = _code(A, "A")
         M, K, lda = _m._rows(A, "A")
         a, device = _m._BlockMatrix(A.data_ptr(), a_dtype, 1, M, K, lda, 0, None, 0, 0), A.device
-    N = B.shape[-2]
+    N, a_rows, source_p = B.shape[-2], M, None
+    if source is not None:
+        if offsets is None or by != "rows" or source.dim() != 1 or repeat < 1:
+            raise ValueError("source must be 1-D, with offsets, by='rows' and repeat >= 1")
+        M = source.shape[0]
+        source_p = _flat(source, torch.int32, (M,), "source")
     if offsets is None:
         how, groups, offsets_p, lead = MADDNESS_DENSE, 1, None, ()
         if len(B.shape) != 2:
@@ -219,13 +227,13 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", ou
         raise ValueError(f"out must have shape {(*lead, M, N)}{'' if out_dtype is None else f' and dtype {out_dtype}'}")
     elif lead and not out.is_contiguous():
         raise ValueError("out must be contiguous")
-    _same_device(B.q, out, offsets, A.q if isinstance(A, BlockMatrix) else A, workspace)
+    _same_device(B.q, out, offsets, source, A.q if isinstance(A, BlockMatrix) else A, workspace)
     ldo = _m._rows(out.view(-1, N) if lead and N else out[0] if lead else out, "out")[2]
     L = _m.lib()
-    need = L.maddness_block_product_workspace(M, N, K, groups, how, a_dtype) if a_dtype != MADDNESS_E4M3 else 0
+    need = L.maddness_block_product_workspace(a_rows, K, how, a_dtype) if a_dtype != MADDNESS_E4M3 else 0
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    _m._check(L.maddness_block_product(C.byref(a), C.byref(B._struct), how, groups, offsets_p, out.data_ptr(), _code(out, "out"), ldo,
+    _m._check(L.maddness_block_product(C.byref(a), C.byref(B._struct), how, groups, offsets_p, source_p, M, repeat, out.data_ptr(), _code(out, "out"), ldo,
                                        _m._ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(),
                                        _m._stream(stream)))
     return out

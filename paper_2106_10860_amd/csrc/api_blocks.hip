@@ -112,14 +112,15 @@ int maddness_quantise_blocks(const void *x, int32_t dtype, int64_t count, int64_
                                   ldq, scale, lds, qt, ldqt, scale_t, ldst, static_cast<hipStream_t>(stream));
 }
 
-size_t maddness_block_product_workspace(int64_t M, int64_t N, int64_t K, int32_t groups, int32_t by, int32_t a_dtype)
+size_t maddness_block_product_workspace(int64_t a_rows, int64_t K, int32_t by, int32_t a_dtype)
 {
-    if (M < 1 || K < 1 || N < 1 || a_dtype == kE4M3 || rounds_inside(M, N, K, groups, by)) return 0;
-    return (size_t)Rounded(M, K).bytes;
+    if (a_rows < 1 || K < 1 || a_dtype == kE4M3 || rounds_inside(a_rows, K, by)) return 0;
+    return (size_t)Rounded(a_rows, K).bytes;
 }
 
 int maddness_block_product(const maddness_block_matrix *A, const maddness_block_matrix *B, int32_t by, int32_t groups, const int32_t *offsets,
-                           void *out, int32_t out_dtype, int64_t ldo, void *workspace, size_t workspace_bytes, void *stream)
+                           const int32_t *source, int64_t slots, int32_t repeat, void *out, int32_t out_dtype, int64_t ldo, void *workspace,
+                           size_t workspace_bytes, void *stream)
 {
     begin_call();
     if (by < MADDNESS_DENSE || by > MADDNESS_BY_DEPTH) return fail(MADDNESS_E_INVAL, "by = %d is not a maddness_product_groups", by);
@@ -127,7 +128,14 @@ int maddness_block_product(const maddness_block_matrix *A, const maddness_block_
     if ((rc = check_matrix(A, by != MADDNESS_BY_DEPTH, "A")) != MADDNESS_OK || (rc = check_matrix(B, false, "B")) != MADDNESS_OK) return rc;
     if (A->cols != B->cols) return fail(MADDNESS_E_INVAL, "A has %lld columns and B %lld", (long long)A->cols, (long long)B->cols);
     if (!floating(out_dtype)) return fail(MADDNESS_E_INVAL, "out: dtype = %d is not F32, F16 or BF16", out_dtype);
-    const int64_t M = A->rows, N = B->rows, K = A->cols;
+    if (source) {
+        if (by != MADDNESS_BY_ROWS) return fail(MADDNESS_E_INVAL, "source goes with MADDNESS_BY_ROWS");
+        if (repeat < 1) return fail(MADDNESS_E_INVAL, "repeat = %d, must be >= 1", repeat);
+        if ((rc = check_size(slots, "slots")) != MADDNESS_OK) return rc;
+        if (A->rows * repeat > kMostRows) return fail(MADDNESS_E_UNSUPPORTED, "A's rows times repeat = %lld, supported are up to 2^31 - 1", (long long)(A->rows * repeat));
+        if (!aligned(source, 4)) return fail(MADDNESS_E_ALIGN, "source not 4-byte aligned");
+    }
+    const int64_t M = source ? slots : A->rows, N = B->rows, K = A->cols;
     if (by == MADDNESS_DENSE) {
         groups = 1;
     } else {
@@ -137,7 +145,7 @@ int maddness_block_product(const maddness_block_matrix *A, const maddness_block_
         if (!aligned(offsets, 4)) return fail(MADDNESS_E_ALIGN, "offsets not 4-byte aligned");
         if (by == MADDNESS_BY_DEPTH && K > 0 && (A->tile != 1 || B->tile != 1)) return fail(MADDNESS_E_INVAL, "A and B must have tile 1 to be cut by depth");
     }
-    if (M == 0 || N == 0) return MADDNESS_OK;
+    if (M == 0 || N == 0 || (source && A->rows == 0)) return MADDNESS_OK;
     if ((rc = check_floats(out, out_dtype, M, N, ldo, "out")) != MADDNESS_OK) return rc;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     ProductArgs p{};
@@ -145,17 +153,18 @@ int maddness_block_product(const maddness_block_matrix *A, const maddness_block_
     p.b = static_cast<const uint8_t *>(B->data); p.ldb = B->ld; p.stride_b = B->stride;
     p.scale_a = A->scale; p.lds_a = A->lds; p.shift_a = A->tile == kBlock ? 7 : 0;
     p.scale_b = B->scale; p.lds_b = B->lds; p.scale_stride_b = B->scale_stride; p.shift_b = B->tile == kBlock ? 7 : 0;
-    p.M = M; p.N = N; p.K = K; p.by = by; p.groups = groups; p.offsets = offsets;
+    p.M = M; p.N = N; p.K = K; p.a_rows = A->rows; p.by = by; p.groups = groups; p.offsets = offsets;
+    p.source = source; p.source_limit = source ? A->rows * repeat : 0; p.repeat = source ? repeat : 1;
     p.out = out; p.ldo = ldo; p.out_stride = M * ldo;
     int a_dtype = A->dtype;
-    if (a_dtype != kE4M3 && !rounds_inside(M, N, K, groups, by)) {
+    if (a_dtype != kE4M3 && !rounds_inside(A->rows, K, by)) {
         if (K > 0) {
-            const Rounded r(M, K);
+            const Rounded r(A->rows, K);
             if (!workspace || workspace_bytes < (size_t)r.bytes)
                 return fail(MADDNESS_E_UNSUPPORTED, "workspace of %zu bytes given, %lld needed", workspace_bytes, (long long)r.bytes);
             if (!aligned(workspace, 16)) return fail(MADDNESS_E_ALIGN, "workspace not 16-byte aligned");
             uint8_t *q = static_cast<uint8_t *>(workspace), *scale = q + r.scale_at;
-            rc = launch_quantise_blocks(A->data, a_dtype, 1, M, K, A->ld, 0, 1, nullptr, 0, 1, nullptr, q, r.ld, scale, r.lds, nullptr, 0, nullptr, 0, s);
+            rc = launch_quantise_blocks(A->data, a_dtype, 1, A->rows, K, A->ld, 0, 1, nullptr, 0, 1, nullptr, q, r.ld, scale, r.lds, nullptr, 0, nullptr, 0, s);
             if (rc != MADDNESS_OK) return rc;
             p.a = q; p.lda = r.ld; p.scale_a = scale; p.lds_a = r.lds; p.shift_a = 0;
         }

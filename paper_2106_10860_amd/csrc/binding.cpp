@@ -462,11 +462,11 @@ PyObject *quantise_blocks(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (a_is_blocks, A, B, offsets, by_depth, out_dtype, out, workspace, stream) -> out
+// (a_is_blocks, A, B, offsets, by_depth, source, repeat, out_dtype, out, workspace, stream) -> out
 PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
-        if (n != 9) throw NotUsual();
+        if (n != 11) throw NotUsual();
         at::Device device(at::kCPU);
         maddness_block_matrix A{}, B{};
         int64_t experts = -1;
@@ -498,46 +498,55 @@ PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
         } else if (experts != -1) {
             throw NotUsual();
         }
-        void *stream = stream_of(a[8]);
+        int64_t rows = A.rows;
+        const int32_t repeat = narrow(whole(a[6])), *source = nullptr;
+        if (a[5] != Py_None) {
+            const at::Tensor &s = tensor(a[5]);
+            if (by != MADDNESS_BY_ROWS || s.dim() != 1 || s.scalar_type() != at::kInt || !s.is_contiguous() || s.device() != device || repeat < 1)
+                throw NotUsual();
+            rows = s.size(0);
+            source = static_cast<const int32_t *>(s.data_ptr());
+        }
+        void *stream = stream_of(a[10]);
         at::Tensor made, work;
-        const at::ScalarType type = dtype_or(a[5], at::kBFloat16);
+        const at::ScalarType type = dtype_or(a[7], at::kBFloat16);
         void *out;
         int64_t ldo;
         int code;
-        if (a[6] == Py_None) {
+        if (a[8] == Py_None) {
             code = float_code(type);
             const auto opt = at::TensorOptions().dtype(type).device(device);
-            made = by == MADDNESS_BY_DEPTH ? at::empty({groups, A.rows, B.rows}, opt) : at::empty({A.rows, B.rows}, opt);
+            made = by == MADDNESS_BY_DEPTH ? at::empty({groups, A.rows, B.rows}, opt) : at::empty({rows, B.rows}, opt);
             out = made.data_ptr();
             ldo = std::max(B.rows, (int64_t)1);
         } else {
-            const at::Tensor &o = tensor(a[6]);
-            if (by == MADDNESS_BY_DEPTH || o.device() != device || (a[5] != Py_None && o.scalar_type() != type)) throw NotUsual();
+            const at::Tensor &o = tensor(a[8]);
+            if (by == MADDNESS_BY_DEPTH || o.device() != device || (a[7] != Py_None && o.scalar_type() != type)) throw NotUsual();
             const Rows r = rows_of(o);
-            if (r.rows != A.rows || r.cols != B.rows) throw NotUsual();
+            if (r.rows != rows || r.cols != B.rows) throw NotUsual();
             code = float_code(o.scalar_type());
             out = o.data_ptr();
             ldo = r.ld;
         }
         void *work_p = nullptr;
         size_t work_bytes = 0;
-        if (a[7] != Py_None) {
-            const at::Tensor &w = tensor(a[7]);
+        if (a[9] != Py_None) {
+            const at::Tensor &w = tensor(a[9]);
             if (w.scalar_type() != at::kByte || w.device() != device) throw NotUsual();
             work_p = w.data_ptr();
             work_bytes = (size_t)w.numel();
-        } else if ((work_bytes = maddness_block_product_workspace(A.rows, B.rows, A.cols, groups, by, A.dtype))) {
+        } else if ((work_bytes = maddness_block_product_workspace(A.rows, A.cols, by, A.dtype))) {
             work = at::empty({(int64_t)work_bytes}, at::TensorOptions().dtype(at::kByte).device(device));
             work_p = work.data_ptr();
         }
         int rc;
         Py_BEGIN_ALLOW_THREADS
-        rc = maddness_block_product(&A, &B, by, groups, offsets, out, code, ldo, work_p, work_bytes, stream);
+        rc = maddness_block_product(&A, &B, by, groups, offsets, source, rows, repeat, out, code, ldo, work_p, work_bytes, stream);
         Py_END_ALLOW_THREADS
         if (rc != MADDNESS_OK) return int_status(rc);
         if (made.defined()) return THPVariable_Wrap(std::move(made));
-        Py_INCREF(a[6]);
-        return a[6];
+        Py_INCREF(a[8]);
+        return a[8];
     });
 }
 

@@ -18,23 +18,50 @@ __host__ __device__ constexpr T ceil_div(T a, T b) { return (a + b - 1) / b; }
 template <typename T>
 __host__ __device__ constexpr T round_up(T a, T b) { return ceil_div(a, b) * b; }
 
-// Eight consecutive elements (any alignment to the element), widened; those from `n` on are 0.
+// Eight consecutive elements of a row of n, from column c on, as they are in memory (any alignment to the element).  A piece that would pass the
+// row's end is read from n - 8 on instead (n >= 8), and moved into its place by widen: no branch, so that many can be on their way.
 template <int DT>
-__device__ __forceinline__ void load8(const void *base, int64_t at, int n, float (&v)[8])
+struct __attribute__((packed, aligned(elem_size(DT)))) Raw {
+    uint32_t w[2 * elem_size(DT)];
+};
+
+template <int DT>
+__device__ __forceinline__ Raw<DT> load_raw(const void *x, int64_t row_at, int64_t c, int64_t n)
 {
-    if (n >= 8) {
-        struct __attribute__((packed, aligned(elem_size(DT)))) Piece { uint32_t w[2 * elem_size(DT)]; };
-        const Piece p = *reinterpret_cast<const Piece *>(static_cast<const char *>(base) + at * elem_size(DT));
+    return *reinterpret_cast<const Raw<DT> *>(static_cast<const char *>(x) + (row_at + min(c, n - 8)) * elem_size(DT));
+}
+
+// Widened; those from column n on are 0.
+template <int DT>
+__device__ __forceinline__ void widen(const Raw<DT> &r, int64_t c, int64_t n, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (DT == kF32) v[i] = __uint_as_float(r.w[i]);
+        else if constexpr (DT == kBF16) v[i] = __uint_as_float(i & 1 ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16);
+        else v[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(r.w[i / 2] >> (i & 1 ? 16 : 0)));
+    }
+    const int64_t moved = c - (n - 8);                       // the piece's first element is at this place of the 8
+    if (moved > 0) {
+        float in[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) in[i] = v[i];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if constexpr (DT == kF32) v[i] = __uint_as_float(p.w[i]);
-            else if constexpr (DT == kBF16) v[i] = __uint_as_float(i & 1 ? p.w[i / 2] & 0xffff0000u : p.w[i / 2] << 16);
-            else v[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(p.w[i / 2] >> (i & 1 ? 16 : 0)));
-        }
-    } else {
+            v[i] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? widen_at<DT>(base, at + i) : 0.0f;
+            for (int from = i + 1; from < 8; ++from)
+                if (from - i == moved) v[i] = in[from];
+        }
     }
+}
+
+// The same of a row of fewer than 8.
+template <int DT>
+__device__ __forceinline__ void load_short(const void *x, int64_t row_at, int64_t c, int64_t n, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i < n ? widen_at<DT>(x, row_at + c + i) : 0.0f;
 }
 
 // |x| of a finite x as bits (they order as the numbers do), 0 for NaN and the infinities.
@@ -114,55 +141,59 @@ __device__ __forceinline__ int64_t offset_at(const int32_t *offsets, int e, int6
     return min(max((int64_t)offsets[e], (int64_t)0), limit);
 }
 
-// Every expert's rows are cut into pieces of their own, `rows` rows each: lane l gets the bounds lo, hi of expert e0 + l's rows, the
-// number of its pieces and that of the pieces up to and with them.
-__device__ __forceinline__ void pieces_of(const int32_t *offsets, int groups, int64_t limit, int rows, int e0, int &lo, int &hi, int &mine, int &upto)
-{
-    const int lane = threadIdx.x & 63, e = e0 + lane;
-    lo = e < groups ? (int)offset_at(offsets, e, limit) : 0;              // (limit < 2^31)
-    hi = e < groups ? (int)offset_at(offsets, e + 1, limit) : 0;
-    mine = hi > lo ? ceil_div((int64_t)hi - lo, (int64_t)rows) : 0;
-    upto = mine;
+// Every expert's rows are cut into pieces of their own, `rows` rows each, and the pieces are numbered through.  All lanes of a wavefront
+// call count (how many there are; not needed before find) and find with the same arguments.
+struct PieceSearch {
+    int e0 = -1;                    // lane l holds expert e0 + l:
+    int lo, hi, mine, upto;         // its rows' bounds, the number of its pieces, and of those from e0's up to and with them
+
+    __device__ __forceinline__ void look(const int32_t *offsets, int groups, int64_t limit, int rows, int from)
+    {
+        if (e0 == from) return;
+        e0 = from;
+        const int lane = threadIdx.x & 63, e = e0 + lane;
+        lo = e < groups ? (int)offset_at(offsets, e, limit) : 0;              // (limit < 2^31)
+        hi = e < groups ? (int)offset_at(offsets, e + 1, limit) : 0;
+        mine = hi > lo ? (int)ceil_div((uint32_t)(hi - lo), (uint32_t)rows) : 0;
+        upto = mine;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
-    }
-}
-
-__device__ __forceinline__ int64_t count_pieces(const int32_t *offsets, int groups, int64_t limit, int rows)
-{
-    int64_t all = 0;
-    for (int e0 = 0; e0 < groups; e0 += 64) {
-        int lo, hi, mine, upto;
-        pieces_of(offsets, groups, limit, rows, e0, lo, hi, mine, upto);
-        all += __builtin_amdgcn_readlane(upto, 63);
-    }
-    return all;
-}
-
-// The piece with index `piece`: its expert, or -1 where there are fewer; first and one-past-last row.  Every lane of a wavefront calls
-// it with the same piece.
-__device__ __forceinline__ int find_piece(const int32_t *offsets, int groups, int64_t limit, int rows, int64_t piece, int64_t &first, int64_t &last)
-{
-    int64_t before = 0;
-    for (int e0 = 0; e0 < groups; e0 += 64) {
-        int lo, hi, mine, upto;
-        pieces_of(offsets, groups, limit, rows, e0, lo, hi, mine, upto);
-        const int64_t at = piece - before;
-        const uint64_t has = __ballot(at < upto && at >= upto - mine);
-        if (has) {
-            const int l = __ffsll((unsigned long long)has) - 1;
-            const int begin = __builtin_amdgcn_readlane(upto - mine, l);
-            const int64_t low = __builtin_amdgcn_readlane(lo, l), high = __builtin_amdgcn_readlane(hi, l);
-            first = low + (at - begin) * rows;
-            last = min(first + rows, high);
-            return e0 + l;
+        for (int d = 1; d < 64; d *= 2) {
+            const int o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
         }
-        before += __builtin_amdgcn_readlane(upto, 63);
     }
-    return -1;
-}
+
+    __device__ __forceinline__ int64_t count(const int32_t *offsets, int groups, int64_t limit, int rows)
+    {
+        int64_t all = 0;
+        for (int from = 0; from < groups; from += 64) {
+            look(offsets, groups, limit, rows, from);
+            all += __builtin_amdgcn_readlane(upto, 63);
+        }
+        return all;
+    }
+
+    // The expert of piece `piece`, or -1 where there are fewer; first and one-past-last row.
+    __device__ __forceinline__ int find(const int32_t *offsets, int groups, int64_t limit, int rows, int64_t piece, int64_t &first, int64_t &last)
+    {
+        int64_t before = 0;
+        for (int from = 0; from < groups; from += 64) {
+            look(offsets, groups, limit, rows, from);
+            const int64_t at = piece - before;
+            const uint64_t has = __ballot(at < upto && at >= upto - mine);
+            if (has) {
+                const int l = __ffsll((unsigned long long)has) - 1;
+                const int begin = __builtin_amdgcn_readlane(upto - mine, l);
+                const int64_t low = __builtin_amdgcn_readlane(lo, l), high = __builtin_amdgcn_readlane(hi, l);
+                first = low + (at - begin) * rows;
+                last = min(first + rows, high);
+                return from + l;
+            }
+            before += __builtin_amdgcn_readlane(upto, 63);
+        }
+        return -1;
+    }
+};
 
 // Arguments of a product, as the launchers hand them on.
 struct ProductArgs {
@@ -171,9 +202,12 @@ struct ProductArgs {
     int64_t lda, ldb, lds_a, lds_b;
     int64_t stride_b, scale_stride_b;  // between experts
     int shift_a, shift_b;              // row -> row of exponents: 0 or 7
-    int64_t M, N, K;
+    int64_t M, N, K, a_rows;           // (M: rows of out; of A where source is NULL)
     int by, groups;
     const int32_t *offsets;
+    const int32_t *source;             // of each row of out: a slot, whose row of A is slot / repeat; NULL: rows as they are
+    int64_t source_limit;              // a_rows * repeat
+    int repeat;
     void *out;
     int64_t ldo, out_stride;
 };
@@ -184,8 +218,8 @@ int launch_quantise_blocks(const void *x, int dtype, int64_t count, int64_t rows
 
 // a_dtype: kE4M3, or a floating type that the kernel rounds by itself (rounds_inside).
 int launch_block_product(const ProductArgs &p, int a_dtype, int out_dtype, hipStream_t stream);
-// Whether a product of this size rounds a floating A inside its kernel; otherwise A is rounded into the workspace before.
-bool rounds_inside(int64_t M, int64_t N, int64_t K, int groups, int by);
+// Whether a product with a floating A of M rows rounds it inside its kernel; otherwise A is rounded into the workspace before.
+bool rounds_inside(int64_t M, int64_t K, int by);
 
 int launch_route(const void *logits, int dtype, int64_t T, int E, int64_t ldl, const float *bias, int scores, int groups, int kept, int k,
                  bool renormalise, float factor, int32_t *ids, float *weights, hipStream_t stream);

@@ -65,79 +65,9 @@ __device__ __forceinline__ void cut(Piece &p, int64_t kb, int group, int64_t K)
     p.hi = first_bytes(p.hi, K - k - 16);
 }
 
-// A lane's 32 elements of a floating row's block as they are in memory, in pieces of 8.  Pieces that would pass column K are read from K - 8
-// on instead (K >= 8), and moved into their place by round_piece.
-template <int DT>
-struct Raw {
-    uint32_t w[4][2 * elem_size(DT)];
-};
-
-template <int DT>
-__device__ __forceinline__ Raw<DT> load_raw(const void *a, int64_t row_at, int64_t kb, int group, int64_t K)
-{
-    struct __attribute__((packed, aligned(elem_size(DT)))) Words { uint32_t w[2 * elem_size(DT)]; };
-    Raw<DT> r;
-    const int64_t k = kb * kBlock + group * 32;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const Words p = *reinterpret_cast<const Words *>(static_cast<const char *>(a) + (row_at + min(k + 8 * j, K - 8)) * elem_size(DT));
-#pragma unroll
-        for (int i = 0; i < 2 * elem_size(DT); ++i) r.w[j][i] = p.w[i];
-    }
-    return r;
-}
-
-// Rounds them; the block's maximum is that of the four lanes that hold the row.
-template <int DT>
-__device__ __forceinline__ Piece round_piece(const Raw<DT> &r, int64_t kb, int group, int64_t K)
-{
-    float v[4][8];
-    uint32_t top = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (DT == kF32) v[j][i] = __uint_as_float(r.w[j][i]);
-            else if constexpr (DT == kBF16) v[j][i] = __uint_as_float(i & 1 ? r.w[j][i / 2] & 0xffff0000u : r.w[j][i / 2] << 16);
-            else v[j][i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(r.w[j][i / 2] >> (i & 1 ? 16 : 0)));
-        }
-    if ((kb + 1) * kBlock > K) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t moved = kb * kBlock + group * 32 + 8 * j - (K - 8);      // the piece's first element is at this place of the 8
-            float in[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) in[i] = v[j][i];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (moved > 0) v[j][i] = 0.0f;
-#pragma unroll
-                for (int from = i + 1; from < 8; ++from)
-                    if (from - i == moved) v[j][i] = in[from];
-            }
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, finite_magnitude(v[j][i]));
-    const auto rows = __builtin_amdgcn_permlane16_swap(top, top, false, false);
-    top = max(rows[0], rows[1]);
-    const auto halves = __builtin_amdgcn_permlane32_swap(top, top, false, false);
-    top = max(halves[0], halves[1]);
-    Piece p;
-    p.byte = exponent_byte(top);
-    const float inv = inverse_scale(p.byte);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[j][i] = scaled(v[j][i], inv);
-        const int lo = (int)pack4(v[j][0], v[j][1], v[j][2], v[j][3]), hi = (int)pack4(v[j][4], v[j][5], v[j][6], v[j][7]);
-        if (j < 2) { p.lo[2 * j] = lo; p.lo[2 * j + 1] = hi; }
-        else { p.hi[2 * j - 4] = lo; p.hi[2 * j - 3] = hi; }
-    }
-    return p;
-}
+// Whether A's rows are rounded within the few-rows kernel, by every workgroup for itself: while they fill 32 KiB of LDS at most, which costs a
+// workgroup up to 64 values a thread (1.5 us), a launch of their own costs 5 us.
+constexpr int64_t kInside = 32768, kInsideRows = 64;
 
 // What a workgroup computes: rows first .. last - 1 of A, with one expert's matrix, over the blocks kb0 .. kb1 - 1.
 struct Part {
@@ -146,7 +76,7 @@ struct Part {
     int64_t out_at;
 };
 
-__device__ __forceinline__ bool find_part(const ProductArgs &p, int rows, int64_t piece, int64_t group, Part &w)
+__device__ __forceinline__ bool find_part(const ProductArgs &p, PieceSearch &search, int rows, int64_t piece, int64_t group, Part &w)
 {
     w.b = p.b;
     w.scale_b = p.scale_b;
@@ -154,7 +84,7 @@ __device__ __forceinline__ bool find_part(const ProductArgs &p, int rows, int64_
     w.K = p.K;
     w.kb0 = 0;
     if (p.by == MADDNESS_BY_ROWS) {
-        const int e = find_piece(p.offsets, p.groups, p.M, rows, piece, w.first, w.last);
+        const int e = search.find(p.offsets, p.groups, p.M, rows, piece, w.first, w.last);
         if (e < 0) return false;
         w.b += e * p.stride_b;
         w.scale_b += e * p.scale_stride_b;
@@ -172,59 +102,96 @@ __device__ __forceinline__ bool find_part(const ProductArgs &p, int rows, int64_
     return true;
 }
 
+// Row m of the product's A: itself, or that of the slot's token; -1 where there is none.
+__device__ __forceinline__ int64_t row_of_a(const ProductArgs &p, int64_t m)
+{
+    if (!p.source) return m;
+    const int s = p.source[m];
+    return s < 0 || s >= p.source_limit ? -1 : s / p.repeat;
+}
+
 // Few rows: 16 MT rows by 16 NT columns to a workgroup; its wavefronts take every WAVES-th block of the sum, DEPTH of them asked for
-// at once, and add up in LDS, in their order.  Operands come straight from memory, in pieces of 32 bytes to a lane.
+// at once, and add up in LDS, in their order.  B comes straight from memory, in pieces of 32 bytes to a lane, and so does an 8-bit A; a floating
+// A is rounded into LDS while the first of B is on its way.
 template <int AT, int MT, int NT, int WAVES, int DEPTH, int OUT>
 __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, uint32_t col_tiles)
 {
+    constexpr bool ROUND = AT != kE4M3;
     __shared__ f32x4 sums[WAVES][MT * NT][64];
+    __shared__ __attribute__((aligned(16))) uint8_t rounded[ROUND ? kInside + kInsideRows * 16 : 16], bytes[ROUND ? kInside / kBlock + kInsideRows : 16];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r16 = lane % 16, g = lane / 16;
     const int64_t n0 = (int64_t)(blockIdx.x % col_tiles) * (16 * NT);
     Part w;
-    if (!find_part(p, 16 * MT, blockIdx.x / col_tiles, blockIdx.y, w)) return;
+    PieceSearch search;
+    if (!find_part(p, search, 16 * MT, blockIdx.x / col_tiles, blockIdx.y, w)) return;
     const uint8_t *row_b[NT], *row_a[MT], *scale_a[MT], *scale_b[NT];
-    int64_t at_a[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int64_t m = min(w.first + t * 16 + r16, w.last - 1);
-        at_a[t] = m * p.lda;
-        row_a[t] = p.a + (AT == kE4M3 ? at_a[t] : 0);
-        scale_a[t] = AT == kE4M3 ? p.scale_a + (m >> p.shift_a) * p.lds_a : nullptr;
-    }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int64_t n = min(n0 + t * 16 + r16, p.N - 1);
         row_b[t] = w.b + n * p.ldb;
         scale_b[t] = w.scale_b + (n >> p.shift_b) * p.lds_b;
     }
+    Piece b[DEPTH][NT], a[DEPTH][MT];
+    auto load = [&](int64_t kb0) INLINE_LAMBDA {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) b[d][t] = load_piece(row_b[t], scale_b[t], min(kb0 + d * WAVES, w.kb1 - 1), g, w.K);
+    };
+    const int64_t kb_first = w.kb0 + wave;
+    if (kb_first < w.kb1) load(kb_first);
+
+    const int blocks = ROUND ? (int)w.kb1 : 0, stride = blocks * kBlock + 16;
+    if constexpr (ROUND) {
+        for (int unit = threadIdx.x / 16; unit < (int)p.a_rows * blocks; unit += WAVES * 4) {
+            const int row = unit / blocks, kb = unit % blocks;
+            const int64_t k = (int64_t)kb * kBlock + r16 * 8;
+            float v[8];
+            widen<AT>(load_raw<AT>(p.a, row * p.lda, k, p.K), k, p.K, v);
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, finite_magnitude(v[i]));
+            const uint32_t byte = exponent_byte(row16_max(top));
+            const float inv = inverse_scale(byte);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = scaled(v[i], inv);
+            *reinterpret_cast<uint2 *>(rounded + row * stride + kb * kBlock + r16 * 8) = make_uint2(pack4(v[0], v[1], v[2], v[3]), pack4(v[4], v[5], v[6], v[7]));
+            if (r16 == 0) bytes[unit] = (uint8_t)byte;
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int64_t m = max(row_of_a(p, min(w.first + t * 16 + r16, w.last - 1)), (int64_t)0);
+        row_a[t] = ROUND ? rounded + m * stride : p.a + m * p.lda;
+        scale_a[t] = ROUND ? bytes + m * blocks : p.scale_a + (m >> p.shift_a) * p.lds_a;
+    }
     f32x4 acc[MT][NT] = {};
-    for (int64_t kb0 = w.kb0 + wave; kb0 < w.kb1; kb0 += DEPTH * WAVES) {
-        Piece b[DEPTH][NT], a[DEPTH][MT];
-        Raw<AT == kE4M3 ? kF32 : AT> raw[DEPTH][MT];
+    for (int64_t kb0 = kb_first; kb0 < w.kb1; kb0 += DEPTH * WAVES) {
+        if (kb0 != kb_first) load(kb0);
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
             const int64_t kb = min(kb0 + d * WAVES, w.kb1 - 1);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) b[d][t] = load_piece(row_b[t], scale_b[t], kb, g, w.K);
-#pragma unroll
             for (int t = 0; t < MT; ++t) {
-                if constexpr (AT == kE4M3) a[d][t] = load_piece(row_a[t], scale_a[t], kb, g, w.K);
-                else raw[d][t] = load_raw<AT>(p.a, at_a[t], kb, g, w.K);
+                if constexpr (ROUND) {
+                    a[d][t].lo = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32);
+                    a[d][t].hi = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32 + 16);
+                    a[d][t].byte = scale_a[t][kb];
+                } else {
+                    a[d][t] = load_piece(row_a[t], scale_a[t], kb, g, w.K);
+                }
             }
         }
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
             const int64_t kb = kb0 + d * WAVES;
             if (kb >= w.kb1) break;
-            if constexpr (AT != kE4M3)
-#pragma unroll
-                for (int t = 0; t < MT; ++t) a[d][t] = round_piece<AT>(raw[d][t], kb, g, w.K);
             if ((kb + 1) * kBlock > w.K) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) cut(b[d][t], kb, g, w.K);
-                if constexpr (AT == kE4M3)
 #pragma unroll
-                    for (int t = 0; t < MT; ++t) cut(a[d][t], kb, g, w.K);
+                for (int t = 0; t < MT; ++t) cut(a[d][t], kb, g, w.K);
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -253,7 +220,7 @@ __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, 
     __syncthreads();
     for (int o = threadIdx.x; o < MT * NT * 256; o += WAVES * 64) {
         const int m = o / (16 * NT), n = o % (16 * NT);
-        if (w.first + m >= w.last || n0 + n >= p.N) continue;
+        if (w.first + m >= w.last || n0 + n >= p.N || (p.source && row_of_a(p, w.first + m) < 0)) continue;
         const int tile = m / 16 * NT + n / 16, at = m % 16 + n % 16 / 4 * 16;
         float s = 0.0f;
 #pragma unroll
@@ -265,7 +232,8 @@ __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, 
 // Buffers of plain bytes, and the longest row of 8-bit values that 256 of stay below 2^32 bytes.
 constexpr int kBufferFlags = 0x00027000;
 constexpr int64_t kMostStride = (int64_t)1 << 23;
-constexpr int kExpBlocks = 64;          // blocks whose exponents are in LDS at a time
+constexpr int kReads = 0x100, kProducts = 0x8;      // kinds of instructions to __builtin_amdgcn_sched_group_barrier
+constexpr int kExpBlocks = 32;          // blocks whose exponents are in LDS at a time
 
 // Four neighbours of a row of out.
 template <int OUT>
@@ -281,6 +249,28 @@ __device__ __forceinline__ void store4(void *out, int64_t at, f32x4 v, int64_t n
     }
 }
 
+__device__ __forceinline__ i32x4 buffer_of(const uint8_t *base, uint32_t bytes)
+{
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    return i32x4{__builtin_amdgcn_readfirstlane((int)(uint32_t)at), __builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)),
+                 __builtin_amdgcn_readfirstlane((int)bytes), kBufferFlags};
+}
+
+// 16 bytes for each lane from `at` in the buffer to lds + 16 lane, past the registers; zeros from beyond its end.  As text, because the compiler
+// waits for all such loads before any read of LDS: wait_and_meet waits for those that the next block needs.
+__device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t at, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(buffer) : "memory", "m0");
+}
+
+// Waits until at most LEFT of this wavefront's loads are under way and all its reads of LDS are done, then for the workgroup's other wavefronts.
+template <int LEFT>
+__device__ __forceinline__ void wait_and_meet()
+{
+    static_assert(LEFT < 64);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
+
 // The index among a launch's workgroups that work, such that each of the 8 dies (workgroups go to them in turn) gets neighbours.
 __device__ __forceinline__ uint32_t by_die(uint32_t id, uint32_t total)
 {
@@ -291,57 +281,70 @@ __device__ __forceinline__ uint32_t by_die(uint32_t id, uint32_t total)
 // Many rows: BM x BN results to a workgroup of WM x WN wavefronts, each with (BM / WM) x (BN / WN) of them in registers.  Blocks of 128 values
 // of the BM + BN rows go to LDS without passing registers, the next one while this one is multiplied.  A row's eight pieces of 16 bytes lie
 // exchanged by half its index, so that the 16 rows that a read of the lanes goes to fall on all banks.  WIDE: the 16-bit instruction.
-template <int BM, int BN, int WM, int WN, bool WIDE, int OUT>
-__global__ __launch_bounds__(WM * WN * 64, 2) void product_tiles_kernel(ProductArgs p, uint32_t col_tiles)
+template <int BM, int BN, int WM, int WN, int STAGES, bool WIDE, bool GATHER, int OUT>
+__global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) void product_tiles_kernel(ProductArgs p, uint32_t col_tiles)
 {
     constexpr int WAVES = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16, LOADS_A = BM / 8 / WAVES, LOADS_B = BN / 8 / WAVES;
     static_assert(WAVES % 2 == 0 && LOADS_A * 8 * WAVES == BM && LOADS_B * 8 * WAVES == BN, "a wavefront loads whole groups of 8 rows, all at even or all at odd places");
-    __shared__ __attribute__((aligned(128))) uint8_t tiles[2][(BM + BN) * kBlock];
+    __shared__ __attribute__((aligned(128))) uint8_t tiles[STAGES][(BM + BN) * kBlock];
     __shared__ uint32_t exps[kExpBlocks / 4][BM + BN];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r16 = lane % 16, g = lane / 16;
 
-    const uint32_t pieces = p.by == MADDNESS_BY_ROWS ? (uint32_t)count_pieces(p.offsets, p.groups, p.M, BM) : (uint32_t)ceil_div(p.M, (int64_t)BM);
+    PieceSearch search;
+    const uint32_t pieces = p.by == MADDNESS_BY_ROWS ? (uint32_t)search.count(p.offsets, p.groups, p.M, BM) : (uint32_t)ceil_div(p.M, (int64_t)BM);
     if (blockIdx.x >= pieces * col_tiles) return;
     // four pieces by all columns, then the next four: what a die works on at a time shares rows of both operands
     const uint32_t at = by_die(blockIdx.x, pieces * col_tiles), band = at / (4 * col_tiles), in_band = at % (4 * col_tiles);
     const uint32_t height = min(4u, pieces - band * 4);
     const int64_t n0 = (int64_t)(in_band / height) * BN;
     Part w;
-    if (!find_part(p, BM, band * 4 + in_band % height, blockIdx.y, w)) return;
+    if (!find_part(p, search, BM, band * 4 + in_band % height, blockIdx.y, w)) return;
 
     // Rows are addressed by 32-bit offsets within the tile (the launcher keeps row strides to kMostStride).  What lies beyond the tile's last
     // row is out of the buffers' range; what lies beyond column K is cut off in LDS.
     const uint32_t lda = (uint32_t)p.lda, ldb = (uint32_t)p.ldb, blocks = (uint32_t)ceil_div(w.K, (int64_t)kBlock);
     const uint32_t rows = (uint32_t)(w.last - w.first), cols = (uint32_t)min((int64_t)BN, p.N - n0), width = round_up((uint32_t)w.K, 16u);
-    const auto mem_a = __builtin_amdgcn_make_buffer_rsrc((void *)(p.a + w.first * p.lda), 0, (rows - 1) * lda + width, kBufferFlags);
-    const auto mem_b = __builtin_amdgcn_make_buffer_rsrc((void *)(w.b + n0 * p.ldb), 0, (cols - 1) * ldb + width, kBufferFlags);
-    const uint32_t chunk = (uint32_t)((lane % 8) ^ ((wave % 2) * 4 + lane / 16)) * 16, row0 = wave * 8 + lane / 8;
+    const i32x4 mem_a = buffer_of(p.a + (GATHER ? 0 : w.first * p.lda), ((GATHER ? (uint32_t)p.a_rows : rows) - 1) * lda + width);
+    const i32x4 mem_b = buffer_of(w.b + n0 * p.ldb, (cols - 1) * ldb + width);
+    const uint32_t chunk = (uint32_t)((lane % 8) ^ (lane / 8)) * 16, row0 = wave * 8 + lane / 8;
     const uint32_t at_a = row0 * lda + chunk, at_b = row0 * ldb + chunk;
-    // (keeps the compiler from holding every sum of this and a multiple of a stride in a register of its own)
-    auto again = [](uint32_t x) INLINE_LAMBDA { asm volatile("" : "+v"(x)); return x; };
-    auto load = [&](uint8_t *tile, uint32_t kb) INLINE_LAMBDA {
-        const uint32_t lane_a = again(at_a), lane_b = again(at_b);
+    uint32_t from_a[LOADS_A];
+    if constexpr (GATHER) {
 #pragma unroll
         for (int i = 0; i < LOADS_A; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(mem_a, (__attribute__((address_space(3))) void *)(tile + (wave + i * WAVES) * 1024), 16,
-                                                     lane_a + ((i * WAVES * 8) * lda + kb * kBlock), 0, 0, 0);
+            from_a[i] = (uint32_t)max(row_of_a(p, min(w.first + row0 + i * WAVES * 8, w.last - 1)), (int64_t)0) * lda + chunk;
+    }
+    // (keeps the compiler from holding every sum of this and a multiple of a stride in a register of its own)
+    auto again = [](uint32_t x) INLINE_LAMBDA { asm volatile("" : "+v"(x)); return x; };
+    const uint32_t tiles_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)tiles[0] + wave * 1024;
+    auto load = [&](uint32_t stage, uint32_t kb) INLINE_LAMBDA {
+        const uint32_t lane_a = again(at_a), lane_b = again(at_b), to = tiles_at + stage * ((BM + BN) * kBlock);
 #pragma unroll
-        for (int i = 0; i < LOADS_B; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(mem_b, (__attribute__((address_space(3))) void *)(tile + BM * kBlock + (wave + i * WAVES) * 1024), 16,
-                                                     lane_b + ((i * WAVES * 8) * ldb + kb * kBlock), 0, 0, 0);
+        for (int i = 0; i < LOADS_A; ++i) {
+            uint32_t at = lane_a + ((i * WAVES * 8) * lda + kb * kBlock);
+            if constexpr (GATHER) at = from_a[i] + kb * kBlock;
+            load_to_lds(mem_a, at, to + i * WAVES * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS_B; ++i) load_to_lds(mem_b, lane_b + ((i * WAVES * 8) * ldb + kb * kBlock), to + BM * kBlock + i * WAVES * 1024);
     };
     const int wm = wave / WN, wn = wave % WN;
     // The exponents of kExpBlocks blocks, four to a word, by rows.
     auto load_exps = [&](uint32_t kb) INLINE_LAMBDA {
-        const uint32_t some = min((uint32_t)kExpBlocks, blocks - kb);
+        const uint32_t last_word = (blocks - 1) / 4 * 4;
         for (int row = threadIdx.x; row < BM + BN; row += WAVES * 64) {
-            const uint8_t *from = row < BM ? p.scale_a + (min(w.first + row, w.last - 1) >> p.shift_a) * p.lds_a
+            const int64_t m = min(w.first + row, w.last - 1);
+            const uint8_t *from = row < BM ? p.scale_a + ((GATHER ? max(row_of_a(p, m), (int64_t)0) : m) >> p.shift_a) * p.lds_a
                                            : w.scale_b + (min(n0 + row - BM, p.N - 1) >> p.shift_b) * p.lds_b;
-            for (uint32_t q = 0; q * 4 < some; ++q) exps[q][row] = *reinterpret_cast<const uint32_t *>(from + kb + q * 4);
+            uint32_t words[kExpBlocks / 4];                  // (all on their way before the first is needed; beyond the last block that again)
+#pragma unroll
+            for (int q = 0; q < kExpBlocks / 4; ++q) words[q] = *reinterpret_cast<const uint32_t *>(from + min(kb + q * 4, last_word));
+#pragma unroll
+            for (int q = 0; q < kExpBlocks / 4; ++q) exps[q][row] = words[q];
         }
     };
     f32x4 acc[MT][NT] = {};
-    const int half0 = r16 * kBlock + (((2 * g) ^ (r16 / 2)) * 16), half1 = r16 * kBlock + (((2 * g + 1) ^ (r16 / 2)) * 16);
+    const int half0 = r16 * kBlock + (((2 * g) ^ (r16 % 8)) * 16), half1 = r16 * kBlock + (((2 * g + 1) ^ (r16 % 8)) * 16);
     auto fragment = [&](const uint8_t *tile, int row) INLINE_LAMBDA {
         const i32x4 lo = *reinterpret_cast<const i32x4 *>(tile + row * kBlock + half0), hi = *reinterpret_cast<const i32x4 *>(tile + row * kBlock + half1);
         return i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
@@ -349,17 +352,27 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void product_tiles_kernel(ProductA
     // The columns from K on of the last block, in both operands, to zeros.
     auto cut_off = [&](uint8_t *tile) INLINE_LAMBDA {
         for (int row = threadIdx.x; row < BM + BN; row += WAVES * 64)
-            for (int k = (int)(w.K % kBlock); k < kBlock; ++k) tile[row * kBlock + (((k / 16) ^ (row / 2 % 8)) * 16 + k % 16)] = 0;
+            for (int k = (int)(w.K % kBlock); k < kBlock; ++k) tile[row * kBlock + (((k / 16) ^ (row % 8)) * 16 + k % 16)] = 0;
         __syncthreads();
     };
     const uint32_t kb0 = (uint32_t)w.kb0, kb1 = (uint32_t)w.kb1;
     if (kb0 < kb1) {
-        uint8_t *tile = tiles[0], *next = tiles[1];
-        load(tile, kb0);
+        for (uint32_t i = 0; i < STAGES - 1; ++i)
+            if (kb0 + i < kb1) load(i, kb0 + i);
         load_exps(kb0 / kExpBlocks * kExpBlocks);
         uint32_t ea[MT], eb[NT];                             // this block's in the lowest byte
-        __syncthreads();
-        for (uint32_t kb = kb0;; ++kb) {
+        uint32_t stage = 0;
+        for (uint32_t kb = kb0; kb < kb1; ++kb) {
+            // this wavefront's part of the block has come, and so has everybody's; nobody reads the last block any more
+            if (kb + STAGES - 2 < kb1) wait_and_meet<(STAGES - 2) * (LOADS_A + LOADS_B)>();
+            else wait_and_meet<0>();
+            if (kb % kExpBlocks == 0 && kb != kb0) {
+                load_exps(kb);
+                __syncthreads();
+            }
+            if (kb + STAGES - 1 < kb1) load(stage == 0 ? STAGES - 1 : stage - 1, kb + STAGES - 1);
+            uint8_t *tile = tiles[stage];
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
             if (kb + 1 == kb1 && w.K % kBlock) cut_off(tile);
             if (kb % 4 == 0 || kb == kb0) {
                 const uint32_t *from = exps[kb % kExpBlocks / 4] + r16;
@@ -368,20 +381,24 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void product_tiles_kernel(ProductA
 #pragma unroll
                 for (int t = 0; t < NT; ++t) eb[t] = from[BM + (wn * NT + t) * 16] >> (kb % 4 * 8);
             }
-            // All fragments are asked for before the next block is: the compiler lets no read of LDS pass a load into it.
             i32x8 b[NT], a[MT];
 #pragma unroll
             for (int j = 0; j < NT; ++j) b[j] = fragment(tile, BM + (wn * NT + j) * 16);
 #pragma unroll
             for (int i = 0; i < MT; ++i) a[i] = fragment(tile, (wm * MT + i) * 16);
-            __builtin_amdgcn_sched_barrier(0);
-            if (kb + 1 < kb1) load(next, kb + 1);
             if constexpr (!WIDE) {
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
                     for (int j = 0; j < NT; ++j)
                         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], 0, 0, 0, (int)eb[j], 0, (int)ea[i]);
+                // B's fragments and two of A's, then two more of A's before the products of the last two
+                __builtin_amdgcn_sched_group_barrier(kReads, 2 * NT + 4, 0);
+#pragma unroll
+                for (int i = 0; i < MT / 2; ++i) {
+                    if (i + 1 < MT / 2) __builtin_amdgcn_sched_group_barrier(kReads, 4, 0);
+                    __builtin_amdgcn_sched_group_barrier(kProducts, 2 * NT, 0);
+                }
             } else {
                 bf16x8 wb[NT][4];
 #pragma unroll
@@ -401,15 +418,6 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void product_tiles_kernel(ProductA
             for (int t = 0; t < MT; ++t) ea[t] >>= 8;
 #pragma unroll
             for (int t = 0; t < NT; ++t) eb[t] >>= 8;
-            if (kb + 1 >= kb1) break;
-            __syncthreads();
-            if ((kb + 1) % kExpBlocks == 0) {
-                load_exps(kb + 1);
-                __syncthreads();
-            }
-            uint8_t *t = tile;
-            tile = next;
-            next = t;
         }
     }
     constexpr int64_t bytes = OUT == kF32 ? 4 : 2;
@@ -417,7 +425,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void product_tiles_kernel(ProductA
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int64_t m = w.first + (wm * MT + i) * 16 + r16;
-        if (m >= w.last) continue;
+        if (m >= w.last || (GATHER && row_of_a(p, m) < 0)) continue;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             const int64_t n = n0 + (wn * NT + j) * 16 + 4 * g;
@@ -426,32 +434,51 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void product_tiles_kernel(ProductA
     }
 }
 
-template <int BM, int BN, int WM, int WN, int OUT>
+template <int BM, int BN, int WM, int WN, int STAGES, bool GATHER, int OUT>
 int launch_tiles(const ProductArgs &p, hipStream_t stream)
 {
     const int64_t col_tiles = ceil_div(p.N, (int64_t)BN), pieces = ceil_div(p.M, (int64_t)BM) + (p.by == MADDNESS_BY_ROWS ? p.groups : 0);
     if (col_tiles * pieces >= (int64_t)1 << 31) return fail(MADDNESS_E_UNSUPPORTED, "block product: %lld x %lld results are too many", (long long)p.M, (long long)p.N);
     const dim3 grid((unsigned)(col_tiles * pieces), p.by == MADDNESS_BY_DEPTH ? (unsigned)p.groups : 1u);
     note_kernel("product_tiles_kernel", __PRETTY_FUNCTION__);
-    hipLaunchKernelGGL((product_tiles_kernel<BM, BN, WM, WN, OUT == kF32, OUT>), grid, dim3(WM * WN * 64), 0, stream, p, (uint32_t)col_tiles);
+    hipLaunchKernelGGL((product_tiles_kernel<BM, BN, WM, WN, STAGES, OUT == kF32, GATHER, OUT>), grid, dim3(WM * WN * 64), 0, stream, p, (uint32_t)col_tiles);
     return check_hip(hipGetLastError(), "launch product_tiles_kernel");
 }
+
+template <int AT, int OUT, int MT, int NT, int DEPTH>
+int launch_few_as(const ProductArgs &p, hipStream_t stream)
+{
+    constexpr int WAVES = 8;
+    const int64_t col_tiles = ceil_div(p.N, (int64_t)(16 * NT));
+    const int64_t pieces = ceil_div(p.M, (int64_t)(16 * MT)) + (p.by == MADDNESS_BY_ROWS ? p.groups : 0);
+    if (col_tiles * pieces >= (int64_t)1 << 31) return fail(MADDNESS_E_UNSUPPORTED, "block product: %lld x %lld results are too many", (long long)p.M, (long long)p.N);
+    const dim3 grid((unsigned)(col_tiles * pieces), p.by == MADDNESS_BY_DEPTH ? (unsigned)p.groups : 1u);
+    note_kernel("product_few_kernel", __PRETTY_FUNCTION__);
+    hipLaunchKernelGGL((product_few_kernel<AT, MT, NT, WAVES, DEPTH, OUT>), grid, dim3(WAVES * 64), 0, stream, p, (uint32_t)col_tiles);
+    return check_hip(hipGetLastError(), "launch product_few_kernel");
+}
+
+// Rows of A that one matrix of B goes with, about.
+int64_t rows_each(const ProductArgs &p) { return p.by == MADDNESS_BY_ROWS ? ceil_div(p.M, (int64_t)p.groups) : p.M; }
 
 template <int AT, int OUT>
 int launch_few(const ProductArgs &p, hipStream_t stream)
 {
-    constexpr int WAVES = 8;
-    const bool small = p.by == MADDNESS_BY_ROWS ? p.M <= 16 * p.groups : p.M <= 16;
-    const int rows = small ? 16 : 64, cols = small ? 16 : 32;
-    const int64_t col_tiles = ceil_div(p.N, (int64_t)cols);
-    const int64_t pieces = ceil_div(p.M, (int64_t)rows) + (p.by == MADDNESS_BY_ROWS ? p.groups : 0);
-    if (col_tiles * pieces >= (int64_t)1 << 31) return fail(MADDNESS_E_UNSUPPORTED, "block product: %lld x %lld results are too many", (long long)p.M, (long long)p.N);
-    const dim3 grid((unsigned)(col_tiles * pieces), p.by == MADDNESS_BY_DEPTH ? (unsigned)p.groups : 1u);
-    note_kernel("product_few_kernel", __PRETTY_FUNCTION__);
-    if (small) hipLaunchKernelGGL((product_few_kernel<AT, 1, 1, WAVES, AT == kF32 ? 2 : 4, OUT>), grid, dim3(WAVES * 64), 0, stream, p, (uint32_t)col_tiles);
-    else if constexpr (AT == kE4M3)
-        hipLaunchKernelGGL((product_few_kernel<AT, 4, 2, WAVES, 2, OUT>), grid, dim3(WAVES * 64), 0, stream, p, (uint32_t)col_tiles);
-    return check_hip(hipGetLastError(), "launch product_few_kernel");
+    if (rows_each(p) > 16) return launch_few_as<AT, OUT, 4, 2, 2>(p, stream);
+    // a wavefront's share of the sum is one block: more columns to a workgroup instead
+    if (p.K <= 8 * kBlock) return launch_few_as<AT, OUT, 1, 4, 1>(p, stream);
+    return launch_few_as<AT, OUT, 1, 1, 4>(p, stream);
+}
+
+template <bool GATHER, int OUT>
+int launch_shape(const ProductArgs &p, int64_t rows, int64_t groups, hipStream_t stream)
+{
+    if constexpr (OUT != kF32) {
+        // 256 x 256 to a workgroup: less to read for each product, but only where there is one for every compute unit
+        const int64_t large = ceil_div(rows, (int64_t)256) * ceil_div(p.N, (int64_t)256) * groups;
+        if (!GATHER && large >= device_info().cus && rows >= 1024) return launch_tiles<256, 256, 2, 4, 2, false, OUT>(p, stream);
+    }
+    return launch_tiles<128, 128, 2, 2, 2, GATHER, OUT>(p, stream);
 }
 
 template <int OUT>
@@ -460,17 +487,22 @@ int launch_to(const ProductArgs &p, int a_dtype, hipStream_t stream)
     if (a_dtype == MADDNESS_F32) return launch_few<kF32, OUT>(p, stream);
     if (a_dtype == MADDNESS_F16) return launch_few<kF16, OUT>(p, stream);
     if (a_dtype == MADDNESS_BF16) return launch_few<kBF16, OUT>(p, stream);
-    const int64_t groups = p.by == MADDNESS_DENSE ? 1 : p.groups, rows = p.by == MADDNESS_BY_ROWS ? ceil_div(p.M, groups) : p.M;
-    if (rows <= 64 || std::max(p.lda, p.ldb) > kMostStride) return launch_few<kE4M3, OUT>(p, stream);
-    const int64_t large = ceil_div(rows, (int64_t)256) * ceil_div(p.N, (int64_t)256) * groups;
-    if constexpr (OUT != kF32)
-        if (large >= device_info().cus && rows >= 1024) return launch_tiles<256, 256, 2, 4, OUT>(p, stream);
-    return launch_tiles<128, 128, 2, 2, OUT>(p, stream);
+    const int64_t rows = rows_each(p), groups = p.by == MADDNESS_DENSE ? 1 : p.groups;
+    const bool far = std::max(p.lda, p.ldb) > kMostStride || (p.source && p.a_rows * p.lda >= (int64_t)1 << 32);
+    // Small products: the few-rows kernel makes more workgroups of them (1024 x 512 x 512 takes 7.0 us instead of 9.0, 128 x 4096 x 4096
+    // 20 instead of 28, 256 x 4096 x 4096 38 instead of 29).
+    const int64_t depth = p.by == MADDNESS_BY_DEPTH ? ceil_div(p.K, groups) : p.K;
+    if (rows <= 64 || far || rows * p.N * depth * groups <= (int64_t)3 << 30) return launch_few<kE4M3, OUT>(p, stream);
+    if (p.source) return launch_shape<true, OUT>(p, rows, groups, stream);
+    return launch_shape<false, OUT>(p, rows, groups, stream);
 }
 
 }  // namespace
 
-bool rounds_inside(int64_t M, int64_t N, int64_t K, int groups, int by) { return by == MADDNESS_DENSE && M <= 16 && K >= 8; }
+bool rounds_inside(int64_t M, int64_t K, int by)
+{
+    return by != MADDNESS_BY_DEPTH && M <= kInsideRows && K >= 8 && M * round_up(K, (int64_t)kBlock) <= kInside;
+}
 
 int launch_block_product(const ProductArgs &p, int a_dtype, int out_dtype, hipStream_t stream)
 {

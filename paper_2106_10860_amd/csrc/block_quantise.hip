@@ -17,19 +17,18 @@ struct QuantiseArgs {
     int64_t ldq, lds, ldqt, ldst;
 };
 
-// Where row r's elements begin, and the factor of them; false for a row of zeros.
+// Where row r's elements begin, and the factor of them; false for a row of zeros (whose place is that of another).
 __device__ __forceinline__ bool find_row(const QuantiseArgs &a, int64_t r, int64_t &at, float &factor)
 {
     factor = 1.0f;
-    if (!a.source) {
-        at = r * a.ldx;
-        return true;
-    }
-    const int s = a.source[r];
-    if (s < 0 || s >= a.slots) return false;
+    at = r * a.ldx;
+    if (!a.source) return true;
+    int s = a.source[r];
+    const bool there = s >= 0 && s < a.slots;
+    if (!there) s = 0;
     if (a.factors) factor = a.factors[s];
     at = (int64_t)(s / a.repeat) * a.ldx;
-    return true;
+    return there;
 }
 
 // Blocks of 1 x 128, rows only.  16 lanes take a block, 8 values each: the maximum stays within a row of lanes.
@@ -47,11 +46,13 @@ __global__ __launch_bounds__(256) void quantise_rows_kernel(QuantiseArgs a, int6
     int64_t at = 0;
     float factor;
     const bool there = find_row(a, r, at, factor);
-    load8<DT>(x, at + c, there ? (int)min(a.cols - c, (int64_t)8) : 0, v);
+    if (a.cols >= 8) widen<DT>(load_raw<DT>(x, at, c, a.cols), c, a.cols, v);
+    else load_short<DT>(x, at, c, a.cols, v);
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if (a.factors) v[i] *= factor;
+        if (!there) v[i] = 0.0f;
         top = max(top, finite_magnitude(v[i]));
     }
     const uint32_t byte = exponent_byte(row16_max(top));
@@ -78,19 +79,26 @@ __global__ __launch_bounds__(256) void quantise_tiles_kernel(QuantiseArgs a, uin
     const uint32_t cb = blockIdx.x % blocks, rb = blockIdx.x / blocks, row_blocks = gridDim.x / blocks;
     const int64_t m = blockIdx.y, c = (int64_t)cb * kBlock + cg * 8, r0 = (int64_t)rb * kBlock + rg * 8;
     const char *x = static_cast<const char *>(a.x) + m * a.stride_x * elem_size(DT);
-    const int n = (int)max(min(a.cols - c, (int64_t)8), (int64_t)0);
-    float v[8][8];
+    float v[8][8], factor[8];
     uint32_t top_row[8], top_col[8] = {};
+    Raw<DT> raw[8];
+    int64_t at[8] = {};
+    bool there[8];
+    // (rows beyond the end are read as the last, and columns as widen says: everything is asked for before anything is needed)
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
-        int64_t at = 0;
-        float factor = 1.0f;
-        const bool there = r0 + p < a.rows && find_row(a, r0 + p, at, factor);
-        load8<DT>(x, at + c, there ? n : 0, v[p]);
+        there[p] = find_row(a, min(r0 + p, a.rows - 1), at[p], factor[p]) && r0 + p < a.rows;
+        if (a.cols >= 8) raw[p] = load_raw<DT>(x, at[p], c, a.cols);
+    }
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+        if (a.cols >= 8) widen<DT>(raw[p], c, a.cols, v[p]);
+        else load_short<DT>(x, at[p], c, a.cols, v[p]);
         top_row[p] = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (a.factors) v[p][i] *= factor;
+            if (a.factors) v[p][i] *= factor[p];
+            if (!there[p]) v[p][i] = 0.0f;
             const uint32_t t = finite_magnitude(v[p][i]);
             top_row[p] = max(top_row[p], t);
             top_col[i] = max(top_col[i], t);

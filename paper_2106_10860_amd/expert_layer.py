@@ -56,12 +56,8 @@ class ExpertLayer:
         ids, weights = m.maddness_route(logits, self.k, **self.choice, **self.groups)
         # in training the sums over an expert's tokens are products by depth, which go by whole blocks
         offsets, _, source, place = m.maddness_order(ids, self.experts, m.BLOCK if training else 1)
-        x_t = None
-        if training:
-            xq, x_t = m.maddness_quantise_blocks(x, both=True, source=source, repeat=self.k)
-        else:
-            xq = m.maddness_quantise_blocks(x, source=source, repeat=self.k)
-        y = m.maddness_block_product(xq, self.W, offsets, out_dtype=x.dtype)
+        x_t = m.maddness_quantise_blocks(x, transposed=True, source=source, repeat=self.k) if training else None
+        y = m.maddness_block_product(x, self.W, offsets, source=source, repeat=self.k, out_dtype=x.dtype)
         out = m.maddness_combine(y, place, weights)
         if not training:
             return out, Saved(ids, weights)

@@ -51,9 +51,9 @@ def test_block_product_refuses(mad):
     def matrix(**kw):
         return M(**{**dict(data=FAKE, dtype=16, tile=1, rows=20, cols=300, ld=304, stride=0, scale=FAKE, lds=4, scale_stride=0), **kw})
 
-    def call(A=None, B=None, by=0, groups=1, offsets=None, out=FAKE, dtype=2, ldo=30, work=None, size=0):
+    def call(A=None, B=None, by=0, groups=1, offsets=None, source=None, slots=0, repeat=1, out=FAKE, dtype=2, ldo=30, work=None, size=0):
         A, B = A or matrix(), B or matrix(rows=30, tile=128)
-        return mad.lib().maddness_block_product(C.byref(A), C.byref(B), by, groups, offsets, out, dtype, ldo, work, size, None)
+        return mad.lib().maddness_block_product(C.byref(A), C.byref(B), by, groups, offsets, source, slots, repeat, out, dtype, ldo, work, size, None)
 
     for kw, status, text in (
             (dict(by=3), inval, "by"), (dict(A=matrix(rows=-1)), inval, "negative"), (dict(A=matrix(cols=299)), inval, "columns"),
@@ -63,14 +63,17 @@ def test_block_product_refuses(mad):
             (dict(out=None), inval, "out"), (dict(ldo=29), inval, "out"), (dict(out=FAKE + 1), align, "out"), (dict(by=1, groups=0), inval, "groups"),
             (dict(by=1, groups=70000, offsets=FAKE), unsupported, "groups"), (dict(by=1, groups=3), inval, "offsets"),
             (dict(by=1, groups=3, offsets=FAKE + 2), align, "offsets"), (dict(by=2, groups=3, offsets=FAKE), inval, "tile 1"),
+            (dict(source=FAKE, slots=5), inval, "source"), (dict(by=1, groups=3, offsets=FAKE, source=FAKE, slots=5, repeat=0), inval, "repeat"),
+            (dict(by=1, groups=3, offsets=FAKE, source=FAKE, slots=-1), inval, "slots"), (dict(by=1, groups=3, offsets=FAKE, source=FAKE + 1, slots=5), align, "source"),
+            (dict(by=1, groups=3, offsets=FAKE, source=FAKE, slots=5, repeat=1 << 30), unsupported, "repeat"),
             (dict(A=matrix(dtype=2), by=2, groups=3, offsets=FAKE), unsupported, "E4M3"),
             (dict(A=matrix(dtype=2, rows=500)), unsupported, "workspace"),
             (dict(A=matrix(dtype=2, rows=500), work=FAKE + 4, size=1 << 20), align, "workspace")):
         refused(mad, call(**kw), status, text)
-    assert mad.lib().maddness_block_product(None, None, 0, 1, None, FAKE, 2, 30, None, 0, None) == inval
+    assert mad.lib().maddness_block_product(None, None, 0, 1, None, None, 0, 1, FAKE, 2, 30, None, 0, None) == inval
     refused(mad, call(A=matrix(rows=0)), mad.MADDNESS_OK)
     need = mad.lib().maddness_block_product_workspace
-    assert need(500, 30, 300, 1, 0, 2) >= 500 * 304 + 500 * 4 and need(500, 30, 300, 1, 0, 16) == 0 and need(0, 30, 300, 1, 0, 2) == 0
+    assert need(500, 300, 0, 2) >= 500 * 304 + 500 * 4 and need(500, 300, 0, 16) == 0 and need(0, 300, 0, 2) == 0
 
 
 def test_route_and_order_refuse(mad):

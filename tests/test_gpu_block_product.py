@@ -156,7 +156,8 @@ def test_product(mad, M, N, K, tiles):
     assert torch.equal(again, mad.maddness_block_product(A, B, out_dtype=torch.float32))
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 64, 512), (3, 129, 510), (16, 300, 1000), (17, 300, 1000), (200, 130, 77), (400, 260, 640)])
+@pytest.mark.parametrize("M,N,K", [(1, 64, 512), (3, 129, 510), (16, 300, 1000), (17, 300, 1000), (200, 130, 77), (400, 260, 640), (1, 50, 8), (2, 50, 7),
+                                   (64, 70, 510), (37, 33, 9), (8, 40, 4000), (1, 40, 20000)])
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_product_rounds_a_float_operand_as_quantise_does(mad, M, N, K, dtype):
     import torch
@@ -230,6 +231,30 @@ def test_product_by_rows(mad, counts, N, K):
         if counts[e]:
             check(out[off[e]:off[e + 1]], a[off[e]:off[e + 1]], b[e], f"expert {e}")
     assert (out[off[-1]:] == 7).all()
+
+
+@pytest.mark.parametrize("T,counts,k", [(4, [3, 0, 2, 5, 0, 1], 3), (50, [20, 0, 17, 1], 2), (300, [130, 0, 64, 1, 300, 129], 3), (2, [1], 1)])
+@pytest.mark.parametrize("kind", ["e4m3", "bf16", "f32"])
+def test_product_of_gathered_rows(mad, T, counts, k, kind):
+    import torch
+    print("case gathered", T, counts, kind, flush=True)
+    N, K, E, off = 96, 330, len(counts), offsets_of(counts, 4)
+    rng = np.random.default_rng(T)
+    S = int(off[-1]) + 3
+    source = rng.integers(-2, T * k + 2, S).astype(np.int32)              # some rows have none
+    x = data(T, T, K, torch.float32 if kind == "e4m3" else dtype_of(kind)).cuda()
+    A = mad.maddness_quantise_blocks(x)
+    B = mad.maddness_quantise_blocks(data(E, E * N, K, torch.float32).cuda().view(E, N, K), 128)
+    out = torch.full((S, N), 7.0, device="cuda")
+    mad.maddness_block_product(A if kind == "e4m3" else x, B, torch.from_numpy(off).cuda(), source=torch.from_numpy(source).cuda(), repeat=k, out=out)
+    a, b, written = A.values().double().cpu().numpy(), B.values().double().cpu().numpy(), np.zeros(S, bool)
+    for e in range(E):
+        rows = np.arange(off[e], off[e + 1])
+        rows = rows[(source[rows] >= 0) & (source[rows] < T * k)]
+        written[rows] = True
+        if len(rows):
+            check(out[torch.from_numpy(rows).cuda()], a[source[rows] // k], b[e], f"expert {e}")
+    assert (out.cpu()[torch.from_numpy(~written)] == 7).all()
 
 
 @pytest.mark.parametrize("counts", [[128], [0, 3, 0, 200, 129], [1000, 0, 1], [0, 0]])
