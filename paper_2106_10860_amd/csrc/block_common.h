@@ -1,6 +1,8 @@
 // What the kernels on 8-bit block matrices share: the number format, its conversions and the search for an expert's rows.
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 #include "device_common.h"
 
@@ -18,8 +20,8 @@ __host__ __device__ constexpr T ceil_div(T a, T b) { return (a + b - 1) / b; }
 template <typename T>
 __host__ __device__ constexpr T round_up(T a, T b) { return ceil_div(a, b) * b; }
 
-// Eight consecutive elements of a row of n, from column c on, as they are in memory (any alignment to the element).  A piece that would pass the
-// row's end is read from n - 8 on instead (n >= 8), and moved into its place by widen: no branch, so that many can be on their way.
+// Eight consecutive elements of a row of n >= 8, from column c on, as they are in memory (any alignment to the element).  A piece that would
+// pass the row's end is read from n - 8 on instead: no branch, so that many can be on their way.
 template <int DT>
 struct __attribute__((packed, aligned(elem_size(DT)))) Raw {
     uint32_t w[2 * elem_size(DT)];
@@ -31,9 +33,8 @@ __device__ __forceinline__ Raw<DT> load_raw(const void *x, int64_t row_at, int64
     return *reinterpret_cast<const Raw<DT> *>(static_cast<const char *>(x) + (row_at + min(c, n - 8)) * elem_size(DT));
 }
 
-// Widened; those from column n on are 0.
 template <int DT>
-__device__ __forceinline__ void widen(const Raw<DT> &r, int64_t c, int64_t n, float (&v)[8])
+__device__ __forceinline__ void widen(const Raw<DT> &r, float (&v)[8])
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -41,22 +42,19 @@ __device__ __forceinline__ void widen(const Raw<DT> &r, int64_t c, int64_t n, fl
         else if constexpr (DT == kBF16) v[i] = __uint_as_float(i & 1 ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16);
         else v[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(r.w[i / 2] >> (i & 1 ? 16 : 0)));
     }
-    const int64_t moved = c - (n - 8);                       // the piece's first element is at this place of the 8
-    if (moved > 0) {
-        float in[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) in[i] = v[i];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] = 0.0f;
-#pragma unroll
-            for (int from = i + 1; from < 8; ++from)
-                if (from - i == moved) v[i] = in[from];
-        }
-    }
 }
 
-// The same of a row of fewer than 8.
+// How many of the elements of a piece are before c.
+__device__ __forceinline__ int before_column(int64_t c, int64_t n) { return (int)max(c - (n - 8), (int64_t)0); }
+
+// Eight bytes of which the first `skip` are not wanted, those after them in their place, and zeros.
+__device__ __forceinline__ uint2 in_place(uint2 b, int skip)
+{
+    const uint64_t m = skip < 8 ? (((uint64_t)b.y << 32) | b.x) >> (8 * skip) : 0;
+    return make_uint2((uint32_t)m, (uint32_t)(m >> 32));
+}
+
+// A row of fewer than 8, from column c on, and zeros.
 template <int DT>
 __device__ __forceinline__ void load_short(const void *x, int64_t row_at, int64_t c, int64_t n, float (&v)[8])
 {
@@ -81,21 +79,13 @@ __device__ __forceinline__ uint32_t exponent_byte(uint32_t top)
     return (uint32_t)max(e, 1);
 }
 
-// 2^-e for a byte of 1 .. 253, exactly
-__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
-
-// Four values (scaled; at most 448 where finite) to E4M3, nearest, ties to even.
-__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d)
+// Four values divided by 2^(byte - 127), to E4M3, nearest, ties to even; NaN for an infinity.
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d, uint32_t byte)
 {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
-}
-
-// Scaled for pack4: infinities become NaN (the format has none, and the conversion would make 448 of them).
-__device__ __forceinline__ float scaled(float x, float inverse)
-{
-    const float y = x * inverse;
-    return fabsf(x) == __builtin_inff() ? __builtin_nanf("") : y;
+    using pair = __attribute__((ext_vector_type(2))) short;
+    const float scale = __uint_as_float(byte << 23);
+    const pair lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(pair{0, 0}, a, b, scale, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, c, d, scale, true));
 }
 
 // Largest value of the 16 lanes of a row of lanes, in all of them (rotations within the row).
@@ -107,32 +97,23 @@ __device__ __forceinline__ uint32_t row16_max(uint32_t x)
     return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x121, 0xf, 0xf, true));
 }
 
-// fp32 to a result's type, nearest even, NaN kept.
-__device__ __forceinline__ uint16_t to_bf16(float x)
-{
-    const uint32_t b = __float_as_uint(x);
-    if ((b & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((b >> 16) | 0x40u);
-    return (uint16_t)((b + 0x7fffu + ((b >> 16) & 1u)) >> 16);
-}
-
+// fp32 to a result's type, nearest even.
 template <int DT>
 __device__ __forceinline__ void store_as(void *base, int64_t at, float x)
 {
     if constexpr (DT == kF32) static_cast<float *>(base)[at] = x;
     else if constexpr (DT == kF16) static_cast<_Float16 *>(base)[at] = (_Float16)x;
-    else static_cast<uint16_t *>(base)[at] = to_bf16(x);
+    else static_cast<__bf16 *>(base)[at] = (__bf16)x;
 }
 
 // Two results as one word of a narrow type.
 template <int DT>
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
-    if constexpr (DT == kF16) {
-        const uint16_t x = __builtin_bit_cast(uint16_t, (_Float16)a), y = __builtin_bit_cast(uint16_t, (_Float16)b);
-        return x | ((uint32_t)y << 16);
-    } else {
-        return to_bf16(a) | ((uint32_t)to_bf16(b) << 16);
-    }
+    using pair16 = __attribute__((ext_vector_type(2))) _Float16;
+    using pair_b = __attribute__((ext_vector_type(2))) __bf16;
+    if constexpr (DT == kF16) return __builtin_bit_cast(uint32_t, (pair16){(_Float16)a, (_Float16)b});
+    else return __builtin_bit_cast(uint32_t, (pair_b){(__bf16)a, (__bf16)b});
 }
 
 // Entry e of an array of offsets, cut back to 0 .. limit.

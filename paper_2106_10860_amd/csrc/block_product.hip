@@ -10,8 +10,6 @@
 // B's rows (the columns of out) are the instruction's first operand and A's rows its second, so that a lane's four results are
 // four neighbours in a row of out.  Lane l holds row l % 16, values 32 (l / 16) .. + 31 of an operand's block, and results
 // n = 4 (l / 16) + i of row m = l % 16.
-#include <type_traits>
-
 #include "block_common.h"
 
 namespace maddness {
@@ -147,15 +145,14 @@ __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, 
             const int row = unit / blocks, kb = unit % blocks;
             const int64_t k = (int64_t)kb * kBlock + r16 * 8;
             float v[8];
-            widen<AT>(load_raw<AT>(p.a, row * p.lda, k, p.K), k, p.K, v);
+            const int skip = before_column(k, p.K);
+            widen<AT>(load_raw<AT>(p.a, row * p.lda, k, p.K), v);
             uint32_t top = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, finite_magnitude(v[i]));
+            for (int i = 0; i < 8; ++i) top = i < skip ? top : max(top, finite_magnitude(v[i]));
             const uint32_t byte = exponent_byte(row16_max(top));
-            const float inv = inverse_scale(byte);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = scaled(v[i], inv);
-            *reinterpret_cast<uint2 *>(rounded + row * stride + kb * kBlock + r16 * 8) = make_uint2(pack4(v[0], v[1], v[2], v[3]), pack4(v[4], v[5], v[6], v[7]));
+            *reinterpret_cast<uint2 *>(rounded + row * stride + kb * kBlock + r16 * 8) =
+                in_place(make_uint2(pack4(v[0], v[1], v[2], v[3], byte), pack4(v[4], v[5], v[6], v[7], byte)), skip);
             if (r16 == 0) bytes[unit] = (uint8_t)byte;
         }
         __syncthreads();

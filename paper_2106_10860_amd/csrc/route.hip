@@ -616,9 +616,10 @@ __global__ __launch_bounds__(kWaves * 64) void combine_kernel(CombineArgs a)
 {
     constexpr int AT_ONCE = YT == kF32 ? 4 : 8;
     const int lane = threadIdx.x % 64;
-    const int64_t t = (int64_t)blockIdx.x * kWaves + threadIdx.x / 64, c = ((int64_t)blockIdx.y * 64 + lane) * 8;
-    if (t >= a.T || c >= a.N) return;
+    const int64_t t = (int64_t)blockIdx.x * kWaves + threadIdx.x / 64, c0 = ((int64_t)blockIdx.y * 64 + lane) * 8;
+    if (t >= a.T || c0 >= a.N) return;
     const bool shorter = a.N < 8;
+    const int64_t c = shorter ? 0 : min(c0, a.N - 8);        // (the last piece computes some of the one before again, to the same values)
     float sum[8] = {};
     for (int j0 = 0; j0 < a.k; j0 += AT_ONCE) {
         int p[AT_ONCE];
@@ -639,7 +640,7 @@ __global__ __launch_bounds__(kWaves * 64) void combine_kernel(CombineArgs a)
             if (j0 + j >= a.k || a.rows == 0) break;
             float v[8];
             if (shorter) load_short<YT>(a.y, (int64_t)max(p[j], 0) * a.ldy, c, a.N, v);
-            else widen<YT>(raw[j], c, a.N, v);
+            else widen<YT>(raw[j], v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] = p[j] < 0 ? sum[i] : sum[i] + w[j] * v[i];
         }
@@ -676,8 +677,11 @@ __global__ __launch_bounds__(kWaves * 64) void combine_gradient_kernel(CombineAr
                 if (a.N >= 8) {
                     const Raw<GT> raw_g = load_raw<GT>(a.gradient, at_g, c, a.N);
                     const Raw<YT> raw_y = load_raw<YT>(a.y, at_y, c, a.N);
-                    widen<GT>(raw_g, c, a.N, g);
-                    widen<YT>(raw_y, c, a.N, v);
+                    widen<GT>(raw_g, g);
+                    widen<YT>(raw_y, v);
+                    const int skip = before_column(c, a.N);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) g[i] = i < skip ? 0.0f : g[i], v[i] = i < skip ? 0.0f : v[i];
                 } else {
                     load_short<GT>(a.gradient, at_g, c, a.N, g);
                     load_short<YT>(a.y, at_y, c, a.N, v);
