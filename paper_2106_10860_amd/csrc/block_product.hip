@@ -230,7 +230,7 @@ __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, 
 constexpr int kBufferFlags = 0x00027000;
 constexpr int64_t kMostStride = (int64_t)1 << 23;
 constexpr int kReads = 0x100, kProducts = 0x8;      // kinds of instructions to __builtin_amdgcn_sched_group_barrier
-constexpr int kExpBlocks = 32;          // blocks whose exponents are in LDS at a time
+constexpr int kExpBlocks = 32;          // blocks whose exponents come to LDS at a time
 
 // Four neighbours of a row of out.
 template <int OUT>
@@ -260,13 +260,26 @@ __device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t at, uint32_t 
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(buffer) : "memory", "m0");
 }
 
-// Waits until at most LEFT of this wavefront's loads are under way and all its reads of LDS are done, then for the workgroup's other wavefronts.
+// The same where `wanted` is not 0: a branch that the compiler does not see, and so does not gather other instructions around.
+__device__ __forceinline__ void load_to_lds_if(uint32_t wanted, i32x4 buffer, uint32_t at, uint32_t lds)
+{
+    asm volatile("s_cmp_eq_u32 %3, 0\n\ts_cbranch_scc1 .Lno_load%=\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds\n.Lno_load%=:" ::"s"(lds),
+                 "v"(at), "s"(buffer), "s"(wanted)
+                 : "memory", "m0", "scc");
+}
+
+// Waits until at most LEFT of this wavefront's loads are under way and all its reads of LDS are done.
 template <int LEFT>
-__device__ __forceinline__ void wait_and_meet()
+__device__ __forceinline__ void wait_for_loads()
 {
     static_assert(LEFT < 64);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
 }
+
+__device__ __forceinline__ void wait_for_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Waits for the workgroup's other wavefronts.
+__device__ __forceinline__ void meet() { asm volatile("s_barrier" ::: "memory"); }
 
 // The index among a launch's workgroups that work, such that each of the 8 dies (workgroups go to them in turn) gets neighbours.
 __device__ __forceinline__ uint32_t by_die(uint32_t id, uint32_t total)
@@ -275,16 +288,51 @@ __device__ __forceinline__ uint32_t by_die(uint32_t id, uint32_t total)
     return die * each + min(die, more) + id / 8;
 }
 
+template <int B, int A>
+__device__ __forceinline__ f32x4 multiply(i32x8 b, i32x8 a, f32x4 c, int scale_b, int scale_a)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, B, scale_b, A, scale_a);
+}
+
+// The same with the exponents' bytes as arguments, for calls that are written out.
+__device__ __forceinline__ f32x4 multiply(i32x8 b, i32x8 a, f32x4 c, int scale_b, int byte_b, int scale_a, int byte_a)
+{
+    switch (byte_b * 4 + byte_a) {
+    case 0: return multiply<0, 0>(b, a, c, scale_b, scale_a);
+    case 1: return multiply<0, 1>(b, a, c, scale_b, scale_a);
+    case 2: return multiply<0, 2>(b, a, c, scale_b, scale_a);
+    case 3: return multiply<0, 3>(b, a, c, scale_b, scale_a);
+    case 4: return multiply<1, 0>(b, a, c, scale_b, scale_a);
+    case 5: return multiply<1, 1>(b, a, c, scale_b, scale_a);
+    case 6: return multiply<1, 2>(b, a, c, scale_b, scale_a);
+    case 7: return multiply<1, 3>(b, a, c, scale_b, scale_a);
+    case 8: return multiply<2, 0>(b, a, c, scale_b, scale_a);
+    case 9: return multiply<2, 1>(b, a, c, scale_b, scale_a);
+    case 10: return multiply<2, 2>(b, a, c, scale_b, scale_a);
+    case 11: return multiply<2, 3>(b, a, c, scale_b, scale_a);
+    case 12: return multiply<3, 0>(b, a, c, scale_b, scale_a);
+    case 13: return multiply<3, 1>(b, a, c, scale_b, scale_a);
+    case 14: return multiply<3, 2>(b, a, c, scale_b, scale_a);
+    default: return multiply<3, 3>(b, a, c, scale_b, scale_a);
+    }
+}
+
 // Many rows: BM x BN results to a workgroup of WM x WN wavefronts, each with (BM / WM) x (BN / WN) of them in registers.  Blocks of 128 values
-// of the BM + BN rows go to LDS without passing registers, the next one while this one is multiplied.  A row's eight pieces of 16 bytes lie
-// exchanged by half its index, so that the 16 rows that a read of the lanes goes to fall on all banks.  WIDE: the 16-bit instruction.
+// of the BM + BN rows go to LDS without passing registers, the next ones while this one is multiplied.  A row's eight pieces of 16 bytes lie
+// exchanged by its index, so that the rows that a read of the lanes goes to fall on all banks.  WIDE: the 16-bit instruction.
+//
+// Eight wavefronts are two to a SIMD, and take turns: while one half of them reads its fragments of a block from LDS, the other half multiplies the ones
+// that it has read before.  With all eight reading and then all multiplying the matrix cores were busy 43% of the time (16384 x 4096 x 4096 to bfloat16:
+// 268 us; now 234 us, 2350 TFLOP/s, 0.9 of what the library's product of 8-bit matrices without exponents reaches).  What bounds it now is the way from L2 to LDS: 64 KiB
+// a block, of which one is under way at a time, take 1.0 of the 1.7 us.
 template <int BM, int BN, int WM, int WN, int STAGES, bool WIDE, bool GATHER, int OUT>
 __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) void product_tiles_kernel(ProductArgs p, uint32_t col_tiles)
 {
     constexpr int WAVES = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16, LOADS_A = BM / 8 / WAVES, LOADS_B = BN / 8 / WAVES;
+    static_assert(MT % 4 == 0 && NT % 4 == 0, "a lane's exponents are whole words");
     static_assert(WAVES % 2 == 0 && LOADS_A * 8 * WAVES == BM && LOADS_B * 8 * WAVES == BN, "a wavefront loads whole groups of 8 rows, all at even or all at odd places");
     __shared__ __attribute__((aligned(128))) uint8_t tiles[STAGES][(BM + BN) * kBlock];
-    __shared__ uint32_t exps[kExpBlocks / 4][BM + BN];
+    __shared__ uint32_t exps[2][kExpBlocks][(BM + BN) / 4];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r16 = lane % 16, g = lane / 16;
 
     PieceSearch search;
@@ -298,7 +346,7 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
     if (!find_part(p, search, BM, band * 4 + in_band % height, blockIdx.y, w)) return;
 
     // Rows are addressed by 32-bit offsets within the tile (the launcher keeps row strides to kMostStride).  What lies beyond the tile's last
-    // row is out of the buffers' range; what lies beyond column K is cut off in LDS.
+    // row is out of the buffers' range; what lies beyond column K is cut off from the fragments.
     const uint32_t lda = (uint32_t)p.lda, ldb = (uint32_t)p.ldb, blocks = (uint32_t)ceil_div(w.K, (int64_t)kBlock);
     const uint32_t rows = (uint32_t)(w.last - w.first), cols = (uint32_t)min((int64_t)BN, p.N - n0), width = round_up((uint32_t)w.K, 16u);
     const i32x4 mem_a = buffer_of(p.a + (GATHER ? 0 : w.first * p.lda), ((GATHER ? (uint32_t)p.a_rows : rows) - 1) * lda + width);
@@ -314,20 +362,22 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
     // (keeps the compiler from holding every sum of this and a multiple of a stride in a register of its own)
     auto again = [](uint32_t x) INLINE_LAMBDA { asm volatile("" : "+v"(x)); return x; };
     const uint32_t tiles_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)tiles[0] + wave * 1024;
+    auto load_one = [&](int i, uint32_t stage, uint32_t kb, uint32_t wanted, auto always) INLINE_LAMBDA {
+        const uint32_t to = tiles_at + stage * ((BM + BN) * kBlock) + (i < LOADS_A ? i * WAVES * 1024 : BM * kBlock + (i - LOADS_A) * WAVES * 1024);
+        uint32_t at = i < LOADS_A ? again(at_a) + ((i * WAVES * 8) * lda + kb * kBlock) : again(at_b) + (((i - LOADS_A) * WAVES * 8) * ldb + kb * kBlock);
+        if constexpr (GATHER)
+            if (i < LOADS_A) at = from_a[i < LOADS_A ? i : 0] + kb * kBlock;
+        if constexpr (decltype(always)::value) load_to_lds(i < LOADS_A ? mem_a : mem_b, at, to);
+        else load_to_lds_if(wanted, i < LOADS_A ? mem_a : mem_b, at, to);
+    };
     auto load = [&](uint32_t stage, uint32_t kb) INLINE_LAMBDA {
-        const uint32_t lane_a = again(at_a), lane_b = again(at_b), to = tiles_at + stage * ((BM + BN) * kBlock);
 #pragma unroll
-        for (int i = 0; i < LOADS_A; ++i) {
-            uint32_t at = lane_a + ((i * WAVES * 8) * lda + kb * kBlock);
-            if constexpr (GATHER) at = from_a[i] + kb * kBlock;
-            load_to_lds(mem_a, at, to + i * WAVES * 1024);
-        }
-#pragma unroll
-        for (int i = 0; i < LOADS_B; ++i) load_to_lds(mem_b, lane_b + ((i * WAVES * 8) * ldb + kb * kBlock), to + BM * kBlock + i * WAVES * 1024);
+        for (int i = 0; i < LOADS_A + LOADS_B; ++i) load_one(i, stage, kb, 1, std::true_type{});
     };
     const int wm = wave / WN, wn = wave % WN;
-    // The exponents of kExpBlocks blocks, four to a word, by rows.
-    auto load_exps = [&](uint32_t kb) INLINE_LAMBDA {
+    // The exponents of kExpBlocks blocks: of each block the rows' bytes, those of rows r, r + 16, r + 32 and r + 48 of every 64 in a word.  So a lane gets
+    // those of four fragments at once, and the instruction takes the byte that it needs.
+    auto load_exps = [&](uint32_t chunk_of) INLINE_LAMBDA {
         const uint32_t last_word = (blocks - 1) / 4 * 4;
         for (int row = threadIdx.x; row < BM + BN; row += WAVES * 64) {
             const int64_t m = min(w.first + row, w.last - 1);
@@ -335,87 +385,125 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
                                            : w.scale_b + (min(n0 + row - BM, p.N - 1) >> p.shift_b) * p.lds_b;
             uint32_t words[kExpBlocks / 4];                  // (all on their way before the first is needed; beyond the last block that again)
 #pragma unroll
-            for (int q = 0; q < kExpBlocks / 4; ++q) words[q] = *reinterpret_cast<const uint32_t *>(from + min(kb + q * 4, last_word));
+            for (int q = 0; q < kExpBlocks / 4; ++q) words[q] = *reinterpret_cast<const uint32_t *>(from + min(chunk_of * kExpBlocks + q * 4, last_word));
+            uint8_t *to = reinterpret_cast<uint8_t *>(exps[chunk_of % 2][0]) + row / 64 * 64 + row % 16 * 4 + row % 64 / 16;
 #pragma unroll
-            for (int q = 0; q < kExpBlocks / 4; ++q) exps[q][row] = words[q];
+            for (int k = 0; k < kExpBlocks; ++k) to[k * (BM + BN)] = (uint8_t)(words[k / 4] >> (k % 4 * 8));
         }
     };
     f32x4 acc[MT][NT] = {};
-    const int half0 = r16 * kBlock + (((2 * g) ^ (r16 % 8)) * 16), half1 = r16 * kBlock + (((2 * g + 1) ^ (r16 % 8)) * 16);
+    // A lane's 32 values of a row are pieces g and g + 4: the same ones of both operands, and then a read of the 64 lanes takes 4 clocks (of pieces
+    // 2 g and 2 g + 1 it takes 7).
+    const int half0 = r16 * kBlock + ((g ^ (r16 % 8)) * 16), half1 = half0 ^ 64;
     auto fragment = [&](const uint8_t *tile, int row) INLINE_LAMBDA {
         const i32x4 lo = *reinterpret_cast<const i32x4 *>(tile + row * kBlock + half0), hi = *reinterpret_cast<const i32x4 *>(tile + row * kBlock + half1);
         return i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     };
-    // The columns from K on of the last block, in both operands, to zeros.
-    auto cut_off = [&](uint8_t *tile) INLINE_LAMBDA {
-        for (int row = threadIdx.x; row < BM + BN; row += WAVES * 64)
-            for (int k = (int)(w.K % kBlock); k < kBlock; ++k) tile[row * kBlock + (((k / 16) ^ (row % 8)) * 16 + k % 16)] = 0;
-        __syncthreads();
-    };
     const uint32_t kb0 = (uint32_t)w.kb0, kb1 = (uint32_t)w.kb1;
     if (kb0 < kb1) {
-        for (uint32_t i = 0; i < STAGES - 1; ++i)
+        constexpr int LOADS = LOADS_A + LOADS_B, AHEAD = STAGES - 1;
+        constexpr bool TURNS = WAVES == 8;
+        const bool second = TURNS && wave >= WAVES / 2;      // the half that reads while the first multiplies
+        for (uint32_t i = 0; i < AHEAD; ++i)
             if (kb0 + i < kb1) load(i, kb0 + i);
-        load_exps(kb0 / kExpBlocks * kExpBlocks);
-        uint32_t ea[MT], eb[NT];                             // this block's in the lowest byte
+        // Later chunks are fetched when the one before is a quarter done: its place was the one's before that, which nobody reads any more.
+        const uint32_t chunk0 = kb0 / kExpBlocks;
+        load_exps(chunk0);
+        if (kb0 % kExpBlocks > kExpBlocks / 4) load_exps(chunk0 + 1);
+        if (kb0 + AHEAD <= kb1) wait_for_loads<(AHEAD - 1) * LOADS>();
+        else wait_for_loads<0>();
+        meet();
         uint32_t stage = 0;
-        for (uint32_t kb = kb0; kb < kb1; ++kb) {
-            // this wavefront's part of the block has come, and so has everybody's; nobody reads the last block any more
-            if (kb + STAGES - 2 < kb1) wait_and_meet<(STAGES - 2) * (LOADS_A + LOADS_B)>();
-            else wait_and_meet<0>();
-            if (kb % kExpBlocks == 0 && kb != kb0) {
-                load_exps(kb);
-                __syncthreads();
-            }
-            if (kb + STAGES - 1 < kb1) load(stage == 0 ? STAGES - 1 : stage - 1, kb + STAGES - 1);
-            uint8_t *tile = tiles[stage];
-            stage = stage + 1 == STAGES ? 0 : stage + 1;
-            if (kb + 1 == kb1 && w.K % kBlock) cut_off(tile);
-            if (kb % 4 == 0 || kb == kb0) {
-                const uint32_t *from = exps[kb % kExpBlocks / 4] + r16;
+        if (second) {
+            if (kb0 + AHEAD < kb1) load(AHEAD, kb0 + AHEAD);
+            meet();
+        }
+        for (uint32_t kb = kb0;; ++kb) {
+            const uint32_t free_stage = stage == 0 ? AHEAD : stage - 1;
+            if (!second && kb + AHEAD < kb1) load(free_stage, kb + AHEAD);
+            if (kb % kExpBlocks == kExpBlocks / 4 && kb != kb0 && kb / kExpBlocks * kExpBlocks + kExpBlocks < kb1) load_exps(kb / kExpBlocks + 1);
+            const uint8_t *tile = tiles[stage];
+            const uint32_t *from = exps[kb / kExpBlocks % 2][kb % kExpBlocks] + r16;
+            uint32_t ea[ceil_div(MT, 4)], eb[ceil_div(NT, 4)];
 #pragma unroll
-                for (int t = 0; t < MT; ++t) ea[t] = from[(wm * MT + t) * 16] >> (kb % 4 * 8);
+            for (int t = 0; t < MT; t += 4) ea[t / 4] = from[(wm * MT + t) * 4];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) eb[t] = from[BM + (wn * NT + t) * 16] >> (kb % 4 * 8);
-            }
+            for (int t = 0; t < NT; t += 4) eb[t / 4] = from[BM / 4 + (wn * NT + t) * 4];
             i32x8 b[NT], a[MT];
 #pragma unroll
             for (int j = 0; j < NT; ++j) b[j] = fragment(tile, BM + (wn * NT + j) * 16);
 #pragma unroll
             for (int i = 0; i < MT; ++i) a[i] = fragment(tile, (wm * MT + i) * 16);
-            if constexpr (!WIDE) {
+            if (kb + 1 == kb1 && w.K % kBlock) {
+                const int keep = (int)(w.K % kBlock) - g * 16;
+                i32x8 mask;
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                for (int i = 0; i < 8; ++i) {
+                    const int n = min(max(keep - i % 4 * 4 - i / 4 * 64, 0), 4);
+                    mask[i] = n == 4 ? -1 : (int)((1u << (8 * n)) - 1);
+                }
+#pragma unroll
+                for (int j = 0; j < NT; ++j) b[j] &= mask;
+#pragma unroll
+                for (int i = 0; i < MT; ++i) a[i] &= mask;
+            }
+            // The next block has to have come when the first half reads it, which is when the second half has done so with this one.
+            auto next_has_come = [&]() INLINE_LAMBDA {
+                if (kb + AHEAD < kb1) wait_for_loads<(AHEAD - 1) * LOADS>();
+                else wait_for_loads<0>();
+            };
+            if constexpr (TURNS) {
+                if (second) next_has_come();
+                else wait_for_reads();
+                meet();
+                if (WIDE && second && kb + STAGES < kb1) load(stage, kb + STAGES);
+                __builtin_amdgcn_s_setprio(1);               // (the half that multiplies before the one that reads)
+            }
+            if constexpr (!WIDE) {
+                const uint32_t more = __builtin_amdgcn_readfirstlane(TURNS && second && kb + STAGES < kb1);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
 #pragma unroll
                     for (int j = 0; j < NT; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j], a[i], acc[i][j], 0, 0, 0, (int)eb[j], 0, (int)ea[i]);
-                // B's fragments and two of A's, then two more of A's before the products of the last two
-                __builtin_amdgcn_sched_group_barrier(kReads, 2 * NT + 4, 0);
+                        acc[i][j] = multiply(b[j], a[i], acc[i][j], (int)eb[j / 4], j % 4, (int)ea[i / 4], i % 4);
+                    // the second half's loads among its products, as each takes some time to get away
+                    if constexpr (TURNS) {
 #pragma unroll
-                for (int i = 0; i < MT / 2; ++i) {
-                    if (i + 1 < MT / 2) __builtin_amdgcn_sched_group_barrier(kReads, 4, 0);
-                    __builtin_amdgcn_sched_group_barrier(kProducts, 2 * NT, 0);
+                        for (int l = i * LOADS / MT; l < (i + 1) * LOADS / MT; ++l) load_one(l, stage, kb + STAGES, more, std::false_type{});
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                if constexpr (!TURNS) {
+                    // B's fragments and two of A's, then two more of A's before the products of the last two
+                    __builtin_amdgcn_sched_group_barrier(kReads, 2 * NT + 4, 0);
+#pragma unroll
+                    for (int i = 0; i < MT / 2; ++i) {
+                        if (i + 1 < MT / 2) __builtin_amdgcn_sched_group_barrier(kReads, 4, 0);
+                        __builtin_amdgcn_sched_group_barrier(kProducts, 2 * NT, 0);
+                    }
                 }
             } else {
                 bf16x8 wb[NT][4];
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) wb[j][q] = widen8(b[j][2 * q], b[j][2 * q + 1], as_scale(eb[j] & 255));
+                    for (int q = 0; q < 4; ++q) wb[j][q] = widen8(b[j][2 * q], b[j][2 * q + 1], as_scale(eb[j / 4] >> (j % 4 * 8) & 255));
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const bf16x8 wa = widen8(a[i][2 * q], a[i][2 * q + 1], as_scale(ea[i] & 255));
+                        const bf16x8 wa = widen8(a[i][2 * q], a[i][2 * q + 1], as_scale(ea[i / 4] >> (i % 4 * 8) & 255));
 #pragma unroll
                         for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][q], wa, acc[i][j], 0, 0, 0);
                     }
             }
-#pragma unroll
-            for (int t = 0; t < MT; ++t) ea[t] >>= 8;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) eb[t] >>= 8;
+            if constexpr (TURNS) __builtin_amdgcn_s_setprio(0);
+            if (kb + 1 >= kb1) break;
+            if (!second) next_has_come();
+            meet();
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
+        if (TURNS && !second) meet();                        // (the second half is one behind)
     }
     constexpr int64_t bytes = OUT == kF32 ? 4 : 2;
     const bool wide = (reinterpret_cast<uintptr_t>(p.out) | (uint64_t)(p.ldo * bytes) | (uint64_t)(w.out_at * bytes)) % (4 * bytes) == 0;
