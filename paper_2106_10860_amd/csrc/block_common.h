@@ -116,6 +116,20 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     else return __builtin_bit_cast(uint32_t, (pair_b){(__bf16)a, (__bf16)b});
 }
 
+// N neighbouring results (any alignment to the element) in one store.
+template <int DT, int N>
+__device__ __forceinline__ void store_run(void *base, int64_t at, const float (&v)[N])
+{
+    struct __attribute__((packed, aligned(elem_size(DT)))) Words { uint32_t w[N * elem_size(DT) / 4]; };
+    Words r;
+#pragma unroll
+    for (int i = 0; i < N * elem_size(DT) / 4; ++i) {
+        if constexpr (DT == kF32) r.w[i] = __float_as_uint(v[i]);
+        else r.w[i] = pack2<DT>(v[2 * i], v[2 * i + 1]);
+    }
+    *reinterpret_cast<Words *>(static_cast<char *>(base) + at * elem_size(DT)) = r;
+}
+
 // Entry e of an array of offsets, cut back to 0 .. limit.
 __device__ __forceinline__ int64_t offset_at(const int32_t *offsets, int e, int64_t limit)
 {

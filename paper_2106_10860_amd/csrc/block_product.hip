@@ -232,20 +232,6 @@ constexpr int64_t kMostStride = (int64_t)1 << 23;
 constexpr int kReads = 0x100, kProducts = 0x8;      // kinds of instructions to __builtin_amdgcn_sched_group_barrier
 constexpr int kExpBlocks = 32;          // blocks whose exponents come to LDS at a time
 
-// Four neighbours of a row of out.
-template <int OUT>
-__device__ __forceinline__ void store4(void *out, int64_t at, f32x4 v, int64_t n, int64_t N, bool wide)
-{
-    if (wide && n + 3 < N) {
-        if constexpr (OUT == kF32) *reinterpret_cast<f32x4 *>(static_cast<float *>(out) + at) = v;
-        else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + at) = make_uint2(pack2<OUT>(v[0], v[1]), pack2<OUT>(v[2], v[3]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (n + i < N) store_as<OUT>(out, at + i, v[i]);
-    }
-}
-
 __device__ __forceinline__ i32x4 buffer_of(const uint8_t *base, uint32_t bytes)
 {
     const uint64_t at = reinterpret_cast<uint64_t>(base);
@@ -505,16 +491,21 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
         }
         if (TURNS && !second) meet();                        // (the second half is one behind)
     }
-    constexpr int64_t bytes = OUT == kF32 ? 4 : 2;
-    const bool wide = (reinterpret_cast<uintptr_t>(p.out) | (uint64_t)(p.ldo * bytes) | (uint64_t)(w.out_at * bytes)) % (4 * bytes) == 0;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int64_t m = w.first + (wm * MT + i) * 16 + r16;
         if (m >= w.last || (GATHER && row_of_a(p, m) < 0)) continue;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            const int64_t n = n0 + (wn * NT + j) * 16 + 4 * g;
-            store4<OUT>(p.out, w.out_at + m * p.ldo + n, acc[i][j], n, p.N, wide);
+            const int64_t n = n0 + (wn * NT + j) * 16 + 4 * g, at = w.out_at + m * p.ldo + n;
+            const float four[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+            if (n + 4 <= p.N) {
+                store_run<OUT>(p.out, at, four);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    if (n + k < p.N) store_as<OUT>(p.out, at + k, four[k]);
+            }
         }
     }
 }
@@ -574,10 +565,15 @@ int launch_to(const ProductArgs &p, int a_dtype, hipStream_t stream)
     if (a_dtype == MADDNESS_BF16) return launch_few<kBF16, OUT>(p, stream);
     const int64_t rows = rows_each(p), groups = p.by == MADDNESS_DENSE ? 1 : p.groups;
     const bool far = std::max(p.lda, p.ldb) > kMostStride || (p.source && p.a_rows * p.lda >= (int64_t)1 << 32);
-    // Small products: the few-rows kernel makes more workgroups of them (1024 x 512 x 512 takes 7.0 us instead of 9.0, 128 x 4096 x 4096
-    // 20 instead of 28, 256 x 4096 x 4096 38 instead of 29).
-    const int64_t depth = p.by == MADDNESS_BY_DEPTH ? ceil_div(p.K, groups) : p.K;
-    if (rows <= 64 || far || rows * p.N * depth * groups <= (int64_t)3 << 30) return launch_few<kE4M3, OUT>(p, stream);
+    // Between the two by what they take, in microseconds, fitted to sizes from 300 x 300 x 300 to 1024 x 4096 x 4096: the few-rows kernel makes more workgroups of
+    // a product, and so wins where the other leaves compute units without work (1024 x 512 x 512: 7.0 against 9.0, 128 x 4096 x 4096: 20 against 25,
+    // 256 x 4096 x 4096: 38 against 25).
+    const double blocks = (double)ceil_div(p.by == MADDNESS_BY_DEPTH ? ceil_div(p.K, groups) : p.K, (int64_t)kBlock);
+    const double small = (double)(ceil_div(rows, (int64_t)64) * ceil_div(p.N, (int64_t)32) * groups), tiles = (double)(ceil_div(rows, (int64_t)128) * ceil_div(p.N, (int64_t)128) * groups);
+    const double cus = device_info().cus, step = OUT == kF32 ? 0.85 : 0.6;
+    const double few_us = 5.0 + std::max(1.0, small / cus) * (1.0 + 0.45 * blocks);
+    const double tiles_us = 7.5 + std::max(1.0, tiles / cus) * (tiles > cus ? 0.8 : 1.0) * (1.0 + step * blocks);
+    if (far || (rows <= 64 && p.by != MADDNESS_BY_DEPTH) || few_us <= tiles_us) return launch_few<kE4M3, OUT>(p, stream);
     if (p.source) return launch_shape<true, OUT>(p, rows, groups, stream);
     return launch_shape<false, OUT>(p, rows, groups, stream);
 }

@@ -385,8 +385,9 @@ int launch_route_as(RouteArgs a, hipStream_t stream)
 template <int DT>
 int launch_route_typed(const RouteArgs &a, hipStream_t stream)
 {
-    // 16 lanes to a token while a lane then has at most 16 experts, and a group its lane
-    if (a.groups <= 16) {
+    // 16 lanes to a token while a lane then has at most 16 experts, and a group its lane; but not for so few tokens that each has a SIMD to itself and
+    // the shorter way of fewer experts to a lane counts
+    if (a.groups <= 16 && (a.E <= 64 || a.T > 4 * device_info().cus)) {
         if (a.E <= 16) return launch_route_as<DT, 16, 1>(a, stream);
         if (a.E <= 32) return launch_route_as<DT, 16, 2>(a, stream);
         if (a.E <= 64) return launch_route_as<DT, 16, 4>(a, stream);
@@ -645,19 +646,13 @@ __global__ __launch_bounds__(kWaves * 64) void combine_kernel(CombineArgs a)
             for (int i = 0; i < 8; ++i) sum[i] = p[j] < 0 ? sum[i] : sum[i] + w[j] * v[i];
         }
     }
-    const int n = (int)min(a.N - c, (int64_t)8);
     const int64_t at = t * a.ldo + c;
-    constexpr int bytes = elem_size(OT);
-    if (n == 8 && ((reinterpret_cast<uintptr_t>(a.out) + at * bytes) % 16) == 0) {
-        if constexpr (OT == kF32) {
-            static_cast<f32x4 *>(static_cast<void *>(static_cast<float *>(a.out) + at))[0] = f32x4{sum[0], sum[1], sum[2], sum[3]};
-            static_cast<f32x4 *>(static_cast<void *>(static_cast<float *>(a.out) + at))[1] = f32x4{sum[4], sum[5], sum[6], sum[7]};
-        } else {
-            *static_cast<uint4 *>(static_cast<void *>(static_cast<uint16_t *>(a.out) + at)) =
-                make_uint4(pack2<OT>(sum[0], sum[1]), pack2<OT>(sum[2], sum[3]), pack2<OT>(sum[4], sum[5]), pack2<OT>(sum[6], sum[7]));
-        }
+    if (!shorter) {
+        store_run<OT>(a.out, at, sum);
     } else {
-        for (int i = 0; i < n; ++i) store_as<OT>(a.out, at + i, sum[i]);
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < a.N) store_as<OT>(a.out, at + i, sum[i]);
     }
 }
 
