@@ -183,39 +183,42 @@ __global__ __launch_bounds__(256) void quantise_rows_kernel(QuantiseArgs a, int6
     else if (b == blocks - 1 && b + lane < round_up(blocks, 4u)) s[lane] = 127;
 }
 
-// A tile of 128 x 128 to a workgroup, for transposes and common exponents: a thread holds 8 rows of 8 columns.  The transpose's
-// bytes go through LDS in pieces of 8 (rows of one column), the pieces of a column exchanged by the writer's column group so that
-// the lanes of a write fall on different banks.
+// A tile of 128 x 128 to a workgroup, for transposes and common exponents: a thread holds 4 rows of 8 columns (with 8 rows and half the threads the
+// kernel took 8 to 12 us for any small matrix, most of it the way through its instructions).  The transpose's bytes go through LDS in words of 4
+// rows of one column, the words of a column exchanged by the writer's column group so that the lanes of a write fall on different banks.
+constexpr int kTileThreads = 512, kRowsEach = 4;
+
 template <int DT, bool FACTORS, int TILE>
-__global__ __launch_bounds__(256) void quantise_tiles_kernel(QuantiseArgs a, uint32_t blocks)
+__global__ __launch_bounds__(kTileThreads) void quantise_tiles_kernel(QuantiseArgs a, uint32_t blocks)
 {
     using V = Eight<DT, FACTORS>;
-    __shared__ uint32_t tops[4][kBlock];
-    __shared__ uint2 turned[kBlock * 16];
+    constexpr int WAVES = kTileThreads / 64;
+    __shared__ uint32_t tops[WAVES][kBlock];
+    __shared__ __attribute__((aligned(16))) uint32_t turned[kBlock][kBlock / kRowsEach];
     const int tid = threadIdx.x, cg = tid % 16, rg = tid / 16, wave = tid / 64;
     const uint32_t cb = blockIdx.x % blocks, rb = blockIdx.x / blocks, row_blocks = gridDim.x / blocks;
-    const int64_t m = blockIdx.y, r0 = (int64_t)rb * kBlock + rg * 8;
+    const int64_t m = blockIdx.y, r0 = (int64_t)rb * kBlock + rg * kRowsEach;
     const Columns col((int64_t)cb * kBlock + cg * 8, a.cols);
     const char *x = static_cast<const char *>(a.x) + m * a.stride_x * elem_size(DT);
-    V v[8];
-    float factor[8];
-    bool there[8];
+    V v[kRowsEach];
+    float factor[kRowsEach];
+    bool there[kRowsEach];
     // (rows beyond the end are read as the last: everything is asked for before anything is needed)
 #pragma unroll
-    for (int p = 0; p < 8; ++p) {
+    for (int p = 0; p < kRowsEach; ++p) {
         int64_t at;
         there[p] = find_row(a, min(r0 + p, a.rows - 1), at, factor[p]) && r0 + p < a.rows;
         v[p].load(x, at, col.c, a.cols);
     }
 #pragma unroll
-    for (int p = 0; p < 8; ++p) v[p].keep(col.skip, there[p], factor[p]);
-    uint32_t top_row[8], top_col[V::WORDS];
+    for (int p = 0; p < kRowsEach; ++p) v[p].keep(col.skip, there[p], factor[p]);
+    uint32_t top_row[kRowsEach], top_col[V::WORDS];
     auto largest = [&](auto finite) INLINE_LAMBDA {
         uint32_t all = 0;
 #pragma unroll
         for (int i = 0; i < V::WORDS; ++i) top_col[i] = 0;
 #pragma unroll
-        for (int p = 0; p < 8; ++p) {
+        for (int p = 0; p < kRowsEach; ++p) {
             uint32_t t = 0;
 #pragma unroll
             for (int i = 0; i < V::WORDS; ++i) {
@@ -237,7 +240,7 @@ __global__ __launch_bounds__(256) void quantise_tiles_kernel(QuantiseArgs a, uin
     if constexpr (TILE == 1) {
         if (a.q) {
 #pragma unroll
-            for (int p = 0; p < 8; ++p) {
+            for (int p = 0; p < kRowsEach; ++p) {
                 const uint32_t byte = exponent_byte(row16_max(V::fp32_bits(top_row[p])));
                 store_rows(p, __uint_as_float(byte << 23));
                 if (r0 + p >= a.rows) continue;
@@ -259,33 +262,40 @@ __global__ __launch_bounds__(256) void quantise_tiles_kernel(QuantiseArgs a, uin
                 if (i >= col.skip) tops[wave][cg * 8 + i - col.skip] = V::PAIRS ? top_col[i / (8 / V::WORDS)] >> (i % 2 * 16) & 0xffffu : top_col[i / (8 / V::WORDS)];
         }
         __syncthreads();
+        // each column's exponent once, for all
+        if (tid < kBlock) {
+            uint32_t t = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int k = cg * 8 + max(i - col.skip, 0);
-            const uint32_t byte = exponent_byte(V::fp32_bits(max(max(tops[0][k], tops[1][k]), max(tops[2][k], tops[3][k]))));
-            scale_col[i] = __uint_as_float(byte << 23);
-            const int64_t c = col.c + i - col.skip;
-            if (rg == 0 && i >= col.skip && c < a.cols) {
+            for (int k = 0; k < WAVES; ++k) t = max(t, tops[k][tid]);
+            const uint32_t byte = exponent_byte(V::fp32_bits(t));
+            tops[0][tid] = byte;
+            const int64_t c = (int64_t)cb * kBlock + tid;
+            if (c < a.cols) {
                 uint8_t *s = a.scale_t + (m * a.cols + c) * a.ldst + rb;
                 *s = (uint8_t)byte;
                 if (rb == row_blocks - 1)
                     for (uint32_t pad = rb + 1; pad < round_up(row_blocks, 4u); ++pad) *++s = 127;
             }
         }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) scale_col[i] = __uint_as_float(tops[0][cg * 8 + max(i - col.skip, 0)] << 23);
     } else {
         uint32_t top = 0;
 #pragma unroll
-        for (int p = 0; p < 8; ++p) top = max(top, top_row[p]);
+        for (int p = 0; p < kRowsEach; ++p) top = max(top, top_row[p]);
         top = row16_max(top);
         top = max(top, (uint32_t)__shfl_xor((int)top, 16));
         top = max(top, (uint32_t)__shfl_xor((int)top, 32));
         if (tid % 64 == 0) tops[wave][0] = top;
         __syncthreads();
-        const uint32_t byte = exponent_byte(V::fp32_bits(max(max(tops[0][0], tops[1][0]), max(tops[2][0], tops[3][0]))));
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) top = max(top, tops[k][0]);
+        const uint32_t byte = exponent_byte(V::fp32_bits(top));
         scale_tile = __uint_as_float(byte << 23);
         if (a.q) {
 #pragma unroll
-            for (int p = 0; p < 8; ++p) store_rows(p, scale_tile);
+            for (int p = 0; p < kRowsEach; ++p) store_rows(p, scale_tile);
             if (tid < 4) {
                 uint8_t *s = a.scale + (m * row_blocks + rb) * a.lds + cb;
                 if (tid == 0) *s = (uint8_t)byte;
@@ -302,31 +312,28 @@ __global__ __launch_bounds__(256) void quantise_tiles_kernel(QuantiseArgs a, uin
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float scale = TILE == 1 ? scale_col[i] : scale_tile;
-        i16x2 bytes[2] = {};
+        i16x2 bytes = {0, 0};
 #pragma unroll
-        for (int p = 0; p < 8; p += 2) {
-            i16x2 &to = bytes[p / 4];
+        for (int p = 0; p < kRowsEach; p += 2) {
             if constexpr (V::PAIRS) {
                 const uint32_t a0 = v[p].w[i / 2], a1 = v[p + 1].w[i / 2];
                 const uint32_t pair = i % 2 ? __builtin_amdgcn_perm(a1, a0, 0x07060302) : __builtin_amdgcn_perm(a1, a0, 0x05040100);
-                to = p % 4 ? convert_pair<DT, true>(to, pair, scale) : convert_pair<DT, false>(to, pair, scale);
+                bytes = p ? convert_pair<DT, true>(bytes, pair, scale) : convert_pair<DT, false>(bytes, pair, scale);
             } else {
                 const float f0 = __uint_as_float(v[p].w[i]), f1 = __uint_as_float(v[p + 1].w[i]);
-                to = p % 4 ? convert<true>(to, f0, f1, scale) : convert<false>(to, f0, f1, scale);
+                bytes = p ? convert<true>(bytes, f0, f1, scale) : convert<false>(bytes, f0, f1, scale);
             }
         }
-        if (i >= col.skip)
-            turned[(cg * 8 + i - col.skip) * 16 + (rg ^ cg)] = make_uint2(__builtin_bit_cast(uint32_t, bytes[0]), __builtin_bit_cast(uint32_t, bytes[1]));
+        if (i >= col.skip) turned[cg * 8 + i - col.skip][rg ^ (cg % 8 * 4)] = __builtin_bit_cast(uint32_t, bytes);
     }
     __syncthreads();
     const int64_t row_end = round_up(a.rows, (int64_t)16);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int at = k * 256 + tid, out_col = at / 8, piece = at % 8;
+    for (int k = 0; k < kBlock * 8 / kTileThreads; ++k) {
+        const int at = k * kTileThreads + tid, out_col = at / 8, piece = at % 8;
         const int64_t row = (int64_t)cb * kBlock + out_col, c = (int64_t)rb * kBlock + piece * 16;
         if (row >= a.cols || c >= row_end) continue;
-        const uint2 lo = turned[out_col * 16 + ((piece * 2) ^ (out_col / 8))], hi = turned[out_col * 16 + ((piece * 2 + 1) ^ (out_col / 8))];
-        *reinterpret_cast<uint4 *>(a.qt + (m * a.cols + row) * a.ldqt + c) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        *reinterpret_cast<uint4 *>(a.qt + (m * a.cols + row) * a.ldqt + c) = *reinterpret_cast<const uint4 *>(&turned[out_col][(piece * 4) ^ (out_col / 8 % 8 * 4)]);
     }
 }
 
@@ -349,8 +356,8 @@ int launch_typed(const QuantiseArgs &a, int64_t count, int tile, hipStream_t str
     }
     const dim3 grid((unsigned)(blocks * ceil_div(a.rows, (int64_t)kBlock)), (unsigned)count);
     note_kernel("quantise_tiles_kernel", __PRETTY_FUNCTION__);
-    if (tile == 1) hipLaunchKernelGGL((quantise_tiles_kernel<DT, FACTORS, 1>), grid, dim3(256), 0, stream, a, (uint32_t)blocks);
-    else hipLaunchKernelGGL((quantise_tiles_kernel<DT, FACTORS, kBlock>), grid, dim3(256), 0, stream, a, (uint32_t)blocks);
+    if (tile == 1) hipLaunchKernelGGL((quantise_tiles_kernel<DT, FACTORS, 1>), grid, dim3(kTileThreads), 0, stream, a, (uint32_t)blocks);
+    else hipLaunchKernelGGL((quantise_tiles_kernel<DT, FACTORS, kBlock>), grid, dim3(kTileThreads), 0, stream, a, (uint32_t)blocks);
     return check_hip(hipGetLastError(), "launch quantise_tiles_kernel");
 }
 
