@@ -433,6 +433,19 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
 #pragma unroll
                 for (int i = 0; i < MT; ++i) a[i] &= mask;
             }
+            bf16x8 wb[WIDE ? NT : 1][4], wa[WIDE && TURNS ? MT : 1][4];
+            auto widen_fragment = [&](const i32x8 &v, uint32_t byte, bf16x8 (&to)[4]) INLINE_LAMBDA {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) to[q] = widen8(v[2 * q], v[2 * q + 1], as_scale(byte & 255));
+            };
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) widen_fragment(b[j], eb[j / 4] >> (j % 4 * 8), wb[j]);
+                if constexpr (TURNS) {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) widen_fragment(a[i], ea[i / 4] >> (i % 4 * 8), wa[i]);
+                }
+            }
             // The next block has to have come when the first half reads it, which is when the second half has done so with this one.
             auto next_has_come = [&]() INLINE_LAMBDA {
                 if (kb + AHEAD < kb1) wait_for_loads<(AHEAD - 1) * LOADS>();
@@ -442,7 +455,6 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
                 if (second) next_has_come();
                 else wait_for_reads();
                 meet();
-                if (WIDE && second && kb + STAGES < kb1) load(stage, kb + STAGES);
                 __builtin_amdgcn_s_setprio(1);               // (the half that multiplies before the one that reads)
             }
             if constexpr (!WIDE) {
@@ -469,19 +481,21 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
                     }
                 }
             } else {
-                bf16x8 wb[NT][4];
+                const uint32_t more = __builtin_amdgcn_readfirstlane(TURNS && second && kb + STAGES < kb1);
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
+                for (int i = 0; i < MT; ++i) {
+                    if constexpr (!TURNS) widen_fragment(a[i], ea[i / 4] >> (i % 4 * 8), wa[0]);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) wb[j][q] = widen8(b[j][2 * q], b[j][2 * q + 1], as_scale(eb[j / 4] >> (j % 4 * 8) & 255));
+                    for (int q = 0; q < 4; ++q)
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                        for (int j = 0; j < NT; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][q], wa[TURNS ? i : 0][q], acc[i][j], 0, 0, 0);
+                    if constexpr (TURNS) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const bf16x8 wa = widen8(a[i][2 * q], a[i][2 * q + 1], as_scale(ea[i / 4] >> (i % 4 * 8) & 255));
-#pragma unroll
-                        for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][q], wa, acc[i][j], 0, 0, 0);
+                        for (int l = i * LOADS / MT; l < (i + 1) * LOADS / MT; ++l) load_one(l, stage, kb + STAGES, more, std::false_type{});
+                        __builtin_amdgcn_sched_barrier(0);
                     }
+                }
             }
             if constexpr (TURNS) __builtin_amdgcn_s_setprio(0);
             if (kb + 1 >= kb1) break;
@@ -549,10 +563,16 @@ int launch_few(const ProductArgs &p, hipStream_t stream)
 template <bool GATHER, int OUT>
 int launch_shape(const ProductArgs &p, int64_t rows, int64_t groups, hipStream_t stream)
 {
-    if constexpr (OUT != kF32) {
-        // 256 x 256 to a workgroup: less to read for each product, but only where there is one for every compute unit
-        const int64_t large = ceil_div(rows, (int64_t)256) * ceil_div(p.N, (int64_t)256) * groups;
-        if (!GATHER && large >= device_info().cus && rows >= 1024) return launch_tiles<256, 256, 2, 4, 2, false, OUT>(p, stream);
+    // Larger tiles have less to read for each product, but need enough of them for every compute unit: 256 x 256 one each (8192 x 4096 x 4096 to
+    // bfloat16 127 us, 143 by 128 x 128; 2048 x 4096 x 4096 57 and 38), of 256 x 128 with the 16-bit instruction two (225 and 241 us; 62 and 66).  Rows that
+    // are gathered come in short pieces, which larger tiles leave half empty.
+    if constexpr (!GATHER) {
+        constexpr int64_t BN = OUT == kF32 ? 128 : 256;
+        const int64_t large = ceil_div(rows, (int64_t)256) * ceil_div(p.N, BN) * groups;
+        if (rows >= 1024 && large >= (OUT == kF32 ? 2 : 1) * device_info().cus) {
+            if constexpr (OUT == kF32) return launch_tiles<256, 128, 4, 2, 2, false, OUT>(p, stream);
+            else return launch_tiles<256, 256, 2, 4, 2, false, OUT>(p, stream);
+        }
     }
     return launch_tiles<128, 128, 2, 2, 2, GATHER, OUT>(p, stream);
 }
