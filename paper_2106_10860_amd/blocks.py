@@ -28,6 +28,19 @@ def _up(n: int, to: int) -> int:
     return -(-n // to) * to
 
 
+def _on(stream):
+    """A call with ``stream`` runs with that as the current one, so that its results and workspace are that stream's memory too: nothing
+    else gets it before the call's kernels are done with it."""
+    torch = _m._torch or _m._torch_module()
+    return torch.cuda.stream(stream)
+
+
+def _fits(**numbers) -> None:
+    for name, v in numbers.items():
+        if not -_INT_MAX - 1 <= v <= _INT_MAX:
+            raise ValueError(f"{name} = {v} does not fit 32 bits")
+
+
 def _code(t, name: str) -> int:
     """The dtype code of a floating device tensor."""
     torch = _m._torch or _m._torch_module()
@@ -139,7 +152,10 @@ def maddness_quantise_blocks(x, tile: int = 1, transposed: bool = False, both: b
 
     ``source`` (int32 [rows']): row r of the result is x[source[r] // repeat] (times factors[source[r]] where ``factors``, fp32, is
     given), zeros where source[r] is negative; x is 2-D then."""
-    r = _m._native.quantise_blocks(x, tile, transposed, both, source, repeat, factors, stream)
+    if stream is not None:
+        with _on(stream):
+            return maddness_quantise_blocks(x, tile, transposed, both, source, repeat, factors)
+    r = _m._native.quantise_blocks(x, tile, transposed, both, source, repeat, factors)
     if r is not NotImplemented:
         r = _m._done(r)
         return (BlockMatrix._made(r[0], r[1], tile), BlockMatrix._made(r[2], r[3], tile)) if both else BlockMatrix._made(r[0], r[1], tile)
@@ -162,6 +178,7 @@ def maddness_quantise_blocks(x, tile: int = 1, transposed: bool = False, both: b
     else:
         if source.dim() != 1 or repeat < 1:
             raise ValueError("source must be 1-D and repeat >= 1")
+        _fits(repeat=repeat)
         _same_device(x, source, factors)
         rows = source.shape[0]
         source_p = _flat(source, torch.int32, (rows,), "source")
@@ -172,7 +189,7 @@ def maddness_quantise_blocks(x, tile: int = 1, transposed: bool = False, both: b
     _m._check(_m.lib().maddness_quantise_blocks(
         x.data_ptr(), code, count, rows, cols, ldx, stride_x, tile, source_p, x_rows, repeat, factors_p,
         s and s.data, s.ld if s else 0, s and s.scale, s.lds if s else 0, t and t.data, t.ld if t else 0, t and t.scale, t.lds if t else 0,
-        _m._stream(stream)))
+        _m._stream(None)))
     return (a, b) if both else (b if transposed else a)
 
 
@@ -189,7 +206,10 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", so
         raise TypeError("B must be a BlockMatrix")
     if by != "rows" and by != "depth":
         raise ValueError(f"by must be 'rows' or 'depth', is {by!r}")
-    r = _m._native.block_product(isinstance(A, BlockMatrix), A, B, offsets, by == "depth", source, repeat, out_dtype, out, workspace, stream)
+    if stream is not None:
+        with _on(stream):
+            return maddness_block_product(A, B, offsets, by, source, repeat, out_dtype, out, workspace)
+    r = _m._native.block_product(isinstance(A, BlockMatrix), A, B, offsets, by == "depth", source, repeat, out_dtype, out, workspace)
     if r is not NotImplemented:
         return _m._done(r)
     torch = _m._torch or _m._torch_module()
@@ -205,8 +225,9 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", so
     if source is not None:
         if offsets is None or by != "rows" or source.dim() != 1 or repeat < 1:
             raise ValueError("source must be 1-D, with offsets, by='rows' and repeat >= 1")
+        _fits(repeat=repeat)
         M = source.shape[0]
-        source_p = _flat(source, torch.int32, (M,), "source")
+        source_p = _flat(source, torch.int32, (M,), "source") if M else offsets.data_ptr()      # (an empty one may have no address, and is not read)
     if offsets is None:
         how, groups, offsets_p, lead = MADDNESS_DENSE, 1, None, ()
         if len(B.shape) != 2:
@@ -235,7 +256,7 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", so
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
     _m._check(L.maddness_block_product(C.byref(a), C.byref(B._struct), how, groups, offsets_p, source_p, M, repeat, out.data_ptr(), _code(out, "out"), ldo,
                                        _m._ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(),
-                                       _m._stream(stream)))
+                                       _m._stream(None)))
     return out
 
 
@@ -248,7 +269,10 @@ def _scores(scores: str) -> int:
 def maddness_route(logits, k: int, scores: str = "softmax", bias=None, groups: int = 1, kept_groups: int = 1, renormalise: bool = True,
                    factor: float = 1.0, stream=None):
     """Which k experts each token goes to, and with which weights: (ids int32 [T, k], -1 where there is none; weights fp32 [T, k])."""
-    r = _m._native.route(logits, k, _scores(scores) == 1, bias, groups, kept_groups, renormalise, factor, stream)
+    if stream is not None:
+        with _on(stream):
+            return maddness_route(logits, k, scores, bias, groups, kept_groups, renormalise, factor)
+    r = _m._native.route(logits, k, _scores(scores) == 1, bias, groups, kept_groups, renormalise, factor)
     if r is not NotImplemented:
         return _m._done(r)
     torch = _m._torch or _m._torch_module()
@@ -256,18 +280,22 @@ def maddness_route(logits, k: int, scores: str = "softmax", bias=None, groups: i
     T, E, ldl = _m._rows(logits, "logits")
     _same_device(logits, bias)
     bias_p = _flat(bias, torch.float32, (E,), "bias")
-    if not 0 < k <= _INT_MAX:
+    _fits(k=k, groups=groups, kept_groups=kept_groups)
+    if k < 1:
         raise ValueError(f"k must be positive, is {k}")
     ids = torch.empty((T, k), dtype=torch.int32, device=logits.device)
     weights = torch.empty((T, k), dtype=torch.float32, device=logits.device)
     _m._check(_m.lib().maddness_route(logits.data_ptr(), code, T, E, ldl, bias_p, _scores(scores), groups, kept_groups, k,
-                                      1 if renormalise else 0, factor, ids.data_ptr(), weights.data_ptr(), _m._stream(stream)))
+                                      1 if renormalise else 0, factor, ids.data_ptr(), weights.data_ptr(), _m._stream(None)))
     return ids, weights
 
 
 def maddness_route_gradient(logits, ids, weights_gradient, scores: str = "softmax", renormalise: bool = True, factor: float = 1.0, stream=None):
     """The gradient of the logits (their dtype, [T, E]) from that of the weights that maddness_route gave with these ids."""
-    r = _m._native.route_gradient(logits, ids, weights_gradient, _scores(scores) == 1, renormalise, factor, stream)
+    if stream is not None:
+        with _on(stream):
+            return maddness_route_gradient(logits, ids, weights_gradient, scores, renormalise, factor)
+    r = _m._native.route_gradient(logits, ids, weights_gradient, _scores(scores) == 1, renormalise, factor)
     if r is not NotImplemented:
         return _m._done(r)
     torch = _m._torch or _m._torch_module()
@@ -281,14 +309,17 @@ def maddness_route_gradient(logits, ids, weights_gradient, scores: str = "softma
     dw_p = _flat(weights_gradient, torch.float32, (T, k), "weights_gradient")
     out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
     _m._check(_m.lib().maddness_route_gradient(logits.data_ptr(), code, T, E, ldl, _scores(scores), k, 1 if renormalise else 0, factor, ids_p,
-                                               dw_p, out.data_ptr(), E, _m._stream(stream)))
+                                               dw_p, out.data_ptr(), E, _m._stream(None)))
     return out
 
 
 def maddness_order(ids, experts: int, align: int = 1, stream=None):
     """The slots (choice j of token t is slot t * k + j) in the order of their experts: (offsets int32 [experts + 1], each expert's places
     a multiple of ``align``; counts int32 [experts]; source int32 [places], the slot at each place or -1; place int32 of ids' shape, or -1)."""
-    r = _m._native.order(ids, experts, align, stream)
+    if stream is not None:
+        with _on(stream):
+            return maddness_order(ids, experts, align)
+    r = _m._native.order(ids, experts, align)
     if r is not NotImplemented:
         return _m._done(r)
     torch = _m._torch or _m._torch_module()
@@ -302,13 +333,16 @@ def maddness_order(ids, experts: int, align: int = 1, stream=None):
     offsets, counts, source, workspace = ints.split([experts + 1, experts, capacity, need // 4])
     place = torch.empty(ids.shape, dtype=torch.int32, device=dev)
     _m._check(L.maddness_order(ids_p, slots, experts, align, offsets.data_ptr(), counts.data_ptr(), source.data_ptr(), capacity,
-                               place.data_ptr(), workspace.data_ptr(), need, _m._stream(stream)))
+                               place.data_ptr(), workspace.data_ptr(), need, _m._stream(None)))
     return offsets, counts, source, place
 
 
 def maddness_combine(y, place, weights=None, out_dtype=None, out=None, stream=None):
     """out[t] = sum over j of weights[t, j] * y[place[t, j]]; a negative place adds nothing, weights None are 1."""
-    r = _m._native.combine(y, place, weights, out_dtype, out, stream)
+    if stream is not None:
+        with _on(stream):
+            return maddness_combine(y, place, weights, out_dtype, out)
+    r = _m._native.combine(y, place, weights, out_dtype, out)
     if r is not NotImplemented:
         return _m._done(r)
     torch = _m._torch or _m._torch_module()
@@ -324,14 +358,17 @@ def maddness_combine(y, place, weights=None, out_dtype=None, out=None, stream=No
     _same_device(y, place, weights, out)
     _m._check(_m.lib().maddness_combine(y.data_ptr(), code, rows, N, ldy, _flat(place, torch.int32, (T, k), "place"),
                                         _flat(weights, torch.float32, (T, k), "weights"), T, k, out.data_ptr(), _code(out, "out"),
-                                        _m._rows(out, "out")[2], _m._stream(stream)))
+                                        _m._rows(out, "out")[2], _m._stream(None)))
     return out
 
 
 def maddness_combine_gradient(gradient, y, place, stream=None):
     """The gradient of maddness_combine's weights, fp32 [T, k].  (That of y: maddness_quantise_blocks of the gradient with ``source``
     and ``factors``, or the gradient's rows times the weights.)"""
-    r = _m._native.combine_gradient(gradient, y, place, stream)
+    if stream is not None:
+        with _on(stream):
+            return maddness_combine_gradient(gradient, y, place)
+    r = _m._native.combine_gradient(gradient, y, place)
     if r is not NotImplemented:
         return _m._done(r)
     torch = _m._torch or _m._torch_module()
@@ -344,5 +381,5 @@ def maddness_combine_gradient(gradient, y, place, stream=None):
     _same_device(gradient, y, place)
     out = torch.empty((T, k), dtype=torch.float32, device=y.device)
     _m._check(_m.lib().maddness_combine_gradient(gradient.data_ptr(), code, ldg, y.data_ptr(), y_code, rows, N, ldy,
-                                                 _flat(place, torch.int32, (T, k), "place"), T, k, out.data_ptr(), _m._stream(stream)))
+                                                 _flat(place, torch.int32, (T, k), "place"), T, k, out.data_ptr(), _m._stream(None)))
     return out

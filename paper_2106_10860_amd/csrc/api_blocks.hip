@@ -98,10 +98,9 @@ int maddness_quantise_blocks(const void *x, int32_t dtype, int64_t count, int64_
         if ((rc = check_size(source_rows, "source_rows")) != MADDNESS_OK) return rc;
         if (source_rows * repeat > kMostRows) return fail(MADDNESS_E_UNSUPPORTED, "source_rows repeat = %lld, supported are up to 2^31 - 1", (long long)(source_rows * repeat));
         if (!aligned(source, 4) || !aligned(factors, 4)) return fail(MADDNESS_E_ALIGN, "source / factors not 4-byte aligned");
-    } else if (factors) {
-        return fail(MADDNESS_E_INVAL, "factors without source");
     }
     if (count == 0 || rows == 0 || cols == 0) return MADDNESS_OK;
+    if (factors && !source) return fail(MADDNESS_E_INVAL, "factors without source");
     if ((rc = check_floats(x, dtype, source ? source_rows : rows, cols, ldx, "x")) != MADDNESS_OK) return rc;
     if (!q && !qt) return fail(MADDNESS_E_INVAL, "both q and qt are NULL");
     if (q && (rc = check_blocks(q, cols, ldq, 0, scale, lds, 0, "q")) != MADDNESS_OK) return rc;

@@ -410,11 +410,11 @@ NewBlocks new_blocks(int64_t count, int64_t rows, int64_t cols, int64_t tile, co
     return b;
 }
 
-// (x, tile, transposed, both, source, repeat, factors, stream) -> (q, scale) or (q, scale, qt, scale_t)
+// (x, tile, transposed, both, source, repeat, factors) -> (q, scale) or (q, scale, qt, scale_t)
 PyObject *quantise_blocks(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
-        if (n != 8) throw NotUsual();
+        if (n != 7) throw NotUsual();
         const at::Tensor &x = tensor(a[0]);
         const int code = float_code(x.scalar_type());
         const int64_t tile = whole(a[1]);
@@ -438,7 +438,7 @@ PyObject *quantise_blocks(PyObject *, PyObject *const *a, Py_ssize_t n)
         } else if (a[6] != Py_None) {
             throw NotUsual();
         }
-        void *stream = stream_of(a[7]);
+        void *stream = stream_of(Py_None);
         NewBlocks straight, turned;
         if (both || !transposed) straight = new_blocks(-1, rows, rx.cols, tile, x.device());
         if (both || transposed) turned = new_blocks(-1, rx.cols, rows, tile, x.device());
@@ -462,11 +462,11 @@ PyObject *quantise_blocks(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (a_is_blocks, A, B, offsets, by_depth, source, repeat, out_dtype, out, workspace, stream) -> out
+// (a_is_blocks, A, B, offsets, by_depth, source, repeat, out_dtype, out, workspace) -> out
 PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
-        if (n != 11) throw NotUsual();
+        if (n != 10) throw NotUsual();
         at::Device device(at::kCPU);
         maddness_block_matrix A{}, B{};
         int64_t experts = -1;
@@ -505,9 +505,9 @@ PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
             if (by != MADDNESS_BY_ROWS || s.dim() != 1 || s.scalar_type() != at::kInt || !s.is_contiguous() || s.device() != device || repeat < 1)
                 throw NotUsual();
             rows = s.size(0);
-            source = static_cast<const int32_t *>(s.data_ptr());
+            source = rows ? static_cast<const int32_t *>(s.data_ptr()) : offsets;      // (an empty one may have no address, and is not read)
         }
-        void *stream = stream_of(a[10]);
+        void *stream = stream_of(Py_None);
         at::Tensor made, work;
         const at::ScalarType type = dtype_or(a[7], at::kBFloat16);
         void *out;
@@ -550,11 +550,11 @@ PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (logits, k, sigmoid, bias, groups, kept, renormalise, factor, stream) -> (ids, weights)
+// (logits, k, sigmoid, bias, groups, kept, renormalise, factor) -> (ids, weights)
 PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
-        if (n != 9 || !PyFloat_CheckExact(a[7])) throw NotUsual();
+        if (n != 8 || !PyFloat_CheckExact(a[7])) throw NotUsual();
         const at::Tensor &x = tensor(a[0]);
         const int code = float_code(x.scalar_type());
         const Rows r = rows_of(x);
@@ -562,7 +562,7 @@ PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n)
         const bool sigmoid = truth(a[2]), renormalise = truth(a[6]);
         if (k < 1 || r.cols > MADDNESS_MAX_EXPERTS) throw NotUsual();
         const float *bias = flat_or_null<const float>(a[3], at::kFloat, {r.cols}, x.device());
-        void *stream = stream_of(a[8]);
+        void *stream = stream_of(Py_None);
         const auto opt = at::TensorOptions().device(x.device());
         at::Tensor ids = at::empty({r.rows, k}, opt.dtype(at::kInt)), weights = at::empty({r.rows, k}, opt.dtype(at::kFloat));
         int32_t *ids_p = static_cast<int32_t *>(ids.data_ptr());
@@ -582,11 +582,11 @@ PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (logits, ids, weights_gradient, sigmoid, renormalise, factor, stream) -> gradient
+// (logits, ids, weights_gradient, sigmoid, renormalise, factor) -> gradient
 PyObject *route_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
-        if (n != 7 || !PyFloat_CheckExact(a[5])) throw NotUsual();
+        if (n != 6 || !PyFloat_CheckExact(a[5])) throw NotUsual();
         const at::Tensor &x = tensor(a[0]), &ids = tensor(a[1]);
         const int code = float_code(x.scalar_type());
         const Rows r = rows_of(x);
@@ -595,7 +595,7 @@ PyObject *route_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int32_t *ids_p = flat_or_null<const int32_t>(a[1], at::kInt, {r.rows, k}, x.device());
         const float *dw = flat_or_null<const float>(a[2], at::kFloat, {r.rows, k}, x.device());
         const bool sigmoid = truth(a[3]), renormalise = truth(a[4]);
-        void *stream = stream_of(a[6]);
+        void *stream = stream_of(Py_None);
         at::Tensor out = at::empty({r.rows, r.cols}, x.options());
         const void *x_p = x.data_ptr();
         void *out_p = out.data_ptr();
@@ -610,18 +610,18 @@ PyObject *route_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (ids, experts, align, stream) -> (offsets, counts, source, place)
+// (ids, experts, align) -> (offsets, counts, source, place)
 PyObject *order(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
-        if (n != 4) throw NotUsual();
+        if (n != 3) throw NotUsual();
         const at::Tensor &ids = tensor(a[0]);
         if (ids.scalar_type() != at::kInt || !ids.is_contiguous()) throw NotUsual();
         const int32_t E = narrow(whole(a[1])), align = narrow(whole(a[2]));
         if (E < 1 || E > MADDNESS_MAX_EXPERTS || align < 1) throw NotUsual();
         const int64_t slots = ids.numel(), capacity = maddness_order_capacity(slots, E, align);
         const int64_t work = ((int64_t)maddness_order_workspace(slots, E) + 3) / 4;
-        void *stream = stream_of(a[3]);
+        void *stream = stream_of(Py_None);
         const auto opt = ids.options();
         // one piece of memory: source first, for its alignment
         at::Tensor all = at::empty({capacity + E + 1 + E + work}, opt), place = at::empty(ids.sizes(), opt);
@@ -642,11 +642,11 @@ PyObject *order(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (y, place, weights, out_dtype, out, stream) -> out
+// (y, place, weights, out_dtype, out) -> out
 PyObject *combine(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
-        if (n != 6) throw NotUsual();
+        if (n != 5) throw NotUsual();
         const at::Tensor &y = tensor(a[0]), &place = tensor(a[1]);
         const int code = float_code(y.scalar_type());
         const Rows r = rows_of(y);
@@ -657,7 +657,7 @@ PyObject *combine(PyObject *, PyObject *const *a, Py_ssize_t n)
         const float *weights = flat_or_null<const float>(a[2], at::kFloat, {T, k}, y.device());
         const at::ScalarType type = dtype_or(a[3], y.scalar_type());
         const int out_code = float_code(type);
-        void *stream = stream_of(a[5]);
+        void *stream = stream_of(Py_None);
         at::Tensor out = at::empty({T, r.cols}, y.options().dtype(type));
         const void *y_p = y.data_ptr();
         void *out_p = out.data_ptr();
@@ -670,18 +670,18 @@ PyObject *combine(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (gradient, y, place, stream) -> weights_gradient
+// (gradient, y, place) -> weights_gradient
 PyObject *combine_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
-        if (n != 4) throw NotUsual();
+        if (n != 3) throw NotUsual();
         const at::Tensor &g = tensor(a[0]), &y = tensor(a[1]), &place = tensor(a[2]);
         const int code = float_code(g.scalar_type()), y_code = float_code(y.scalar_type());
         const Rows rg = rows_of(g), ry = rows_of(y);
         if (place.dim() != 2 || rg.cols != ry.cols || g.device() != y.device()) throw NotUsual();
         const int32_t k = narrow(place.size(1));
         const int32_t *place_p = flat_or_null<const int32_t>(a[2], at::kInt, {rg.rows, k}, y.device());
-        void *stream = stream_of(a[3]);
+        void *stream = stream_of(Py_None);
         at::Tensor out = at::empty({rg.rows, k}, y.options().dtype(at::kFloat));
         const void *g_p = g.data_ptr(), *y_p = y.data_ptr();
         float *out_p = static_cast<float *>(out.data_ptr());

@@ -10,6 +10,7 @@ namespace maddness {
 
 constexpr int kE4M3 = MADDNESS_E4M3;
 constexpr int kBlock = MADDNESS_BLOCK;
+constexpr int64_t kMostThreads = ((int64_t)1 << 32) - 1;        // that a dimension of a launch may have
 
 using i32x4 = __attribute__((ext_vector_type(4))) int;
 using i32x8 = __attribute__((ext_vector_type(8))) int;

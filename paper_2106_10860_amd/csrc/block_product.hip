@@ -240,7 +240,7 @@ __device__ __forceinline__ i32x4 buffer_of(const uint8_t *base, uint32_t bytes)
 }
 
 // 16 bytes for each lane from `at` in the buffer to lds + 16 lane, past the registers; zeros from beyond its end.  As text, because the compiler
-// waits for all such loads before any read of LDS: wait_and_meet waits for those that the next block needs.
+// waits for all such loads before any read of LDS, the next block's too: wait_for_loads is called where they are needed.
 __device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t at, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(buffer) : "memory", "m0");
@@ -254,13 +254,8 @@ __device__ __forceinline__ void load_to_lds_if(uint32_t wanted, i32x4 buffer, ui
                  : "memory", "m0", "scc");
 }
 
-// Waits until at most LEFT of this wavefront's loads are under way and all its reads of LDS are done.
-template <int LEFT>
-__device__ __forceinline__ void wait_for_loads()
-{
-    static_assert(LEFT < 64);
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
-}
+// Waits until this wavefront's loads have come and its reads of LDS are done.
+__device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 __device__ __forceinline__ void wait_for_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
@@ -311,13 +306,13 @@ __device__ __forceinline__ f32x4 multiply(i32x8 b, i32x8 a, f32x4 c, int scale_b
 // that it has read before.  With all eight reading and then all multiplying the matrix cores were busy 43% of the time (16384 x 4096 x 4096 to bfloat16:
 // 268 us; now 234 us, 2350 TFLOP/s, 0.9 of what the library's product of 8-bit matrices without exponents reaches).  What bounds it now is the way from L2 to LDS: 64 KiB
 // a block, of which one is under way at a time, take 1.0 of the 1.7 us.
-template <int BM, int BN, int WM, int WN, int STAGES, bool WIDE, bool GATHER, int OUT>
-__global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) void product_tiles_kernel(ProductArgs p, uint32_t col_tiles)
+template <int BM, int BN, int WM, int WN, bool WIDE, bool GATHER, int OUT>
+__global__ __launch_bounds__(WM * WN * 64, 2) void product_tiles_kernel(ProductArgs p, uint32_t col_tiles)
 {
     constexpr int WAVES = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16, LOADS_A = BM / 8 / WAVES, LOADS_B = BN / 8 / WAVES;
     static_assert(MT % 4 == 0 && NT % 4 == 0, "a lane's exponents are whole words");
     static_assert(WAVES % 2 == 0 && LOADS_A * 8 * WAVES == BM && LOADS_B * 8 * WAVES == BN, "a wavefront loads whole groups of 8 rows, all at even or all at odd places");
-    __shared__ __attribute__((aligned(128))) uint8_t tiles[STAGES][(BM + BN) * kBlock];
+    __shared__ __attribute__((aligned(128))) uint8_t tiles[2][(BM + BN) * kBlock];
     __shared__ uint32_t exps[2][kExpBlocks][(BM + BN) / 4];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r16 = lane % 16, g = lane / 16;
 
@@ -387,26 +382,23 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
     };
     const uint32_t kb0 = (uint32_t)w.kb0, kb1 = (uint32_t)w.kb1;
     if (kb0 < kb1) {
-        constexpr int LOADS = LOADS_A + LOADS_B, AHEAD = STAGES - 1;
+        constexpr int LOADS = LOADS_A + LOADS_B;
         constexpr bool TURNS = WAVES == 8;
         const bool second = TURNS && wave >= WAVES / 2;      // the half that reads while the first multiplies
-        for (uint32_t i = 0; i < AHEAD; ++i)
-            if (kb0 + i < kb1) load(i, kb0 + i);
+        load(0, kb0);
         // Later chunks are fetched when the one before is a quarter done: its place was the one's before that, which nobody reads any more.
         const uint32_t chunk0 = kb0 / kExpBlocks;
         load_exps(chunk0);
-        if (kb0 % kExpBlocks > kExpBlocks / 4) load_exps(chunk0 + 1);
-        if (kb0 + AHEAD <= kb1) wait_for_loads<(AHEAD - 1) * LOADS>();
-        else wait_for_loads<0>();
+        if (kb0 % kExpBlocks >= kExpBlocks / 4) load_exps(chunk0 + 1);
+        wait_for_loads();
         meet();
         uint32_t stage = 0;
         if (second) {
-            if (kb0 + AHEAD < kb1) load(AHEAD, kb0 + AHEAD);
+            if (kb0 + 1 < kb1) load(1, kb0 + 1);
             meet();
         }
         for (uint32_t kb = kb0;; ++kb) {
-            const uint32_t free_stage = stage == 0 ? AHEAD : stage - 1;
-            if (!second && kb + AHEAD < kb1) load(free_stage, kb + AHEAD);
+            if (!second && kb + 1 < kb1) load(stage ^ 1, kb + 1);
             if (kb % kExpBlocks == kExpBlocks / 4 && kb != kb0 && kb / kExpBlocks * kExpBlocks + kExpBlocks < kb1) load_exps(kb / kExpBlocks + 1);
             const uint8_t *tile = tiles[stage];
             const uint32_t *from = exps[kb / kExpBlocks % 2][kb % kExpBlocks] + r16;
@@ -446,19 +438,15 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
                     for (int i = 0; i < MT; ++i) widen_fragment(a[i], ea[i / 4] >> (i % 4 * 8), wa[i]);
                 }
             }
-            // The next block has to have come when the first half reads it, which is when the second half has done so with this one.
-            auto next_has_come = [&]() INLINE_LAMBDA {
-                if (kb + AHEAD < kb1) wait_for_loads<(AHEAD - 1) * LOADS>();
-                else wait_for_loads<0>();
-            };
             if constexpr (TURNS) {
-                if (second) next_has_come();
+                // (the next block has to have come when the first half reads it, which is when the second half has done so with this one)
+                if (second) wait_for_loads();
                 else wait_for_reads();
                 meet();
                 __builtin_amdgcn_s_setprio(1);               // (the half that multiplies before the one that reads)
             }
             if constexpr (!WIDE) {
-                const uint32_t more = __builtin_amdgcn_readfirstlane(TURNS && second && kb + STAGES < kb1);
+                const uint32_t more = __builtin_amdgcn_readfirstlane(TURNS && second && kb + 2 < kb1);
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
 #pragma unroll
@@ -467,7 +455,7 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
                     // the second half's loads among its products, as each takes some time to get away
                     if constexpr (TURNS) {
 #pragma unroll
-                        for (int l = i * LOADS / MT; l < (i + 1) * LOADS / MT; ++l) load_one(l, stage, kb + STAGES, more, std::false_type{});
+                        for (int l = i * LOADS / MT; l < (i + 1) * LOADS / MT; ++l) load_one(l, stage, kb + 2, more, std::false_type{});
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
@@ -481,7 +469,7 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
                     }
                 }
             } else {
-                const uint32_t more = __builtin_amdgcn_readfirstlane(TURNS && second && kb + STAGES < kb1);
+                const uint32_t more = __builtin_amdgcn_readfirstlane(TURNS && second && kb + 2 < kb1);
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
                     if constexpr (!TURNS) widen_fragment(a[i], ea[i / 4] >> (i % 4 * 8), wa[0]);
@@ -492,16 +480,16 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
                             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][q], wa[TURNS ? i : 0][q], acc[i][j], 0, 0, 0);
                     if constexpr (TURNS) {
 #pragma unroll
-                        for (int l = i * LOADS / MT; l < (i + 1) * LOADS / MT; ++l) load_one(l, stage, kb + STAGES, more, std::false_type{});
+                        for (int l = i * LOADS / MT; l < (i + 1) * LOADS / MT; ++l) load_one(l, stage, kb + 2, more, std::false_type{});
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
             }
             if constexpr (TURNS) __builtin_amdgcn_s_setprio(0);
             if (kb + 1 >= kb1) break;
-            if (!second) next_has_come();
+            if (!second) wait_for_loads();
             meet();
-            stage = stage + 1 == STAGES ? 0 : stage + 1;
+            stage ^= 1;
         }
         if (TURNS && !second) meet();                        // (the second half is one behind)
     }
@@ -524,14 +512,14 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN == 4 && STAGES > 2 ? 1 : 2) v
     }
 }
 
-template <int BM, int BN, int WM, int WN, int STAGES, bool GATHER, int OUT>
+template <int BM, int BN, int WM, int WN, bool GATHER, int OUT>
 int launch_tiles(const ProductArgs &p, hipStream_t stream)
 {
     const int64_t col_tiles = ceil_div(p.N, (int64_t)BN), pieces = ceil_div(p.M, (int64_t)BM) + (p.by == MADDNESS_BY_ROWS ? p.groups : 0);
-    if (col_tiles * pieces >= (int64_t)1 << 31) return fail(MADDNESS_E_UNSUPPORTED, "block product: %lld x %lld results are too many", (long long)p.M, (long long)p.N);
+    if (col_tiles * pieces * WM * WN * 64 > kMostThreads) return fail(MADDNESS_E_UNSUPPORTED, "block product: %lld x %lld results are too many", (long long)p.M, (long long)p.N);
     const dim3 grid((unsigned)(col_tiles * pieces), p.by == MADDNESS_BY_DEPTH ? (unsigned)p.groups : 1u);
     note_kernel("product_tiles_kernel", __PRETTY_FUNCTION__);
-    hipLaunchKernelGGL((product_tiles_kernel<BM, BN, WM, WN, STAGES, OUT == kF32, GATHER, OUT>), grid, dim3(WM * WN * 64), 0, stream, p, (uint32_t)col_tiles);
+    hipLaunchKernelGGL((product_tiles_kernel<BM, BN, WM, WN, OUT == kF32, GATHER, OUT>), grid, dim3(WM * WN * 64), 0, stream, p, (uint32_t)col_tiles);
     return check_hip(hipGetLastError(), "launch product_tiles_kernel");
 }
 
@@ -541,7 +529,7 @@ int launch_few_as(const ProductArgs &p, hipStream_t stream)
     constexpr int WAVES = 8;
     const int64_t col_tiles = ceil_div(p.N, (int64_t)(16 * NT));
     const int64_t pieces = ceil_div(p.M, (int64_t)(16 * MT)) + (p.by == MADDNESS_BY_ROWS ? p.groups : 0);
-    if (col_tiles * pieces >= (int64_t)1 << 31) return fail(MADDNESS_E_UNSUPPORTED, "block product: %lld x %lld results are too many", (long long)p.M, (long long)p.N);
+    if (col_tiles * pieces * WAVES * 64 > kMostThreads) return fail(MADDNESS_E_UNSUPPORTED, "block product: %lld x %lld results are too many", (long long)p.M, (long long)p.N);
     const dim3 grid((unsigned)(col_tiles * pieces), p.by == MADDNESS_BY_DEPTH ? (unsigned)p.groups : 1u);
     note_kernel("product_few_kernel", __PRETTY_FUNCTION__);
     hipLaunchKernelGGL((product_few_kernel<AT, MT, NT, WAVES, DEPTH, OUT>), grid, dim3(WAVES * 64), 0, stream, p, (uint32_t)col_tiles);
@@ -570,11 +558,11 @@ int launch_shape(const ProductArgs &p, int64_t rows, int64_t groups, hipStream_t
         constexpr int64_t BN = OUT == kF32 ? 128 : 256;
         const int64_t large = ceil_div(rows, (int64_t)256) * ceil_div(p.N, BN) * groups;
         if (rows >= 1024 && large >= (OUT == kF32 ? 2 : 1) * device_info().cus) {
-            if constexpr (OUT == kF32) return launch_tiles<256, 128, 4, 2, 2, false, OUT>(p, stream);
-            else return launch_tiles<256, 256, 2, 4, 2, false, OUT>(p, stream);
+            if constexpr (OUT == kF32) return launch_tiles<256, 128, 4, 2, false, OUT>(p, stream);
+            else return launch_tiles<256, 256, 2, 4, false, OUT>(p, stream);
         }
     }
-    return launch_tiles<128, 128, 2, 2, 2, GATHER, OUT>(p, stream);
+    return launch_tiles<128, 128, 2, 2, GATHER, OUT>(p, stream);
 }
 
 template <int OUT>

@@ -15,6 +15,7 @@ using f16x2 = __attribute__((ext_vector_type(2))) _Float16;
 struct QuantiseArgs {
     const void *x;
     int64_t rows, cols, ldx, stride_x;
+    int64_t readable;          // cols, or 0 where x has no rows (and source makes rows of zeros)
     const int32_t *source;
     int64_t slots;             // source_rows * repeat
     int repeat;
@@ -32,7 +33,7 @@ __device__ __forceinline__ bool find_row(const QuantiseArgs &a, int64_t r, int64
     int s = a.source[r];
     const bool there = s >= 0 && s < a.slots;
     if (!there) s = 0;
-    if (a.factors) factor = a.factors[s];
+    if (a.factors && a.slots > 0) factor = a.factors[s];
     at = (int64_t)(s / a.repeat) * a.ldx;
     return there;
 }
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(256) void quantise_rows_kernel(QuantiseArgs a, int6
     int64_t at;
     float factor;
     const bool there = find_row(a, r, at, factor);
-    v.load(x, at, col.c, a.cols);
+    v.load(x, at, col.c, a.readable);
     v.keep(col.skip, there, factor);
     auto largest = [&](auto finite) INLINE_LAMBDA {
         uint32_t t = 0;
@@ -208,7 +209,7 @@ __global__ __launch_bounds__(kTileThreads) void quantise_tiles_kernel(QuantiseAr
     for (int p = 0; p < kRowsEach; ++p) {
         int64_t at;
         there[p] = find_row(a, min(r0 + p, a.rows - 1), at, factor[p]) && r0 + p < a.rows;
-        v[p].load(x, at, col.c, a.cols);
+        v[p].load(x, at, col.c, a.readable);
     }
 #pragma unroll
     for (int p = 0; p < kRowsEach; ++p) v[p].keep(col.skip, there[p], factor[p]);
@@ -342,8 +343,8 @@ int launch_typed(const QuantiseArgs &a, int64_t count, int tile, hipStream_t str
 {
     const int64_t blocks = ceil_div(a.cols, (int64_t)kBlock);
     if (tile == 1 && !a.qt) {
-        // as many rows as 2^30 blocks make to a launch
-        const int64_t most = std::max((int64_t)1, ((int64_t)1 << 30) / blocks);
+        // as many rows as 2^27 blocks make to a launch
+        const int64_t most = std::max((int64_t)1, ((int64_t)1 << 27) / blocks);
         for (int64_t r = 0; r < a.rows; r += most) {
             const uint32_t units = (uint32_t)(std::min(most, a.rows - r) * blocks);
             note_kernel("quantise_rows_kernel", __PRETTY_FUNCTION__);
@@ -355,6 +356,7 @@ int launch_typed(const QuantiseArgs &a, int64_t count, int tile, hipStream_t str
         return MADDNESS_OK;
     }
     const dim3 grid((unsigned)(blocks * ceil_div(a.rows, (int64_t)kBlock)), (unsigned)count);
+    if (grid.x * (int64_t)kTileThreads > kMostThreads) return fail(MADDNESS_E_UNSUPPORTED, "quantise: %lld x %lld values are too many", (long long)a.rows, (long long)a.cols);
     note_kernel("quantise_tiles_kernel", __PRETTY_FUNCTION__);
     if (tile == 1) hipLaunchKernelGGL((quantise_tiles_kernel<DT, FACTORS, 1>), grid, dim3(kTileThreads), 0, stream, a, (uint32_t)blocks);
     else hipLaunchKernelGGL((quantise_tiles_kernel<DT, FACTORS, kBlock>), grid, dim3(kTileThreads), 0, stream, a, (uint32_t)blocks);
@@ -373,7 +375,7 @@ int launch_quantise_blocks(const void *x, int dtype, int64_t count, int64_t rows
                            const int32_t *source, int64_t source_rows, int repeat, const float *factors, uint8_t *q, int64_t ldq,
                            uint8_t *scale, int64_t lds, uint8_t *qt, int64_t ldqt, uint8_t *scale_t, int64_t ldst, hipStream_t stream)
 {
-    QuantiseArgs a{x, rows, cols, ldx, stride_x, source, source_rows * repeat, repeat, factors, q, scale, qt, scale_t, ldq, lds, ldqt, ldst};
+    QuantiseArgs a{x, rows, cols, ldx, stride_x, source && source_rows == 0 ? 0 : cols, source, source_rows * repeat, repeat, factors, q, scale, qt, scale_t, ldq, lds, ldqt, ldst};
     if (dtype == MADDNESS_F32) return launch_of<kF32>(a, count, tile, stream);
     if (dtype == MADDNESS_F16) return launch_of<kF16>(a, count, tile, stream);
     return launch_of<kBF16>(a, count, tile, stream);

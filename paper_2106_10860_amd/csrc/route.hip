@@ -369,7 +369,6 @@ int launch_route_as(RouteArgs a, hipStream_t stream)
 {
     constexpr int TOKENS = 256 / LANES;
     const int64_t blocks = ceil_div(a.T, (int64_t)TOKENS), bytes = std::min(R * elem_size(DT), 16);
-    if (blocks >= (int64_t)1 << 31) return fail(MADDNESS_E_UNSUPPORTED, "route: %lld tokens are too many", (long long)a.T);
     const uintptr_t places = reinterpret_cast<uintptr_t>(a.logits) | reinterpret_cast<uintptr_t>(a.gradient) | (uintptr_t)((a.ldl | a.ldd) * elem_size(DT));
     a.pieces = a.E % R == 0 && places % bytes == 0;
     if (a.gradient) {
@@ -383,7 +382,7 @@ int launch_route_as(RouteArgs a, hipStream_t stream)
 }
 
 template <int DT>
-int launch_route_typed(const RouteArgs &a, hipStream_t stream)
+int launch_route_some(const RouteArgs &a, hipStream_t stream)
 {
     // 16 lanes to a token while a lane then has at most 16 experts, and a group its lane; but not for so few tokens that each has a SIMD to itself and
     // the shorter way of fewer experts to a lane counts
@@ -397,6 +396,29 @@ int launch_route_typed(const RouteArgs &a, hipStream_t stream)
     if (a.E <= 256) return launch_route_as<DT, 64, 4>(a, stream);
     if (a.E <= 512) return launch_route_as<DT, 64, 8>(a, stream);
     return launch_route_as<DT, 64, 16>(a, stream);
+}
+
+constexpr int64_t kMostTokens = (int64_t)1 << 25;               // of a launch, so that its threads can be counted in 32 bits
+
+template <int DT>
+int launch_route_typed(const RouteArgs &a, hipStream_t stream)
+{
+    int rc = MADDNESS_OK;
+    for (int64_t t = 0; t < a.T && rc == MADDNESS_OK; t += kMostTokens) {
+        RouteArgs part = a;
+        part.T = std::min(kMostTokens, a.T - t);
+        part.logits = static_cast<const char *>(a.logits) + t * a.ldl * elem_size(DT);
+        if (a.gradient) {
+            part.chosen += t * a.k;
+            part.dweights += t * a.k;
+            part.gradient = static_cast<char *>(a.gradient) + t * a.ldd * elem_size(DT);
+        } else {
+            part.ids += t * a.k;
+            part.weights += t * a.k;
+        }
+        rc = launch_route_some<DT>(part, stream);
+    }
+    return rc;
 }
 
 int launch_route_any(const RouteArgs &a, int dtype, hipStream_t stream)
@@ -691,11 +713,10 @@ __global__ __launch_bounds__(kWaves * 64) void combine_gradient_kernel(CombineAr
 }
 
 template <int YT, int OT>
-int launch_combine_as(const CombineArgs &a, hipStream_t stream)
+int launch_combine_some(const CombineArgs &a, hipStream_t stream)
 {
     const int64_t blocks = ceil_div(a.T, (int64_t)kWaves);
-    if (blocks >= (int64_t)1 << 31) return fail(MADDNESS_E_UNSUPPORTED, "combine: %lld tokens are too many", (long long)a.T);
-    if (a.gradient) {
+    if (a.dweights) {
         note_kernel("combine_gradient_kernel", __PRETTY_FUNCTION__);
         hipLaunchKernelGGL((combine_gradient_kernel<OT, YT>), dim3((unsigned)blocks), dim3(kWaves * 64), 0, stream, a);
         return check_hip(hipGetLastError(), "launch combine_gradient_kernel");
@@ -705,6 +726,26 @@ int launch_combine_as(const CombineArgs &a, hipStream_t stream)
     note_kernel("combine_kernel", __PRETTY_FUNCTION__);
     hipLaunchKernelGGL((combine_kernel<YT, OT>), dim3((unsigned)blocks, (unsigned)across), dim3(kWaves * 64), 0, stream, a);
     return check_hip(hipGetLastError(), "launch combine_kernel");
+}
+
+template <int YT, int OT>
+int launch_combine_as(const CombineArgs &a, hipStream_t stream)
+{
+    int rc = MADDNESS_OK;
+    for (int64_t t = 0; t < a.T && rc == MADDNESS_OK; t += kMostTokens) {
+        CombineArgs part = a;
+        part.T = std::min(kMostTokens, a.T - t);
+        part.place += t * a.k;
+        if (a.weights) part.weights += t * a.k;
+        if (a.dweights) {
+            part.gradient = static_cast<const char *>(a.gradient) + t * a.ldg * elem_size(OT);
+            part.dweights += t * a.k;
+        } else {
+            part.out = static_cast<char *>(a.out) + t * a.ldo * elem_size(OT);
+        }
+        rc = launch_combine_some<YT, OT>(part, stream);
+    }
+    return rc;
 }
 
 template <int YT>

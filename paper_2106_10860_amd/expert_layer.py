@@ -70,6 +70,8 @@ class ExpertLayer:
             raise ValueError("saved is of a forward pass without training=True")
         if tuple(grad.shape) != (saved.tokens, self.W.shape[1]):
             raise ValueError(f"grad must be [{saved.tokens}, {self.W.shape[1]}]")
+        if grad.stride(1) != 1 or grad.stride(0) < grad.shape[1]:        # (the gradient of a sum is one number in every place)
+            grad = grad.contiguous()
         dweights = m.maddness_combine_gradient(grad, saved.y, saved.place)
         dlogits = m.maddness_route_gradient(saved.logits, saved.ids, dweights, **self.choice)
         dy, dy_t = m.maddness_quantise_blocks(grad, both=True, source=saved.source, repeat=self.k, factors=saved.weights)

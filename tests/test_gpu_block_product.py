@@ -336,3 +336,115 @@ def test_other_stream_and_graph(mad):
         assert torch.equal(out, want) and torch.equal(small, want_small)
         mad.maddness_block_product(A, B)
         torch.cuda.synchronize()
+
+
+def check_some(got, A, B, label, seed=0):
+    """As check, of a few rows and columns, the first and the last ones among them."""
+    import torch
+    rng = np.random.default_rng(seed)
+    rows, cols = (torch.from_numpy(np.unique(np.concatenate([np.arange(min(n, 20)), np.arange(max(n - 20, 0), n), rng.integers(0, n, 100)]))).cuda()
+                  for n in got.shape)
+    check(got[rows][:, cols], A[rows].double().cpu().numpy(), B[cols].double().cpu().numpy(), label)
+
+
+def rough(seed, *shape):
+    """Rows of very different sizes, made on the device."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda") * torch.exp2(torch.randint(-6, 6, (*shape[:-1], 1), generator=g, device="cuda").float())
+
+
+@pytest.mark.parametrize("M,N,K", [(4100, 4100, 300), (1030, 13100, 5000), (2049, 8200, 4097), (1100, 300, 9000), (3000, 16500, 127)])
+def test_product_of_many_rows(mad, M, N, K):
+    """Enough for the large tiles; more blocks than exponents are fetched at a time."""
+    import torch
+    print("case many rows", M, N, K, flush=True)
+    A, B = mad.maddness_quantise_blocks(rough(M, M, K)), mad.maddness_quantise_blocks(rough(N, N, K), 128)
+    a, b = A.values(), B.values()
+    for dt in (torch.float32, torch.bfloat16):
+        check_some(mad.maddness_block_product(A, B, out_dtype=dt), a, b, f"{M} x {N} x {K} {dt}")
+
+
+# lengths that begin at any of the blocks whose exponents are fetched together, and are longer than what is fetched at a time
+@pytest.mark.parametrize("counts", [[1024, 4224, 5, 0, 900, 4100, 1, 128, 300, 0, 7, 4096], [1152, 6000, 896, 5000, 1, 2, 3, 4, 5, 6, 7, 8]])
+@pytest.mark.parametrize("M,N", [(1030, 1100), (700, 500)])
+def test_product_by_depth_of_many_rows(mad, counts, M, N):
+    import torch
+    print("case by depth, many rows", counts, M, N, flush=True)
+    off = offsets_of(counts, 128)
+    S = int(off[-1])
+    A, B = mad.maddness_quantise_blocks(rough(M, M, S)), mad.maddness_quantise_blocks(rough(N + S, N, S))
+    a, b = A.values(), B.values()
+    for dt in (torch.float32, torch.bfloat16):
+        got = mad.maddness_block_product(A, B, torch.from_numpy(off).cuda(), by="depth", out_dtype=dt)
+        for e in range(len(counts)):
+            if off[e + 1] > off[e]:
+                check_some(got[e], a[:, off[e]:off[e + 1]], b[:, off[e]:off[e + 1]], f"expert {e} {dt}")
+            else:
+                assert (got[e] == 0).all()
+
+
+def test_rows_of_a_matrix_without_rows_are_zeros(mad):
+    import torch
+    x, source = torch.zeros(0, 200, dtype=torch.bfloat16, device="cuda"), torch.full((140,), -1, dtype=torch.int32, device="cuda")
+    for factors in (None, torch.zeros(0, device="cuda")):
+        for got in mad.maddness_quantise_blocks(x, both=True, source=source, repeat=2, factors=factors):
+            assert (got.q.view(torch.uint8) == 0).all() and (got.scale == 127).all()
+        assert (mad.maddness_quantise_blocks(x, source=source, repeat=2, factors=factors).q.view(torch.uint8) == 0).all()
+    short = mad.maddness_quantise_blocks(torch.zeros(0, 3, device="cuda"), both=True, source=source)
+    assert all((b.q.view(torch.uint8) == 0).all() for b in short)
+
+
+def test_a_source_without_slots(mad):
+    import torch
+    none, off = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    x = torch.ones(5, 64, device="cuda")
+    B = mad.maddness_quantise_blocks(torch.ones(2, 30, 64, device="cuda"), 128)
+    assert mad.maddness_block_product(x, B, off, source=none, repeat=2).shape == (0, 30)
+    assert mad.maddness_block_product(mad.maddness_quantise_blocks(x), B, off, source=none, repeat=2).shape == (0, 30)
+    got = mad.maddness_quantise_blocks(x, both=True, source=none, repeat=2, factors=torch.ones(10, device="cuda"))
+    assert got[0].shape == (0, 64) and got[1].shape == (64, 0)
+
+
+def test_places_beyond_32_bits(mad):
+    """More than 2^31 values in each of x, its 8-bit form and the result: the last rows are those of themselves alone."""
+    import torch
+    rows, cols = (1 << 21) + 100, 1032
+    part = rough(3, 4000, cols).to(torch.bfloat16)
+    x = part[:1].expand(rows, cols).contiguous()
+    x[-4000:] = part
+    A, few = mad.maddness_quantise_blocks(x), mad.maddness_quantise_blocks(part)
+    assert torch.equal(A.q[-4000:].view(torch.uint8), few.q.view(torch.uint8)) and torch.equal(A.scale[-4000:, :9], few.scale[:, :9])
+    turned = mad.maddness_quantise_blocks(x, 128, transposed=True)
+    assert torch.equal(turned.q[:, -4000:].view(torch.uint8), mad.maddness_quantise_blocks(x[-4068:], 128, transposed=True).q[:, -4000:].view(torch.uint8))
+    del x, turned
+    B = mad.maddness_quantise_blocks(rough(4, 1040, cols), 128)
+    got = mad.maddness_block_product(A, B)
+    check_some(got[-4000:], few.values(), B.values(), "last rows")
+    source = torch.arange(rows - 4000, rows, dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 4000], dtype=torch.int32, device="cuda")
+    B3 = mad.BlockMatrix(B.q.unsqueeze(0), B.scale.unsqueeze(0), 128)
+    check_some(mad.maddness_block_product(A, B3, off, source=source), few.values(), B.values(), "gathered last rows")
+
+
+def test_a_stream_that_is_given_owns_what_the_call_makes(mad):
+    """What a call on another stream allocates does not come from the current stream's memory, which that stream may still be using."""
+    import torch
+    x, side = rough(1, 300, 512), torch.cuda.Stream()
+    B = mad.maddness_quantise_blocks(rough(2, 200, 512), 128)
+    want = mad.maddness_block_product(x, B)
+    free = torch.empty_like(want)
+    at = free.data_ptr()
+    torch.cuda.synchronize()
+    del free                                               # the current stream's, and the first that it would hand out again
+    got = mad.maddness_block_product(x, B, stream=side)
+    side.synchronize()
+    assert got.data_ptr() != at and torch.equal(got, want)
+    logits = rough(5, 60, 32)
+    ids, weights = mad.maddness_route(logits, 4, stream=side)
+    offsets, _, source, place = mad.maddness_order(ids, 32, stream=side)
+    y = mad.maddness_combine(got[:40].float(), place, weights, stream=side)
+    side.synchronize()
+    ids2, weights2 = mad.maddness_route(logits, 4)
+    assert torch.equal(ids, ids2) and torch.equal(weights, weights2)
+    assert torch.equal(y, mad.maddness_combine(got[:40].float(), mad.maddness_order(ids2, 32)[3], weights2))

@@ -277,3 +277,41 @@ def test_calls_without_the_native_marshalling_give_the_same(mad, monkeypatch):
     plain = all_calls()
     for i, (a, b) in enumerate(zip(native, plain)):
         assert a.dtype is b.dtype and torch.equal(a, b), i
+
+
+def test_sums_over_no_columns(mad):
+    import torch
+    place = torch.zeros(5, 2, dtype=torch.int32, device="cuda")
+    y, gradient = torch.zeros(7, 0, device="cuda"), torch.zeros(5, 0, device="cuda")
+    assert mad.maddness_combine(y, place).shape == (5, 0)
+    assert torch.equal(mad.maddness_combine_gradient(gradient, y, place), torch.zeros(5, 2, device="cuda"))
+
+
+def test_more_tokens_than_a_launch_takes(mad):
+    import torch
+    T = (1 << 25) + 77
+    logits = torch.randn(T, 4, dtype=torch.float16, device="cuda")
+    ids, weights = mad.maddness_route(logits, 1, "sigmoid", renormalise=False)
+    last, last_weights = mad.maddness_route(logits[-500:], 1, "sigmoid", renormalise=False)
+    assert torch.equal(ids[-500:], last) and torch.equal(weights[-500:], last_weights)
+    gradient = mad.maddness_route_gradient(logits, ids, weights, "sigmoid", renormalise=False)
+    assert torch.equal(gradient[-500:], mad.maddness_route_gradient(logits[-500:], last, last_weights, "sigmoid", renormalise=False))
+    del logits, gradient, weights
+    y = torch.randn(4, 8, device="cuda").to(torch.bfloat16)
+    out = mad.maddness_combine(y, ids)
+    assert torch.equal(out, y[ids[:, 0].long()])
+    dw = mad.maddness_combine_gradient(out, y, ids)
+    assert torch.equal(dw[-500:], mad.maddness_combine_gradient(out[-500:], y, ids[-500:]))
+
+
+def test_layer_takes_the_gradient_of_a_sum(mad):
+    """One number in every place, which the caller has as a tensor without strides."""
+    import torch
+    from paper_2106_10860_amd.expert_layer import ExpertLayer
+    g = torch.Generator(device="cuda").manual_seed(2)
+    layer = ExpertLayer.from_weights(torch.randn(4, 96, 64, generator=g, device="cuda"), 2)
+    x, logits = torch.randn(50, 64, generator=g, device="cuda"), torch.randn(50, 4, generator=g, device="cuda")
+    _, saved = layer.forward(x, logits, training=True)
+    ones = torch.ones((), device="cuda").expand(50, 96)
+    for got, want in zip(layer.backward(saved, ones), layer.backward(saved, ones.contiguous())):
+        assert torch.equal(got, want)
