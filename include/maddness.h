@@ -362,10 +362,13 @@ int maddness_quantise_blocks(const void *x, int32_t dtype, int64_t count, int64_
  *         of B.  Rows of out that no expert has are not written.
  *         MADDNESS_BY_DEPTH: out is [groups][M][ldo], the e-th from the columns offsets[e] .. offsets[e + 1] - 1 of A and of B
  *         (0 where there are none); both have tile 1.  For whole blocks, the offsets are multiples of 128.
- * offsets NULL, or [groups + 1] on the device, not decreasing.  One outside the matrix is cut back to it, and for
+ *         MADDNESS_BY_CHOICE: out has `slots` rows, and row r is that of A's row r / repeat with the source[r]-th of `groups`
+ *         matrices of B, zeros where that is outside [0, groups).  For few rows, which need no order: slots up to
+ *         MADDNESS_MAX_CHOSEN, A with at least slots / repeat rows.  The results are those of MADDNESS_BY_ROWS.
+ * offsets NULL, or [groups + 1] on the device (MADDNESS_BY_ROWS and _BY_DEPTH), not decreasing.  One outside the matrix is cut back to it, and for
  *         MADDNESS_BY_DEPTH one that is no multiple of 128 is rounded down to one, so a wrong array gives wrong sums
  *         but no bad access.
- * source  NULL, or [slots] on the device (MADDNESS_BY_ROWS only): out has `slots` rows, and row r is that of A's row
+ * source  NULL, or [slots] on the device (with MADDNESS_BY_CHOICE as above; otherwise MADDNESS_BY_ROWS only): out has `slots` rows, and row r is that of A's row
  *         source[r] / repeat; rows whose source is outside [0, A's rows times repeat) are not written.
  * A       MADDNESS_E4M3, or F32 / F16 / BF16 (not for MADDNESS_BY_DEPTH): then its rows are rounded as
  *         maddness_quantise_blocks does with tile 1; data aligned to its element, scale ignored.
@@ -373,7 +376,8 @@ int maddness_quantise_blocks(const void *x, int32_t dtype, int64_t count, int64_
  *         that is 0); contents undefined afterwards.
  * M = 0 and N = 0 are valid; K = 0 gives zeros.  M, N, K < 2^31.
  */
-typedef enum { MADDNESS_DENSE = 0, MADDNESS_BY_ROWS = 1, MADDNESS_BY_DEPTH = 2 } maddness_product_groups;
+#define MADDNESS_MAX_CHOSEN 512
+typedef enum { MADDNESS_DENSE = 0, MADDNESS_BY_ROWS = 1, MADDNESS_BY_DEPTH = 2, MADDNESS_BY_CHOICE = 4 } maddness_product_groups;
 
 size_t maddness_block_product_workspace(int64_t a_rows, int64_t K, int32_t by, int32_t a_dtype);
 int maddness_block_product(const maddness_block_matrix *A, const maddness_block_matrix *B, int32_t by, int32_t groups,
@@ -429,7 +433,7 @@ int maddness_order(const int32_t *ids, int64_t slots, int32_t E, int32_t align, 
 
 /*
  * out[t] = sum_j weights[t][j] y[place[t][j]], j = 0 .. k - 1 in this order, in fp32 and rounded once to out_dtype; a place outside
- * [0, rows) adds nothing.  y [rows][ldy] of y_dtype, place [T][k], weights [T][k] fp32 or NULL (1), out [T][ldo]; F32, F16 or BF16.
+ * [0, rows) adds nothing.  y [rows][ldy] of y_dtype, place [T][k] or NULL (t k + j, rows >= T k), weights [T][k] fp32 or NULL (1), out [T][ldo]; F32, F16 or BF16.
  * maddness_combine_gradient: weights_gradient[t][j] = sum_n gradient[t][n] y[place[t][j]][n], 0 without a place.  (The
  * gradient of y is the gradient's rows times the weights: source and factors of maddness_quantise_blocks.)
  */

@@ -536,6 +536,7 @@ def maddness_last_kernel() -> str:
 # The exact product at 8 bits and layers of experts (the calls' own module, their names here).
 from .blocks import (  # noqa: E402
     BLOCK,
+    MAX_CHOSEN,
     BlockMatrix,
     maddness_block_product,
     maddness_combine,

@@ -19,7 +19,9 @@ import paper_2106_10860_amd as _m
 
 BLOCK = 128
 MADDNESS_E4M3 = 16
-MADDNESS_DENSE, MADDNESS_BY_ROWS, MADDNESS_BY_DEPTH = 0, 1, 2
+MADDNESS_DENSE, MADDNESS_BY_ROWS, MADDNESS_BY_DEPTH, MADDNESS_BY_CHOICE = 0, 1, 2, 4
+MAX_CHOSEN = 512
+_BY = {"rows": MADDNESS_BY_ROWS, "depth": MADDNESS_BY_DEPTH, "choice": MADDNESS_BY_CHOICE}
 _SCORES = {"softmax": 0, "sigmoid": 1}
 _INT_MAX = 2 ** 31 - 1
 
@@ -201,15 +203,24 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", so
     columns offsets[e] .. offsets[e + 1] - 1 of A [M, K] and B [N, K] (multiples of 128).
 
     With ``source`` (int32 [slots], by="rows") out is [slots, N] and its row r that of A's row source[r] // repeat; rows whose source is
-    negative are left as they are."""
+    negative are left as they are.
+
+    by="choice" takes the experts' ids themselves as ``source`` (int32 [slots] or [M, k], slots up to 512) in place of an order: out is
+    [slots, N] and its row r that of A's row r // repeat (k of a source [M, k]) with B[source[r]], zeros for an id of no expert."""
     if not isinstance(B, BlockMatrix):
         raise TypeError("B must be a BlockMatrix")
-    if by != "rows" and by != "depth":
-        raise ValueError(f"by must be 'rows' or 'depth', is {by!r}")
+    how = _BY.get(by)
+    if how is None:
+        raise ValueError(f"by must be 'rows', 'depth' or 'choice', is {by!r}")
+    if how == MADDNESS_BY_CHOICE:
+        if source is None or offsets is not None:
+            raise ValueError("by='choice' goes with source, and without offsets")
+        if source.dim() == 2:
+            repeat, source = max(source.shape[1], 1), source.view(-1)
     if stream is not None:
         with _on(stream):
             return maddness_block_product(A, B, offsets, by, source, repeat, out_dtype, out, workspace)
-    r = _m._native.block_product(isinstance(A, BlockMatrix), A, B, offsets, by == "depth", source, repeat, out_dtype, out, workspace)
+    r = _m._native.block_product(isinstance(A, BlockMatrix), A, B, offsets, how, source, repeat, out_dtype, out, workspace)
     if r is not NotImplemented:
         return _m._done(r)
     torch = _m._torch or _m._torch_module()
@@ -223,21 +234,25 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", so
         a, device = _m._BlockMatrix(A.data_ptr(), a_dtype, 1, M, K, lda, 0, None, 0, 0), A.device
     N, a_rows, source_p = B.shape[-2], M, None
     if source is not None:
-        if offsets is None or by != "rows" or source.dim() != 1 or repeat < 1:
-            raise ValueError("source must be 1-D, with offsets, by='rows' and repeat >= 1")
+        if how != MADDNESS_BY_CHOICE and (offsets is None or how != MADDNESS_BY_ROWS) or source.dim() != 1 or repeat < 1:
+            raise ValueError("source must be 1-D, with offsets, by='rows' and repeat >= 1, or with by='choice'")
         _fits(repeat=repeat)
         M = source.shape[0]
-        source_p = _flat(source, torch.int32, (M,), "source") if M else offsets.data_ptr()      # (an empty one may have no address, and is not read)
-    if offsets is None:
+        source_p = _flat(source, torch.int32, (M,), "source") if M or offsets is None else offsets.data_ptr()      # (an empty one may have no address, and is not read)
+    if how == MADDNESS_BY_CHOICE:
+        if len(B.shape) != 3:
+            raise ValueError(f"B must be [experts, N, K], has shape {B.shape}")
+        groups, offsets_p, lead = B.shape[0], None, ()
+    elif offsets is None:
         how, groups, offsets_p, lead = MADDNESS_DENSE, 1, None, ()
         if len(B.shape) != 2:
-            raise ValueError("B of several experts needs offsets")
+            raise ValueError("B of several experts needs offsets, or by='choice'")
     else:
         groups = offsets.shape[0] - 1 if offsets.dim() == 1 else -1
         if groups < 1:
             raise ValueError("offsets must be 1-D with one entry more than there are experts")
         offsets_p = _flat(offsets, torch.int32, (groups + 1,), "offsets")
-        how, lead = (MADDNESS_BY_ROWS, ()) if by == "rows" else (MADDNESS_BY_DEPTH, (groups,))
+        lead = () if by == "rows" else (groups,)
         if by == "rows" and (len(B.shape) != 3 or B.shape[0] != groups):
             raise ValueError(f"B must be [experts, N, K] with {groups} experts, has shape {B.shape}")
         if by == "depth" and len(B.shape) != 2:
@@ -337,8 +352,9 @@ def maddness_order(ids, experts: int, align: int = 1, stream=None):
     return offsets, counts, source, place
 
 
-def maddness_combine(y, place, weights=None, out_dtype=None, out=None, stream=None):
-    """out[t] = sum over j of weights[t, j] * y[place[t, j]]; a negative place adds nothing, weights None are 1."""
+def maddness_combine(y, place=None, weights=None, out_dtype=None, out=None, stream=None):
+    """out[t] = sum over j of weights[t, j] * y[place[t, j]]; a negative place adds nothing, weights None are 1.  place None, with weights
+    [T, k]: y[t * k + j]."""
     if stream is not None:
         with _on(stream):
             return maddness_combine(y, place, weights, out_dtype, out)
@@ -348,9 +364,10 @@ def maddness_combine(y, place, weights=None, out_dtype=None, out=None, stream=No
     torch = _m._torch or _m._torch_module()
     code = _code(y, "y")
     rows, N, ldy = _m._rows(y, "y")
-    if place.dim() != 2:
-        raise ValueError("place must be [T, k]")
-    T, k = place.shape
+    slots = weights if place is None else place
+    if slots is None or slots.dim() != 2:
+        raise ValueError("place must be [T, k], or None and weights [T, k]")
+    T, k = slots.shape
     if out is None:
         out = torch.empty((T, N), dtype=out_dtype or y.dtype, device=y.device)
     elif tuple(out.shape) != (T, N) or (out_dtype is not None and out.dtype is not out_dtype):

@@ -122,25 +122,33 @@ int maddness_block_product(const maddness_block_matrix *A, const maddness_block_
                            size_t workspace_bytes, void *stream)
 {
     begin_call();
-    if (by < MADDNESS_DENSE || by > MADDNESS_BY_DEPTH) return fail(MADDNESS_E_INVAL, "by = %d is not a maddness_product_groups", by);
+    if (by != MADDNESS_DENSE && by != MADDNESS_BY_ROWS && by != MADDNESS_BY_DEPTH && by != MADDNESS_BY_CHOICE) return fail(MADDNESS_E_INVAL, "by = %d is not a maddness_product_groups", by);
     int rc;
     if ((rc = check_matrix(A, by != MADDNESS_BY_DEPTH, "A")) != MADDNESS_OK || (rc = check_matrix(B, false, "B")) != MADDNESS_OK) return rc;
     if (A->cols != B->cols) return fail(MADDNESS_E_INVAL, "A has %lld columns and B %lld", (long long)A->cols, (long long)B->cols);
     if (!floating(out_dtype)) return fail(MADDNESS_E_INVAL, "out: dtype = %d is not F32, F16 or BF16", out_dtype);
-    if (source) {
+    if (by == MADDNESS_BY_CHOICE) {
+        if ((rc = check_size(slots, "slots")) != MADDNESS_OK) return rc;
+        if (slots > MADDNESS_MAX_CHOSEN) return fail(MADDNESS_E_UNSUPPORTED, "slots = %lld, supported are up to %d", (long long)slots, MADDNESS_MAX_CHOSEN);
+        if (repeat < 1) return fail(MADDNESS_E_INVAL, "repeat = %d, must be >= 1", repeat);
+        if (A->rows < ceil_div(slots, (int64_t)repeat))
+            return fail(MADDNESS_E_INVAL, "A has %lld rows, %lld slots of %d to a row go with more", (long long)A->rows, (long long)slots, repeat);
+        if (slots > 0 && !source) return fail(MADDNESS_E_INVAL, "source is NULL");
+        if (!aligned(source, 4)) return fail(MADDNESS_E_ALIGN, "source not 4-byte aligned");
+    } else if (source) {
         if (by != MADDNESS_BY_ROWS) return fail(MADDNESS_E_INVAL, "source goes with MADDNESS_BY_ROWS");
         if (repeat < 1) return fail(MADDNESS_E_INVAL, "repeat = %d, must be >= 1", repeat);
         if ((rc = check_size(slots, "slots")) != MADDNESS_OK) return rc;
         if (A->rows * repeat > kMostRows) return fail(MADDNESS_E_UNSUPPORTED, "A's rows times repeat = %lld, supported are up to 2^31 - 1", (long long)(A->rows * repeat));
         if (!aligned(source, 4)) return fail(MADDNESS_E_ALIGN, "source not 4-byte aligned");
     }
-    const int64_t M = source ? slots : A->rows, N = B->rows, K = A->cols;
+    const int64_t M = source || by == MADDNESS_BY_CHOICE ? slots : A->rows, N = B->rows, K = A->cols;
     if (by == MADDNESS_DENSE) {
         groups = 1;
     } else {
         if (groups < 1) return fail(MADDNESS_E_INVAL, "groups = %d, must be >= 1", groups);
         if (groups > 65535) return fail(MADDNESS_E_UNSUPPORTED, "groups = %d, supported are up to 65535", groups);
-        if (!offsets) return fail(MADDNESS_E_INVAL, "offsets is NULL");
+        if (!offsets && by != MADDNESS_BY_CHOICE) return fail(MADDNESS_E_INVAL, "offsets is NULL");
         if (!aligned(offsets, 4)) return fail(MADDNESS_E_ALIGN, "offsets not 4-byte aligned");
         if (by == MADDNESS_BY_DEPTH && K > 0 && (A->tile != 1 || B->tile != 1)) return fail(MADDNESS_E_INVAL, "A and B must have tile 1 to be cut by depth");
     }
@@ -251,7 +259,7 @@ static int check_combine(const void *y, int32_t y_dtype, int64_t rows, int64_t N
     if ((rc = check_size(rows, "rows")) != MADDNESS_OK || (rc = check_size(N, "N")) != MADDNESS_OK || (rc = check_size(T, "T")) != MADDNESS_OK) return rc;
     if (k < 1) return fail(MADDNESS_E_INVAL, "k = %d, must be >= 1", k);
     if ((rc = check_floats(y, y_dtype, rows, N, ldy, "y")) != MADDNESS_OK) return rc;
-    if (T > 0 && !place) return fail(MADDNESS_E_INVAL, "place is NULL");
+    if (!place && T * k > rows) return fail(MADDNESS_E_INVAL, "place is NULL and y has %lld rows, fewer than T k = %lld", (long long)rows, (long long)(T * k));
     if (!aligned(place, 4)) return fail(MADDNESS_E_ALIGN, "place not 4-byte aligned");
     return MADDNESS_OK;
 }

@@ -462,7 +462,7 @@ PyObject *quantise_blocks(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// (a_is_blocks, A, B, offsets, by_depth, source, repeat, out_dtype, out, workspace) -> out
+// (a_is_blocks, A, B, offsets, by, source, repeat, out_dtype, out, workspace) -> out
 PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
@@ -486,23 +486,26 @@ PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
         }
         B = block_matrix(a[2], &device, &experts);
         if (A.cols != B.cols) throw NotUsual();
-        int32_t by = MADDNESS_DENSE, groups = 1;
+        int32_t by = narrow(whole(a[4])), groups = 1;
         const int32_t *offsets = nullptr;
-        if (a[3] != Py_None) {
+        if (by == MADDNESS_BY_CHOICE) {
+            if (experts < 1) throw NotUsual();
+            groups = narrow(experts);
+        } else if (a[3] != Py_None) {
             const at::Tensor &o = tensor(a[3]);
             if (o.dim() != 1 || o.scalar_type() != at::kInt || !o.is_contiguous() || o.device() != device || o.size(0) < 2) throw NotUsual();
             groups = narrow(o.size(0) - 1);
             offsets = static_cast<const int32_t *>(o.data_ptr());
-            by = truth(a[4]) ? MADDNESS_BY_DEPTH : MADDNESS_BY_ROWS;
             if (by == MADDNESS_BY_ROWS ? experts != groups : experts != -1) throw NotUsual();
-        } else if (experts != -1) {
-            throw NotUsual();
+        } else {
+            if (experts != -1) throw NotUsual();
+            by = MADDNESS_DENSE;
         }
         int64_t rows = A.rows;
         const int32_t repeat = narrow(whole(a[6])), *source = nullptr;
         if (a[5] != Py_None) {
             const at::Tensor &s = tensor(a[5]);
-            if (by != MADDNESS_BY_ROWS || s.dim() != 1 || s.scalar_type() != at::kInt || !s.is_contiguous() || s.device() != device || repeat < 1)
+            if ((by != MADDNESS_BY_ROWS && by != MADDNESS_BY_CHOICE) || s.dim() != 1 || s.scalar_type() != at::kInt || !s.is_contiguous() || s.device() != device || repeat < 1)
                 throw NotUsual();
             rows = s.size(0);
             source = rows ? static_cast<const int32_t *>(s.data_ptr()) : offsets;      // (an empty one may have no address, and is not read)
@@ -647,12 +650,12 @@ PyObject *combine(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
         if (n != 5) throw NotUsual();
-        const at::Tensor &y = tensor(a[0]), &place = tensor(a[1]);
+        const at::Tensor &y = tensor(a[0]), &slots = tensor(a[a[1] == Py_None ? 2 : 1]);
         const int code = float_code(y.scalar_type());
         const Rows r = rows_of(y);
-        if (place.dim() != 2 || a[4] != Py_None) throw NotUsual();
-        const int64_t T = place.size(0);
-        const int32_t k = narrow(place.size(1));
+        if (slots.dim() != 2 || a[4] != Py_None) throw NotUsual();
+        const int64_t T = slots.size(0);
+        const int32_t k = narrow(slots.size(1));
         const int32_t *place_p = flat_or_null<const int32_t>(a[1], at::kInt, {T, k}, y.device());
         const float *weights = flat_or_null<const float>(a[2], at::kFloat, {T, k}, y.device());
         const at::ScalarType type = dtype_or(a[3], y.scalar_type());

@@ -66,6 +66,7 @@ __device__ __forceinline__ void cut(Piece &p, int64_t kb, int group, int64_t K)
 // Whether A's rows are rounded within the few-rows kernel, by every workgroup for itself: while they fill 32 KiB of LDS at most, which costs a
 // workgroup up to 64 values a thread (1.5 us), a launch of their own costs 5 us.
 constexpr int64_t kInside = 32768, kInsideRows = 64;
+constexpr int kMostChosen = MADDNESS_MAX_CHOSEN;
 
 // What a workgroup computes: rows first .. last - 1 of A, with one expert's matrix, over the blocks kb0 .. kb1 - 1.
 struct Part {
@@ -111,118 +112,149 @@ __device__ __forceinline__ int64_t row_of_a(const ProductArgs &p, int64_t m)
 // Few rows: 16 MT rows by 16 NT columns to a workgroup; its wavefronts take every WAVES-th block of the sum, DEPTH of them asked for
 // at once, and add up in LDS, in their order.  B comes straight from memory, in pieces of 32 bytes to a lane, and so does an 8-bit A; a floating
 // A is rounded into LDS while the first of B is on its way.
-template <int AT, int MT, int NT, int WAVES, int DEPTH, int OUT>
+//
+// CHOICE: of the slots, those whose id is the workgroup's expert, found by going through all ids, 16 MT at a time; no order of them is needed.  The rows of
+// results are the slots themselves.
+template <int AT, int MT, int NT, int WAVES, int DEPTH, int OUT, bool CHOICE>
 __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, uint32_t col_tiles)
 {
     constexpr bool ROUND = AT != kE4M3;
+    __shared__ int32_t slots[CHOICE ? kMostChosen : 1];
     __shared__ f32x4 sums[WAVES][MT * NT][64];
     __shared__ __attribute__((aligned(16))) uint8_t rounded[ROUND ? kInside + kInsideRows * 16 : 16], bytes[ROUND ? kInside / kBlock + kInsideRows : 16];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r16 = lane % 16, g = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int64_t n0 = (int64_t)(blockIdx.x % col_tiles) * (16 * NT);
     Part w;
     PieceSearch search;
-    if (!find_part(p, search, 16 * MT, blockIdx.x / col_tiles, blockIdx.y, w)) return;
-    const uint8_t *row_b[NT], *row_a[MT], *scale_a[MT], *scale_b[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int64_t n = min(n0 + t * 16 + r16, p.N - 1);
-        row_b[t] = w.b + n * p.ldb;
-        scale_b[t] = w.scale_b + (n >> p.shift_b) * p.lds_b;
-    }
-    Piece b[DEPTH][NT], a[DEPTH][MT];
-    auto load = [&](int64_t kb0) INLINE_LAMBDA {
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) b[d][t] = load_piece(row_b[t], scale_b[t], min(kb0 + d * WAVES, w.kb1 - 1), g, w.K);
-    };
-    const int64_t kb_first = w.kb0 + wave;
-    if (kb_first < w.kb1) load(kb_first);
-
-    const int blocks = ROUND ? (int)w.kb1 : 0, stride = blocks * kBlock + 16;
-    if constexpr (ROUND) {
-        for (int unit = threadIdx.x / 16; unit < (int)p.a_rows * blocks; unit += WAVES * 4) {
-            const int row = unit / blocks, kb = unit % blocks;
-            const int64_t k = (int64_t)kb * kBlock + r16 * 8;
-            float v[8];
-            const int skip = before_column(k, p.K);
-            widen<AT>(load_raw<AT>(p.a, row * p.lda, k, p.K), v);
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = i < skip ? top : max(top, finite_magnitude(v[i]));
-            const uint32_t byte = exponent_byte(row16_max(top));
-            *reinterpret_cast<uint2 *>(rounded + row * stride + kb * kBlock + r16 * 8) =
-                in_place(make_uint2(pack4(v[0], v[1], v[2], v[3], byte), pack4(v[4], v[5], v[6], v[7], byte)), skip);
-            if (r16 == 0) bytes[unit] = (uint8_t)byte;
+    int count = 0;
+    if constexpr (CHOICE) {
+        const int lane = threadIdx.x % 64;
+        const int e = blockIdx.x / col_tiles;
+        for (int base = 0; base < (int)p.M; base += 64) {
+            const int slot = base + lane, id = slot < (int)p.M ? p.source[slot] : e + 1;
+            const uint64_t here = __ballot(id == e);
+            if (wave == 0 && id == e) slots[count + __popcll(here & (((uint64_t)1 << lane) - 1))] = slot;
+            count += __popcll(here);
+            if (e == 0 && wave == 0 && slot < (int)p.M && (id < 0 || id >= p.groups))
+                for (int64_t n = n0; n < min(n0 + 16 * NT, p.N); ++n) store_as<OUT>(p.out, slot * p.ldo + n, 0.0f);
         }
+        if (count == 0) return;
+        w = Part{0, min(count, 16 * MT), 0, ceil_div(p.K, (int64_t)kBlock), p.K, p.b + e * p.stride_b, p.scale_b + e * p.scale_stride_b, 0};
         __syncthreads();
+    } else {
+        if (!find_part(p, search, 16 * MT, blockIdx.x / col_tiles, blockIdx.y, w)) return;
     }
+    for (bool again = false;; again = true) {
+        int lane = threadIdx.x % 64;
+        if constexpr (CHOICE) asm volatile("" : "+v"(lane));  // (or all addresses that stay the same would be kept in registers, which then do for half the workgroups)
+        const int r16 = lane % 16, g = lane / 16;
+        const uint8_t *row_b[NT], *row_a[MT], *scale_a[MT], *scale_b[NT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int64_t m = max(row_of_a(p, min(w.first + t * 16 + r16, w.last - 1)), (int64_t)0);
-        row_a[t] = ROUND ? rounded + m * stride : p.a + m * p.lda;
-        scale_a[t] = ROUND ? bytes + m * blocks : p.scale_a + (m >> p.shift_a) * p.lds_a;
-    }
-    f32x4 acc[MT][NT] = {};
-    for (int64_t kb0 = kb_first; kb0 < w.kb1; kb0 += DEPTH * WAVES) {
-        if (kb0 != kb_first) load(kb0);
+        for (int t = 0; t < NT; ++t) {
+            const int64_t n = min(n0 + t * 16 + r16, p.N - 1);
+            row_b[t] = w.b + n * p.ldb;
+            scale_b[t] = w.scale_b + (n >> p.shift_b) * p.lds_b;
+        }
+        Piece b[DEPTH][NT], a[DEPTH][MT];
+        auto load = [&](int64_t kb0) INLINE_LAMBDA {
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            const int64_t kb = min(kb0 + d * WAVES, w.kb1 - 1);
+            for (int d = 0; d < DEPTH; ++d)
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                if constexpr (ROUND) {
-                    a[d][t].lo = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32);
-                    a[d][t].hi = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32 + 16);
-                    a[d][t].byte = scale_a[t][kb];
-                } else {
-                    a[d][t] = load_piece(row_a[t], scale_a[t], kb, g, w.K);
-                }
+                for (int t = 0; t < NT; ++t) b[d][t] = load_piece(row_b[t], scale_b[t], min(kb0 + d * WAVES, w.kb1 - 1), g, w.K);
+        };
+        const int64_t kb_first = w.kb0 + wave;
+        if (kb_first < w.kb1) load(kb_first);
+
+        const int blocks = ROUND ? (int)w.kb1 : 0, stride = blocks * kBlock + 16;
+        if constexpr (ROUND) {
+            const int units = again ? 0 : (int)p.a_rows * blocks;
+            for (int unit = threadIdx.x / 16; unit < units; unit += WAVES * 4) {
+                const int row = unit / blocks, kb = unit % blocks;
+                const int64_t k = (int64_t)kb * kBlock + r16 * 8;
+                float v[8];
+                const int skip = before_column(k, p.K);
+                widen<AT>(load_raw<AT>(p.a, row * p.lda, k, p.K), v);
+                uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = i < skip ? top : max(top, finite_magnitude(v[i]));
+                const uint32_t byte = exponent_byte(row16_max(top));
+                *reinterpret_cast<uint2 *>(rounded + row * stride + kb * kBlock + r16 * 8) =
+                    in_place(make_uint2(pack4(v[0], v[1], v[2], v[3], byte), pack4(v[4], v[5], v[6], v[7], byte)), skip);
+                if (r16 == 0) bytes[unit] = (uint8_t)byte;
             }
+            __syncthreads();
         }
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            const int64_t kb = kb0 + d * WAVES;
-            if (kb >= w.kb1) break;
-            if ((kb + 1) * kBlock > w.K) {
+        for (int t = 0; t < MT; ++t) {
+            const int64_t at = min(w.first + t * 16 + r16, w.last - 1), m = CHOICE ? slots[at] / p.repeat : max(row_of_a(p, at), (int64_t)0);
+            row_a[t] = ROUND ? rounded + m * stride : p.a + m * p.lda;
+            scale_a[t] = ROUND ? bytes + m * blocks : p.scale_a + (m >> p.shift_a) * p.lds_a;
+        }
+        f32x4 acc[MT][NT] = {};
+        for (int64_t kb0 = kb_first; kb0 < w.kb1; kb0 += DEPTH * WAVES) {
+            if (kb0 != kb_first) load(kb0);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) cut(b[d][t], kb, g, w.K);
-#pragma unroll
-                for (int t = 0; t < MT; ++t) cut(a[d][t], kb, g, w.K);
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                bf16x8 wb[NT], wa[MT];
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const i32x4 v = q < 2 ? b[d][t].lo : b[d][t].hi;
-                    wb[t] = widen8(v[q % 2 * 2], v[q % 2 * 2 + 1], as_scale(b[d][t].byte));
-                }
+            for (int d = 0; d < DEPTH; ++d) {
+                const int64_t kb = min(kb0 + d * WAVES, w.kb1 - 1);
 #pragma unroll
                 for (int t = 0; t < MT; ++t) {
-                    const i32x4 v = q < 2 ? a[d][t].lo : a[d][t].hi;
-                    wa[t] = widen8(v[q % 2 * 2], v[q % 2 * 2 + 1], as_scale(a[d][t].byte));
+                    if constexpr (ROUND) {
+                        a[d][t].lo = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32);
+                        a[d][t].hi = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32 + 16);
+                        a[d][t].byte = scale_a[t][kb];
+                    } else {
+                        a[d][t] = load_piece(row_a[t], scale_a[t], kb, g, w.K);
+                    }
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) {
+                const int64_t kb = kb0 + d * WAVES;
+                if (kb >= w.kb1) break;
+                if ((kb + 1) * kBlock > w.K) {
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) cut(b[d][t], kb, g, w.K);
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) cut(a[d][t], kb, g, w.K);
                 }
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                for (int q = 0; q < 4; ++q) {
+                    bf16x8 wb[NT], wa[MT];
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j], wa[i], acc[i][j], 0, 0, 0);
+                    for (int t = 0; t < NT; ++t) {
+                        const i32x4 v = q < 2 ? b[d][t].lo : b[d][t].hi;
+                        wb[t] = widen8(v[q % 2 * 2], v[q % 2 * 2 + 1], as_scale(b[d][t].byte));
+                    }
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) {
+                        const i32x4 v = q < 2 ? a[d][t].lo : a[d][t].hi;
+                        wa[t] = widen8(v[q % 2 * 2], v[q % 2 * 2 + 1], as_scale(a[d][t].byte));
+                    }
+#pragma unroll
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j], wa[i], acc[i][j], 0, 0, 0);
+                }
             }
         }
-    }
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
-    __syncthreads();
-    for (int o = threadIdx.x; o < MT * NT * 256; o += WAVES * 64) {
-        const int m = o / (16 * NT), n = o % (16 * NT);
-        if (w.first + m >= w.last || n0 + n >= p.N || (p.source && row_of_a(p, w.first + m) < 0)) continue;
-        const int tile = m / 16 * NT + n / 16, at = m % 16 + n % 16 / 4 * 16;
-        float s = 0.0f;
+            for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
+        __syncthreads();
+        for (int o = threadIdx.x; o < MT * NT * 256; o += WAVES * 64) {
+            const int m = o / (16 * NT), n = o % (16 * NT);
+            if (w.first + m >= w.last || n0 + n >= p.N || (!CHOICE && p.source && row_of_a(p, w.first + m) < 0)) continue;
+            const int tile = m / 16 * NT + n / 16, at = m % 16 + n % 16 / 4 * 16;
+            float s = 0.0f;
 #pragma unroll
-        for (int k = 0; k < WAVES; ++k) s += sums[k][tile][at][n % 4];
-        store_as<OUT>(p.out, w.out_at + (w.first + m) * p.ldo + n0 + n, s);
+            for (int k = 0; k < WAVES; ++k) s += sums[k][tile][at][n % 4];
+            store_as<OUT>(p.out, w.out_at + (CHOICE ? slots[w.first + m] : w.first + m) * p.ldo + n0 + n, s);
+        }
+        w.first += 16 * MT;
+        if (!CHOICE || w.first >= count) break;
+        w.last = min(w.first + 16 * MT, (int64_t)count);
+        __syncthreads();
     }
 }
 
@@ -523,16 +555,16 @@ int launch_tiles(const ProductArgs &p, hipStream_t stream)
     return check_hip(hipGetLastError(), "launch product_tiles_kernel");
 }
 
-template <int AT, int OUT, int MT, int NT, int DEPTH>
+template <int AT, int OUT, int MT, int NT, int DEPTH, bool CHOICE>
 int launch_few_as(const ProductArgs &p, hipStream_t stream)
 {
     constexpr int WAVES = 8;
     const int64_t col_tiles = ceil_div(p.N, (int64_t)(16 * NT));
-    const int64_t pieces = ceil_div(p.M, (int64_t)(16 * MT)) + (p.by == MADDNESS_BY_ROWS ? p.groups : 0);
+    const int64_t pieces = CHOICE ? p.groups : ceil_div(p.M, (int64_t)(16 * MT)) + (p.by == MADDNESS_BY_ROWS ? p.groups : 0);
     if (col_tiles * pieces * WAVES * 64 > kMostThreads) return fail(MADDNESS_E_UNSUPPORTED, "block product: %lld x %lld results are too many", (long long)p.M, (long long)p.N);
     const dim3 grid((unsigned)(col_tiles * pieces), p.by == MADDNESS_BY_DEPTH ? (unsigned)p.groups : 1u);
     note_kernel("product_few_kernel", __PRETTY_FUNCTION__);
-    hipLaunchKernelGGL((product_few_kernel<AT, MT, NT, WAVES, DEPTH, OUT>), grid, dim3(WAVES * 64), 0, stream, p, (uint32_t)col_tiles);
+    hipLaunchKernelGGL((product_few_kernel<AT, MT, NT, WAVES, DEPTH, OUT, CHOICE>), grid, dim3(WAVES * 64), 0, stream, p, (uint32_t)col_tiles);
     return check_hip(hipGetLastError(), "launch product_few_kernel");
 }
 
@@ -542,10 +574,11 @@ int64_t rows_each(const ProductArgs &p) { return p.by == MADDNESS_BY_ROWS ? ceil
 template <int AT, int OUT>
 int launch_few(const ProductArgs &p, hipStream_t stream)
 {
-    if (rows_each(p) > 16) return launch_few_as<AT, OUT, 4, 2, 2>(p, stream);
     // a wavefront's share of the sum is one block: more columns to a workgroup instead
-    if (p.K <= 8 * kBlock) return launch_few_as<AT, OUT, 1, 4, 1>(p, stream);
-    return launch_few_as<AT, OUT, 1, 1, 4>(p, stream);
+    const bool shallow = p.K <= 8 * kBlock;
+    if (p.by == MADDNESS_BY_CHOICE) return shallow ? launch_few_as<AT, OUT, 1, 4, 1, true>(p, stream) : launch_few_as<AT, OUT, 1, 1, 4, true>(p, stream);
+    if (rows_each(p) > 16) return launch_few_as<AT, OUT, 4, 2, 2, false>(p, stream);
+    return shallow ? launch_few_as<AT, OUT, 1, 4, 1, false>(p, stream) : launch_few_as<AT, OUT, 1, 1, 4, false>(p, stream);
 }
 
 template <bool GATHER, int OUT>
@@ -571,6 +604,7 @@ int launch_to(const ProductArgs &p, int a_dtype, hipStream_t stream)
     if (a_dtype == MADDNESS_F32) return launch_few<kF32, OUT>(p, stream);
     if (a_dtype == MADDNESS_F16) return launch_few<kF16, OUT>(p, stream);
     if (a_dtype == MADDNESS_BF16) return launch_few<kBF16, OUT>(p, stream);
+    if (p.by == MADDNESS_BY_CHOICE) return launch_few<kE4M3, OUT>(p, stream);
     const int64_t rows = rows_each(p), groups = p.by == MADDNESS_DENSE ? 1 : p.groups;
     const bool far = std::max(p.lda, p.ldb) > kMostStride || (p.source && p.a_rows * p.lda >= (int64_t)1 << 32);
     // Between the two by what they take, in microseconds, fitted to sizes from 300 x 300 x 300 to 1024 x 4096 x 4096: the few-rows kernel makes more workgroups of

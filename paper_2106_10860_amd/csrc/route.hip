@@ -651,7 +651,7 @@ __global__ __launch_bounds__(kWaves * 64) void combine_kernel(CombineArgs a)
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
             const int64_t at = t * a.k + min(j0 + j, a.k - 1);
-            p[j] = a.place[at];
+            p[j] = a.place ? a.place[at] : (int)at;
             w[j] = a.weights ? a.weights[at] : 1.0f;
             if (j0 + j >= a.k || p[j] >= a.rows) p[j] = -1;
         }
@@ -685,7 +685,7 @@ __global__ __launch_bounds__(kWaves * 64) void combine_gradient_kernel(CombineAr
     const int64_t t = (int64_t)blockIdx.x * kWaves + threadIdx.x / 64;
     if (t >= a.T) return;
     for (int j = 0; j < a.k; ++j) {
-        const int p = a.place[t * a.k + j];
+        const int64_t p = a.place ? a.place[t * a.k + j] : t * a.k + j;
         float sum = 0.0f;
         if (p >= 0 && p < a.rows) {
             const int64_t at_g = t * a.ldg, at_y = p * a.ldy;
@@ -735,7 +735,8 @@ int launch_combine_as(const CombineArgs &a, hipStream_t stream)
     for (int64_t t = 0; t < a.T && rc == MADDNESS_OK; t += kMostTokens) {
         CombineArgs part = a;
         part.T = std::min(kMostTokens, a.T - t);
-        part.place += t * a.k;
+        if (a.place) part.place += t * a.k;
+        else part.y = static_cast<const char *>(a.y) + t * a.k * a.ldy * elem_size(YT), part.rows -= t * a.k;
         if (a.weights) part.weights += t * a.k;
         if (a.dweights) {
             part.gradient = static_cast<const char *>(a.gradient) + t * a.ldg * elem_size(OT);

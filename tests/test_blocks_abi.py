@@ -139,3 +139,18 @@ def test_python_calls_refuse_host_tensors_and_wrong_types(mad):
                  lambda: mad.maddness_order(torch.zeros(4, dtype=torch.int32), 3)):
         with pytest.raises(TypeError):
             call()
+
+
+def test_product_by_choice_refuses(mad):
+    M, inval, unsupported, align = mad._BlockMatrix, mad.MADDNESS_E_INVAL, mad.MADDNESS_E_UNSUPPORTED, mad.MADDNESS_E_ALIGN
+    A, B = (M(data=FAKE, dtype=16, tile=1, rows=rows, cols=300, ld=304, stride=0, scale=FAKE, lds=4, scale_stride=0) for rows in (20, 30))
+
+    def call(groups=4, source=FAKE, slots=40, repeat=2, out=FAKE):
+        return mad.lib().maddness_block_product(C.byref(A), C.byref(B), 4, groups, None, source, slots, repeat, out, 2, 30, None, 0, None)
+
+    for kw, status, text in (
+            (dict(slots=-1), inval, "slots"), (dict(slots=513, repeat=100), unsupported, "slots"), (dict(repeat=0), inval, "repeat"),
+            (dict(slots=41), inval, "rows"), (dict(source=None), inval, "source"), (dict(source=FAKE + 2), align, "source"),
+            (dict(groups=0), inval, "groups"), (dict(groups=70000), unsupported, "groups"), (dict(out=None), inval, "out")):
+        refused(mad, call(**kw), status, text)
+    refused(mad, call(slots=0, source=None), mad.MADDNESS_OK)

@@ -315,3 +315,106 @@ def test_layer_takes_the_gradient_of_a_sum(mad):
     ones = torch.ones((), device="cuda").expand(50, 96)
     for got, want in zip(layer.backward(saved, ones), layer.backward(saved, ones.contiguous())):
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("T,E,k,K,N", [(1, 1, 1, 8, 1), (1, 8, 2, 512, 96), (4, 64, 6, 1024, 512), (37, 5, 3, 330, 70), (50, 3, 2, 2000, 33), (256, 40, 2, 200, 129)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("skew", [False, True])
+def test_product_by_choice_is_that_by_rows(mad, T, E, k, K, N, dtype, skew):
+    """Every slot's row by its expert's matrix: within the bound of its terms, and what an order of the slots gives."""
+    import torch
+    from test_gpu_block_product import check
+    print("case by choice", T, E, k, K, N, dtype, skew, flush=True)
+    rng = np.random.default_rng(T + E)
+    ids = rng.integers(-2, E + 2, (T, k)).astype(np.int32)                # some of no expert
+    if skew:
+        ids[rng.random((T, k)) < 0.8] = E // 2
+    x = torch.from_numpy(rng.standard_normal((T, K))).to(getattr(torch, dtype)).cuda()
+    W = mad.maddness_quantise_blocks(torch.from_numpy(rng.standard_normal((E, N, K)).astype(np.float32)).cuda(), 128)
+    ids_d = torch.from_numpy(ids).cuda()
+    A = mad.maddness_quantise_blocks(x)
+    flat = ids.reshape(-1)
+    for a in (x, A):
+        out = torch.full((T * k, N + 2), 7.0, dtype=torch.float32, device="cuda")
+        mad.maddness_block_product(a, W, by="choice", source=ids_d, out=out[:, 1:N + 1])
+        assert (out[:, 0] == 7).all() and (out[:, N + 1:] == 7).all()
+        out = out[:, 1:N + 1]
+        assert (out.cpu()[torch.from_numpy((flat < 0) | (flat >= E))] == 0).all()
+        for e in range(E):
+            slots = np.nonzero(flat == e)[0]
+            if len(slots):
+                check(out[torch.from_numpy(slots).cuda()], A.values()[torch.from_numpy(slots // k).cuda()].double().cpu().numpy(),
+                      W.values()[e].double().cpu().numpy(), f"expert {e}")
+    weights = torch.rand(T, k, device="cuda")
+    y = mad.maddness_block_product(x, W, by="choice", source=ids_d, out_dtype=x.dtype)
+    got = mad.maddness_combine(y, None, weights)
+    want = sum(weights[:, j:j + 1].double() * y.view(T, k, N)[:, j].double() for j in range(k))
+    size = sum(weights[:, j:j + 1].double() * y.view(T, k, N)[:, j].double().abs() for j in range(k))
+    # k roundings of fp32 and one of the result
+    unit = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}[dtype]
+    assert ((got.double() - want).abs() <= (k + 1) * 2.0 ** -23 * size + 1.01 * unit * want.abs() + 2.0 ** -24).all()
+    # one slot at a time: source as it is, of any rows
+    assert torch.equal(mad.maddness_block_product(x, W, by="choice", source=ids_d.view(-1), repeat=k, out_dtype=x.dtype), y)
+
+
+def test_product_by_choice_of_nothing(mad):
+    import torch
+    W = mad.maddness_quantise_blocks(torch.ones(3, 20, 32, device="cuda"), 128)
+    none = torch.zeros(0, 2, dtype=torch.int32, device="cuda")
+    assert mad.maddness_block_product(torch.zeros(0, 32, device="cuda"), W, by="choice", source=none).shape == (0, 20)
+    assert mad.maddness_block_product(torch.ones(4, 32, device="cuda"), W, by="choice", source=none).shape == (0, 20)
+    W0 = mad.BlockMatrix.empty((3, 20, 0), 128)
+    got = mad.maddness_block_product(torch.ones(2, 0, device="cuda"), W0, by="choice", source=torch.tensor([[0], [2]], dtype=torch.int32, device="cuda"))
+    assert torch.equal(got, torch.zeros(2, 20, dtype=torch.bfloat16, device="cuda"))
+
+
+def test_layer_by_choice_is_the_layer_by_order(mad, monkeypatch):
+    import torch
+    from paper_2106_10860_amd.expert_layer import ExpertLayer
+    g = torch.Generator(device="cuda").manual_seed(4)
+    layer = ExpertLayer.from_weights(torch.randn(24, 200, 300, generator=g, device="cuda"), 4)
+    for T in (1, 5, 60):
+        x, logits = torch.randn(T, 300, generator=g, device="cuda").half(), torch.randn(T, 24, generator=g, device="cuda")
+        logits[T // 2] = float("-inf")                                     # a token without an expert
+        assert layer.by_choice(T)
+        out, saved = layer.forward(x, logits)
+        assert (out[T // 2] == 0).all() and out.isfinite().all()
+        with monkeypatch.context() as way:
+            way.setattr(ExpertLayer, "by_choice", lambda self, tokens: False)
+            other, _ = layer.forward(x, logits)
+        assert torch.equal(out, other)
+    assert not layer.by_choice(97)
+
+
+def test_choice_refuses(mad):
+    import torch
+    W = mad.maddness_quantise_blocks(torch.ones(3, 20, 32, device="cuda"), 128)
+    x, ids = torch.ones(4, 32, device="cuda"), torch.zeros(4, 2, dtype=torch.int32, device="cuda")
+    for kw, error in ((dict(by="choice"), "source"), (dict(by="choice", source=ids, offsets=torch.zeros(4, dtype=torch.int32, device="cuda")), "offsets"),
+                      (dict(by="choice", source=ids[:, :1]), "contiguous|view"), (dict(by="choices", source=ids), "by must"),
+                      (dict(by="choice", source=ids.view(-1)), "rows"), (dict(by="choice", source=ids.view(-1), repeat=0), "repeat")):
+        with pytest.raises((ValueError, RuntimeError), match=error):
+            mad.maddness_block_product(x, W, **kw)
+    with pytest.raises((ValueError, RuntimeError), match="slots"):
+        mad.maddness_block_product(torch.ones(600, 32, device="cuda"), W, by="choice", source=torch.zeros(600, dtype=torch.int32, device="cuda"))
+    with pytest.raises((TypeError, ValueError), match="int32"):
+        mad.maddness_block_product(x, W, by="choice", source=ids.long())
+    with pytest.raises((ValueError, RuntimeError), match="place"):
+        mad.maddness_combine(torch.ones(7, 20, device="cuda"), None, torch.ones(4, 2, device="cuda"))
+    with pytest.raises(ValueError, match="place"):
+        mad.maddness_combine(torch.ones(8, 20, device="cuda"))
+
+
+def test_choice_without_the_native_marshalling_gives_the_same(mad, monkeypatch):
+    import torch
+    W = mad.maddness_quantise_blocks(torch.randn(3, 20, 32, device="cuda"), 128)
+    x, ids = torch.randn(4, 32, device="cuda"), torch.tensor([[0, 2], [1, -1], [2, 2], [5, 0]], dtype=torch.int32, device="cuda")
+    weights = torch.rand(4, 2, device="cuda")
+
+    def all_of():
+        y = mad.maddness_block_product(x, W, by="choice", source=ids)
+        return y, mad.maddness_combine(y, None, weights), mad.maddness_combine(y, weights=weights)
+    want = all_of()
+    monkeypatch.setattr(mad, "_native", mad._NotBuilt)
+    for a, b in zip(want, all_of()):
+        assert torch.equal(a, b)
