@@ -355,7 +355,7 @@ int maddness_quantise_blocks(const void *x, int32_t dtype, int64_t count, int64_
  * out[m][n] = sum_k A[m][k] B[n][k] of two block matrices, every 8-bit value times its power of two, rounded once to
  * out_dtype (F32, F16 or BF16).  Products and sums are those of fp32 where out_dtype is F32 or the rows are few; for results
  * of 16 bits the 128 products of a block may be cut off at 2^-11 of the largest of them before they are added up in fp32.
- * The order of the sum depends on the sizes only.
+ * The order of the sum depends on the sizes and types only.
  *
  * by      MADDNESS_DENSE: A is [M][K], B [N][K], out [M][ldo].
  *         MADDNESS_BY_ROWS: rows offsets[e] .. offsets[e + 1] - 1 of A are multiplied with the e-th of `groups` matrices
@@ -418,7 +418,7 @@ int maddness_route_gradient(const void *logits, int32_t dtype, int64_t T, int32_
 /*
  * The slots 0 .. slots - 1 (slot t k + j is the j-th choice of token t) in the order of their experts, and in their own order
  * for one expert.  An id outside [0, E) has no place.
- * offsets [E + 1]: expert e has the places offsets[e] .. offsets[e + 1] - 1, a multiple of `align` of them; counts [E]
+ * offsets [E + 1]: expert e has the places offsets[e] .. offsets[e + 1] - 1, a multiple of `align` (1 .. 65536) of them; counts [E]
  *         (or NULL): how many are taken, the first ones.
  * source  [capacity]: the slot at each place, -1 where there is none.
  * place   [slots]: the place of each slot, -1 where it has none.

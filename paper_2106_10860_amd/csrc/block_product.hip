@@ -8,8 +8,8 @@
 // come from the first, fp32 results from the second; few rows always from the second, as memory bounds them.
 //
 // B's rows (the columns of out) are the instruction's first operand and A's rows its second, so that a lane's four results are
-// four neighbours in a row of out.  Lane l holds row l % 16, values 32 (l / 16) .. + 31 of an operand's block, and results
-// n = 4 (l / 16) + i of row m = l % 16.
+// four neighbours in a row of out.  Lane l holds 32 values of row l % 16 of an operand's block (which 32 does not matter as long as they are
+// the same ones of both operands), and results n = 4 (l / 16) + i of row m = l % 16.
 #include "block_common.h"
 
 namespace maddness {
@@ -111,10 +111,11 @@ __device__ __forceinline__ int64_t row_of_a(const ProductArgs &p, int64_t m)
 
 // Few rows: 16 MT rows by 16 NT columns to a workgroup; its wavefronts take every WAVES-th block of the sum, DEPTH of them asked for
 // at once, and add up in LDS, in their order.  B comes straight from memory, in pieces of 32 bytes to a lane, and so does an 8-bit A; a floating
-// A is rounded into LDS while the first of B is on its way.
+// A is rounded into LDS while the first of B is on its way.  Bound by the way of one piece: 1 x 4096 x 4096 6.7 us (16.8 MB, 2.5 TB/s),
+// 37 x 1000 x 510 8.1.
 //
 // CHOICE: of the slots, those whose id is the workgroup's expert, found by going through all ids, 16 MT at a time; no order of them is needed.  The rows of
-// results are the slots themselves.
+// results are the slots themselves.  (24 slots of 64 experts of 1024 x 512: 10.0 us; 7.0 and a launch of 4.5 before it with an order.)
 template <int AT, int MT, int NT, int WAVES, int DEPTH, int OUT, bool CHOICE>
 __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, uint32_t col_tiles)
 {

@@ -192,7 +192,8 @@ __device__ __forceinline__ void sort_down(double (&x)[R])
 }
 
 // LANES lanes to a token, R experts to a lane.  The lane sorts its experts; then k times the first of all lanes is the next choice, and leaves its
-// lane's list.  Bound by the vector units: E / LANES exponentials, divisions and a sort for each lane.  KEEP: how much of a lane's list is needed for k.
+// lane's list.  Bound by the vector units: E / LANES exponentials, divisions and a sort for each lane (32768 tokens, 8 of 256 experts out of 4 of 8 groups
+// 32.5 us).  KEEP: how much of a lane's list is needed for k (with all 16 of it 37.6).
 template <int DT, int LANES, int R, int KEEP>
 __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
 {
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
 }
 
 // w_j = factor s_j (/ sum of the chosen s): with g_j the gradient of s_j, dx = s (g - sum g s) for the softmax and g s (1 - s) for
-// the sigmoid.  The few g_j are spread over the row in LDS.
+// the sigmoid.  The few g_j are spread over the row in LDS.  Bound by memory where there are many tokens (32768 of 256 experts 18.4 us, 67 MB).
 template <int DT, int LANES, int R>
 __global__ __launch_bounds__(256) void route_gradient_kernel(RouteArgs a)
 {
@@ -549,7 +550,8 @@ __device__ __forceinline__ uint64_t same_expert(int e, int E)
     return same;
 }
 
-// Up to kOrderAtOnce slots: all of it by one workgroup, each wavefront with a stretch of the slots, in a launch instead of three.
+// Up to kOrderAtOnce slots: all of it by one workgroup, each wavefront with a stretch of the slots, in a launch instead of three (8198 slots 8.4 us;
+// the three, for 49152, 5 each).
 constexpr int64_t kOrderAtOnce = 16384;
 
 __global__ __launch_bounds__(1024) void order_kernel(const int32_t *ids, int slots, int E, int align, int32_t *offsets, int32_t *counts, int32_t *source,
@@ -656,7 +658,8 @@ struct CombineArgs {
     float *dweights;
 };
 
-// A wavefront to a token (several where the rows are long); up to 8 of the token's rows are on their way at once.
+// A wavefront to a token (several where the rows are long); up to 8 of the token's rows are on their way at once.  Bound by memory: 8192 tokens, 6
+// rows of 1024 bfloat16 each, 19 us, 6.1 TB/s.
 template <int YT, int OT>
 __global__ __launch_bounds__(kWaves * 64) void combine_kernel(CombineArgs a)
 {
