@@ -353,8 +353,11 @@ int maddness_quantise_blocks(const void *x, int32_t dtype, int64_t count, int64_
 
 /*
  * out[m][n] = sum_k A[m][k] B[n][k] of two block matrices, every 8-bit value times its power of two, rounded once to
- * out_dtype (F32, F16 or BF16).  Products and sums are those of fp32 where out_dtype is F32 or the rows are few; for results
- * of 16 bits the 128 products of a block may be cut off at 2^-11 of the largest of them before they are added up in fp32.
+ * out_dtype (F32, F16 or BF16).  Products and sums are those of fp32, but for BF16 results of many rows: there the products of
+ * each eight neighbours along the sum (k = 0 .. 7, 8 .. 15, ..) are cut off, towards 0, at 2^-13 of the largest of them before they
+ * are added up in fp32, so that a result may be off by 7 2^-13 of the sum of its products' magnitudes beside its rounding
+ * (factors below 2^-6 of their power of two count as that much).  Whether the rows are many depends on all sizes, so
+ * the same row may have other low bits beside more rows; F32 results are cut at no size.
  * The order of the sum depends on the sizes and types only.
  *
  * by      MADDNESS_DENSE: A is [M][K], B [N][K], out [M][ldo].

@@ -1,0 +1,70 @@
+"""The product of many rows, by the kernel for them: every result against 64 bits, and which kernel it was."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mad():
+    import torch
+    import paper_2106_10860_amd as m
+    assert torch.cuda.is_available()
+    m.lib()
+    return m
+
+
+def factors(b):
+    """What a matrix stands for, and its magnitudes where those below 2^-6 of their power of two (not normal numbers) count as that much."""
+    import torch
+    v = b.values().double()
+    rows, cols = v.shape
+    e = b.scale[:, : -(-cols // 128)].double().repeat_interleave(128, 1)[:, :cols].repeat_interleave(b.tile, 0)[:rows]
+    return v, torch.maximum(v.abs(), torch.exp2(e - 127 - 6))
+
+
+def bound(A, B, dtype):
+    """The product in 64 bits and how far a result may be off: K products and sums in fp32, one rounding to the result's type; for
+    bfloat16, of every eight products seven cut off at 2^-13 of the largest."""
+    import torch
+    (a, a_cut), (b, b_cut) = A, B
+    want = a @ b.T
+    unit, least = {torch.float32: (2.0 ** -24, 2.0 ** -150), torch.float16: (2.0 ** -11, 2.0 ** -25), torch.bfloat16: (2.0 ** -8, 2.0 ** -134)}[dtype]
+    tol = (a.shape[1] + 8) * 2.0 ** -23 * (a.abs() @ b.abs().T) * 1.01 + unit * want.abs() * 1.01 + least
+    return want, tol + 7 * 2.0 ** -13 * (a_cut @ b_cut.T) if dtype is torch.bfloat16 else tol
+
+
+def check(got, A, B, label):
+    want, tol = bound(A, B, got.dtype)
+    worst = float(((got.double() - want).abs() / tol).max())
+    assert worst <= 1, f"{label}: {worst:.2f} of the bound"
+
+
+# rows, columns, and the tiles that results of 16 and of 32 bits take
+LARGE, SMALL = (4096, 4096), (2048, 2048)
+
+
+def tiles_of(kernel):
+    assert kernel.startswith("product_tiles_kernel"), kernel
+    return tuple(int(kernel.split(f"{n} = ")[1].split(",")[0]) for n in ("BM", "BN"))
+
+
+def dtype_of(name):
+    import torch
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+@pytest.mark.parametrize("M,N", [LARGE, SMALL])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_small_products_beside_a_large_one(mad, M, N, dtype):
+    """Of every eight products one is 1 and seven are some 2^-11 to 2^-14 of it, all of one sign: an instruction that cuts them off takes them all away."""
+    import torch
+    print("case small beside large", M, N, dtype, flush=True)
+    K, dt = 256, dtype_of(dtype)
+    small = 1.875 * torch.exp2(-14 + torch.arange(M, device="cuda") % 4).view(M, 1)
+    x = torch.where(torch.arange(K, device="cuda") % 8 == 3, 1.0, small)
+    A, B = mad.maddness_quantise_blocks(x), mad.maddness_quantise_blocks(torch.ones(N, K, device="cuda"), 128)
+    assert torch.equal(A.values(), x)
+    got = mad.maddness_block_product(A, B, out_dtype=dt)
+    assert tiles_of(mad.maddness_last_kernel()) == ((256, 256 if dtype == "bf16" else 128) if (M, N) == LARGE else (128, 128))
+    check(got, factors(A), factors(B), f"{M} x {N} {dtype}")
