@@ -29,15 +29,24 @@ class Saved:
 
 class ExpertLayer:
     """W: BlockMatrix [experts, outputs, inputs] in tiles of 128; Wt: the same transposed, for the backward pass (or None).
-    The choice is that of ``maddness_route``."""
+    The choice is that of ``maddness_route``.
+
+    ``slot_dtype`` is what a token's k results are held in between their products and the weighted sum (and those of the backward pass).  In
+    fp32, the default, out and the gradients are rounded once, to the types that they are returned in.  A narrower type halves the bytes of
+    that step and rounds every one of the k; float16 makes a result beyond 65504 infinite, also where its weight is 0 or the sum would be in
+    range."""
 
     def __init__(self, W: "m.BlockMatrix", Wt=None, k: int = 1, scores: str = "softmax", bias=None, groups: int = 1, kept_groups: int = 1,
-                 renormalise: bool = True, factor: float = 1.0):
+                 renormalise: bool = True, factor: float = 1.0, slot_dtype=None):
         if len(W.shape) != 3:
             raise ValueError("W must be [experts, outputs, inputs]")
         if Wt is not None and Wt.shape != (W.shape[0], W.shape[2], W.shape[1]):
             raise ValueError("Wt must be the transpose of W")
-        self.W, self.Wt, self.experts, self.k = W, Wt, W.shape[0], k
+        if slot_dtype is None:
+            import torch
+            slot_dtype = torch.float32
+        m.blocks._float_code(slot_dtype, "slot_dtype")
+        self.W, self.Wt, self.experts, self.k, self.slot_dtype = W, Wt, W.shape[0], k, slot_dtype
         self.choice = {"scores": scores, "renormalise": renormalise, "factor": factor}
         self.groups = {"bias": bias, "groups": groups, "kept_groups": kept_groups}
 
@@ -62,13 +71,13 @@ class ExpertLayer:
             raise ValueError("training needs Wt")
         ids, weights = m.maddness_route(logits, self.k, **self.choice, **self.groups)
         if not training and self.by_choice(x.shape[0]):
-            y = m.maddness_block_product(x, self.W, by="choice", source=ids, out_dtype=x.dtype)
-            return m.maddness_combine(y, None, weights), Saved(ids, weights)
+            y = m.maddness_block_product(x, self.W, by="choice", source=ids, out_dtype=self.slot_dtype)
+            return m.maddness_combine(y, None, weights, out_dtype=x.dtype), Saved(ids, weights)
         # in training the sums over an expert's tokens are products by depth, which go by whole blocks
         offsets, _, source, place = m.maddness_order(ids, self.experts, m.BLOCK if training else 1)
         x_t = m.maddness_quantise_blocks(x, transposed=True, source=source, repeat=self.k) if training else None
-        y = m.maddness_block_product(x, self.W, offsets, source=source, repeat=self.k, out_dtype=x.dtype)
-        out = m.maddness_combine(y, place, weights)
+        y = m.maddness_block_product(x, self.W, offsets, source=source, repeat=self.k, out_dtype=self.slot_dtype)
+        out = m.maddness_combine(y, place, weights, out_dtype=x.dtype)
         if not training:
             return out, Saved(ids, weights)
         return out, Saved(ids, weights, logits, offsets, source, place, x_t, y, x.shape[0])
@@ -85,7 +94,7 @@ class ExpertLayer:
         dweights = m.maddness_combine_gradient(grad, saved.y, saved.place)
         dlogits = m.maddness_route_gradient(saved.logits, saved.ids, dweights, **self.choice)
         dy, dy_t = m.maddness_quantise_blocks(grad, both=True, source=saved.source, repeat=self.k, factors=saved.weights)
-        dx = m.maddness_combine(m.maddness_block_product(dy, self.Wt, saved.offsets, out_dtype=grad.dtype), saved.place)
+        dx = m.maddness_combine(m.maddness_block_product(dy, self.Wt, saved.offsets, out_dtype=self.slot_dtype), saved.place, out_dtype=grad.dtype)
         dW = m.maddness_block_product(dy_t, saved.x_t, saved.offsets, by="depth", out_dtype=weight_dtype or grad.dtype)
         return dx, dW, dlogits
 
