@@ -80,7 +80,8 @@ class ExpertLayer:
         out = m.maddness_combine(y, place, weights, out_dtype=x.dtype)
         if not training:
             return out, Saved(ids, weights)
-        return out, Saved(ids, weights, logits, offsets, source, place, x_t, y, x.shape[0])
+        # (a copy: the caller may write to its logits before the backward pass)
+        return out, Saved(ids, weights, logits.clone(), offsets, source, place, x_t, y, x.shape[0])
 
     def backward(self, saved: Saved, grad, weight_dtype=None):
         """The gradient of out [T, outputs] -> those of x, of the matrices [experts, outputs, inputs] (of ``weight_dtype``, or grad's
