@@ -212,6 +212,8 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", so
     how = _BY.get(by)
     if how is None:
         raise ValueError(f"by must be 'rows', 'depth' or 'choice', is {by!r}")
+    if how == MADDNESS_BY_DEPTH and offsets is None:
+        raise ValueError("by='depth' needs offsets")
     if how == MADDNESS_BY_CHOICE:
         if source is None or offsets is not None:
             raise ValueError("by='choice' goes with source, and without offsets")

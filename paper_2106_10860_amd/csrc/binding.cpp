@@ -498,7 +498,7 @@ PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
             offsets = static_cast<const int32_t *>(o.data_ptr());
             if (by == MADDNESS_BY_ROWS ? experts != groups : experts != -1) throw NotUsual();
         } else {
-            if (experts != -1) throw NotUsual();
+            if (experts != -1 || by != MADDNESS_BY_ROWS) throw NotUsual();
             by = MADDNESS_DENSE;
         }
         int64_t rows = A.rows;
