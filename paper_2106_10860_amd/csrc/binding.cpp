@@ -419,7 +419,7 @@ PyObject *quantise_blocks(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int code = float_code(x.scalar_type());
         const int64_t tile = whole(a[1]);
         const bool transposed = truth(a[2]), both = truth(a[3]);
-        const int64_t repeat = whole(a[5]);
+        const int32_t repeat = narrow(whole(a[5]));
         if (x.dim() != 2 || (tile != 1 && tile != MADDNESS_BLOCK) || repeat < 1) throw NotUsual();
         const Rows rx = rows_of(x);
         int64_t rows = rx.rows;
@@ -447,7 +447,7 @@ PyObject *quantise_blocks(PyObject *, PyObject *const *a, Py_ssize_t n)
         uint8_t *q = bytes(straight.q), *s = bytes(straight.scale), *qt = bytes(turned.q), *st = bytes(turned.scale);
         int rc;
         Py_BEGIN_ALLOW_THREADS
-        rc = maddness_quantise_blocks(x_p, code, 1, rows, rx.cols, rx.ld, 0, (int32_t)tile, source, rx.rows, (int32_t)repeat, factors, q,
+        rc = maddness_quantise_blocks(x_p, code, 1, rows, rx.cols, rx.ld, 0, (int32_t)tile, source, rx.rows, repeat, factors, q,
                                       q ? straight.ld : 0, s, q ? straight.lds : 0, qt, qt ? turned.ld : 0, st, qt ? turned.lds : 0, stream);
         Py_END_ALLOW_THREADS
         if (rc != MADDNESS_OK) return int_status(rc);

@@ -68,3 +68,15 @@ def test_small_products_beside_a_large_one(mad, M, N, dtype):
     got = mad.maddness_block_product(A, B, out_dtype=dt)
     assert tiles_of(mad.maddness_last_kernel()) == ((256, 256 if dtype == "bf16" else 128) if (M, N) == LARGE else (128, 128))
     check(got, factors(A), factors(B), f"{M} x {N} {dtype}")
+
+
+def test_a_repeat_beyond_32_bits_is_refused(mad):
+    import torch
+    x, source = torch.ones(5, 64, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    B = mad.maddness_quantise_blocks(torch.ones(2, 30, 64, device="cuda"), 128)
+    off = torch.tensor([0, 1, 3], dtype=torch.int32, device="cuda")
+    for repeat in (2 ** 31, 2 ** 32 + 1, 2 ** 70):
+        with pytest.raises(ValueError, match="repeat"):
+            mad.maddness_quantise_blocks(x, source=source, repeat=repeat)
+        with pytest.raises(ValueError, match="repeat"):
+            mad.maddness_block_product(x, B, off, source=source, repeat=repeat)
