@@ -233,7 +233,9 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
             const int n = whole ? size / R * 2 : size;
             for (int i = 0; i < n; ++i) rank(all_keys[mine][lane * n + i]);
         }
-        const float value = best > kNone ? (second > kNone ? best + second : best) : kNone;
+        // (a sum of two keys may be minus infinity where both are near the lowest number; a group without an expert has none: NaN is before nothing)
+        const bool any = best > kNone;
+        const float value = any ? (second > kNone ? best + second : best) : __builtin_nanf("");
         if (lane < a.groups) all_values[mine][lane] = value;
         wave_lds_fence();
         int before = 0;
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
             const float other = all_values[mine][g];
             before += other > value || (other == value && g < lane);
         }
-        uint64_t kept = __ballot(lane < a.groups && value > kNone && before < a.kept);
+        uint64_t kept = __ballot(lane < a.groups && any && before < a.kept);
         if constexpr (LANES == 16) kept = kept >> (threadIdx.x & 48) & 0xffff;
         int g = e0 / size, end = (g + 1) * size;
         if (whole) {
