@@ -10,6 +10,9 @@ float, its rows are then rounded within the call.  With W of shape [outputs, inp
     dy, dy_t = maddness_quantise_blocks(grad, both=True)
     dx = maddness_block_product(dy, Wt)
     dw = maddness_block_product(dy_t, maddness_quantise_blocks(x, transposed=True), out_dtype=torch.float32)
+
+The calls are no part of torch's autograd: an operand that requires a gradient is refused while gradients are recorded.  A program calls
+the gradients' own calls, as above, or makes a torch.autograd.Function of both.
 """
 from __future__ import annotations
 
@@ -43,11 +46,18 @@ def _fits(**numbers) -> None:
             raise ValueError(f"{name} = {v} does not fit 32 bits")
 
 
+def _no_gradient(t, name: str) -> None:
+    if t.requires_grad and _m._torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which these calls do not record: give {name}.detach(), or call under torch.no_grad() "
+                         "or in a torch.autograd.Function, whose backward makes the gradients' calls")
+
+
 def _code(t, name: str) -> int:
     """The dtype code of a floating device tensor."""
     torch = _m._torch or _m._torch_module()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
+    _no_gradient(t, name)
     return _float_code(t.dtype, name)
 
 
@@ -71,6 +81,7 @@ def _flat(t, dtype, shape, name: str):
     if t is None:
         return None
     p = _m._ptr(t, dtype, name)
+    _no_gradient(t, name)
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, has {tuple(t.shape)}")
     if not t.is_contiguous():

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -353,10 +354,18 @@ at::ScalarType dtype_or(PyObject *o, at::ScalarType otherwise)
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
+// A tensor that nothing is to be recorded of: the Python code says so of one that has a gradient.
+const at::Tensor &plain(PyObject *o)
+{
+    const at::Tensor &t = tensor(o);
+    if (t.requires_grad() && c10::GradMode::is_enabled()) throw NotUsual();
+    return t;
+}
+
 // A contiguous tensor of this type and these sizes.
 const at::Tensor &flat(PyObject *o, at::ScalarType type, at::IntArrayRef sizes, const at::Device &device)
 {
-    const at::Tensor &t = tensor(o);
+    const at::Tensor &t = plain(o);
     if (t.scalar_type() != type || t.sizes() != sizes || !t.is_contiguous() || t.device() != device) throw NotUsual();
     return t;
 }
@@ -415,7 +424,7 @@ PyObject *quantise_blocks(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
         if (n != 7) throw NotUsual();
-        const at::Tensor &x = tensor(a[0]);
+        const at::Tensor &x = plain(a[0]);
         const int code = float_code(x.scalar_type());
         const int64_t tile = whole(a[1]);
         const bool transposed = truth(a[2]), both = truth(a[3]);
@@ -431,7 +440,7 @@ PyObject *quantise_blocks(PyObject *, PyObject *const *a, Py_ssize_t n)
             rows = s.size(0);
             source = static_cast<const int32_t *>(s.data_ptr());
             if (a[6] != Py_None) {
-                const at::Tensor &f = tensor(a[6]);
+                const at::Tensor &f = plain(a[6]);
                 if (f.scalar_type() != at::kFloat || !f.is_contiguous() || f.numel() != rx.rows * repeat || f.device() != x.device()) throw NotUsual();
                 factors = static_cast<const float *>(f.data_ptr());
             }
@@ -474,7 +483,7 @@ PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
             A = block_matrix(a[1], nullptr, &experts, &device);
             if (experts != -1) throw NotUsual();
         } else {
-            const at::Tensor &x = tensor(a[1]);
+            const at::Tensor &x = plain(a[1]);
             const Rows r = rows_of(x);
             A.data = x.data_ptr();
             A.dtype = float_code(x.scalar_type());
@@ -523,7 +532,7 @@ PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
             out = made.data_ptr();
             ldo = std::max(B.rows, (int64_t)1);
         } else {
-            const at::Tensor &o = tensor(a[8]);
+            const at::Tensor &o = plain(a[8]);
             if (by == MADDNESS_BY_DEPTH || o.device() != device || (a[7] != Py_None && o.scalar_type() != type)) throw NotUsual();
             const Rows r = rows_of(o);
             if (r.rows != rows || r.cols != B.rows) throw NotUsual();
@@ -558,7 +567,7 @@ PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
         if (n != 8 || !PyFloat_CheckExact(a[7])) throw NotUsual();
-        const at::Tensor &x = tensor(a[0]);
+        const at::Tensor &x = plain(a[0]);
         const int code = float_code(x.scalar_type());
         const Rows r = rows_of(x);
         const int32_t k = narrow(whole(a[1])), groups = narrow(whole(a[4])), kept = narrow(whole(a[5]));
@@ -590,7 +599,7 @@ PyObject *route_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
         if (n != 6 || !PyFloat_CheckExact(a[5])) throw NotUsual();
-        const at::Tensor &x = tensor(a[0]), &ids = tensor(a[1]);
+        const at::Tensor &x = plain(a[0]), &ids = tensor(a[1]);
         const int code = float_code(x.scalar_type());
         const Rows r = rows_of(x);
         if (ids.dim() != 2 || r.cols > MADDNESS_MAX_EXPERTS) throw NotUsual();
@@ -650,7 +659,7 @@ PyObject *combine(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
         if (n != 5) throw NotUsual();
-        const at::Tensor &y = tensor(a[0]), &slots = tensor(a[a[1] == Py_None ? 2 : 1]);
+        const at::Tensor &y = plain(a[0]), &slots = tensor(a[a[1] == Py_None ? 2 : 1]);
         const int code = float_code(y.scalar_type());
         const Rows r = rows_of(y);
         if (slots.dim() != 2 || a[4] != Py_None) throw NotUsual();
@@ -678,7 +687,7 @@ PyObject *combine_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return usual([&]() -> PyObject * {
         if (n != 3) throw NotUsual();
-        const at::Tensor &g = tensor(a[0]), &y = tensor(a[1]), &place = tensor(a[2]);
+        const at::Tensor &g = plain(a[0]), &y = plain(a[1]), &place = tensor(a[2]);
         const int code = float_code(g.scalar_type()), y_code = float_code(y.scalar_type());
         const Rows rg = rows_of(g), ry = rows_of(y);
         if (place.dim() != 2 || rg.cols != ry.cols || g.device() != y.device()) throw NotUsual();
