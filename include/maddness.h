@@ -367,7 +367,8 @@ int maddness_quantise_blocks(const void *x, int32_t dtype, int64_t count, int64_
  *         (0 where there are none); both have tile 1.  For whole blocks, the offsets are multiples of 128.
  *         MADDNESS_BY_CHOICE: out has `slots` rows, and row r is that of A's row r / repeat with the source[r]-th of `groups`
  *         matrices of B, zeros where that is outside [0, groups).  For few rows, which need no order: slots up to
- *         MADDNESS_MAX_CHOSEN, A with at least slots / repeat rows.  The results are those of MADDNESS_BY_ROWS.
+ *         MADDNESS_MAX_CHOSEN, A with at least slots / repeat rows.  Products and sums are those of fp32 for every type; the low bits are
+ *         those of MADDNESS_BY_ROWS where that takes the kernel for few rows too.
  * offsets NULL, or [groups + 1] on the device (MADDNESS_BY_ROWS and _BY_DEPTH), not decreasing.  One outside the matrix is cut back to it, and for
  *         MADDNESS_BY_DEPTH one that is no multiple of 128 is rounded down to one, so a wrong array gives wrong sums
  *         but no bad access.

@@ -80,3 +80,32 @@ def test_a_repeat_beyond_32_bits_is_refused(mad):
             mad.maddness_quantise_blocks(x, source=source, repeat=repeat)
         with pytest.raises(ValueError, match="repeat"):
             mad.maddness_block_product(x, B, off, source=source, repeat=repeat)
+
+
+@pytest.mark.parametrize("T,E,k,K,N,same", [(64, 8, 2, 1024, 256, True), (256, 40, 2, 512, 512, True), (256, 2, 2, 4096, 4096, False), (170, 1, 3, 2048, 4100, False)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_product_by_choice_beside_the_product_by_rows(mad, T, E, k, K, N, same, dtype):
+    """The same results where both take the kernel for few rows; where the rows by an order are many, each within the bound of its own sums."""
+    import torch
+    print("case choice and rows", T, E, k, K, N, dtype, flush=True)
+    g, dt = torch.Generator(device="cuda").manual_seed(T), dtype_of(dtype)
+    x = torch.randn(T, K, generator=g, device="cuda")
+    W = mad.maddness_quantise_blocks(torch.randn(E, N, K, generator=g, device="cuda"), 128)
+    ids = torch.randint(E, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    A = mad.maddness_quantise_blocks(x)
+    by_choice = mad.maddness_block_product(A, W, by="choice", source=ids, out_dtype=dt)
+    assert mad.maddness_last_kernel().startswith("product_few_kernel")
+    offsets, _, source, place = mad.maddness_order(ids, E)
+    by_rows = mad.maddness_block_product(A, W, offsets, source=source, repeat=k, out_dtype=dt)
+    assert mad.maddness_last_kernel().startswith("product_few_kernel" if same else "product_tiles_kernel")
+    by_rows = by_rows[place.view(-1).long()]
+    assert not same or torch.equal(by_choice, by_rows)
+    a, flat = factors(A), ids.view(-1)
+    for e in range(E):
+        slots = (flat == e).nonzero().view(-1)
+        of = tuple(v[slots // k] for v in a)
+        b = factors(mad.BlockMatrix(W.q[e], W.scale[e], 128))
+        check(by_rows[slots], of, b, f"by rows, expert {e}")
+        want, tol = bound(of, b, torch.float32)            # (by choice no product is cut off)
+        unit = {"f32": 0, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype]
+        assert ((by_choice[slots].double() - want).abs() <= tol + 1.01 * unit * want.abs() + 2.0 ** -25).all()
