@@ -358,6 +358,8 @@ int maddness_quantise_blocks(const void *x, int32_t dtype, int64_t count, int64_
  * are added up in fp32, so that a result may be off by 7 2^-13 of the sum of its products' magnitudes beside its rounding
  * (factors below 2^-6 of their power of two count as that much).  Whether the rows are many depends on all sizes, so
  * the same row may have other low bits beside more rows; F32 results are cut at no size.
+ * Products of fp32 take a value times its power of two as a bfloat16 number.  That is what it is for the exponent bytes 3 to 246; below
+ * them it is rounded to a multiple of 2^-133, and one of 2^128 or more (which maddness_quantise_blocks makes of |x| above 3.296e38) is infinite.
  * The order of the sum depends on the sizes and types only.
  *
  * by      MADDNESS_DENSE: A is [M][K], B [N][K], out [M][ldo].

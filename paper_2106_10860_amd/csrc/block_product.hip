@@ -19,7 +19,8 @@ namespace {
 using bf16x2 = __attribute__((ext_vector_type(2))) __bf16;
 using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
 
-// Eight E4M3 values times 2^(byte - 127), exactly; scale = byte << 23 (the conversion reads its exponent only, 255 gives NaN).
+// Eight E4M3 values times 2^(byte - 127) as bfloat16 numbers: exactly for the bytes 3 to 246 (the values are multiples of 2^-9 of up to 448, bfloat16 has
+// the multiples of 2^-133 with 8 digits below 2^128).  scale = byte << 23 (the conversion reads its exponent only, 255 gives NaN).
 __device__ __forceinline__ bf16x8 widen8(int lo, int hi, float scale)
 {
     const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);

@@ -109,3 +109,28 @@ def test_product_by_choice_beside_the_product_by_rows(mad, T, E, k, K, N, same, 
         want, tol = bound(of, b, torch.float32)            # (by choice no product is cut off)
         unit = {"f32": 0, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype]
         assert ((by_choice[slots].double() - want).abs() <= tol + 1.01 * unit * want.abs() + 2.0 ** -25).all()
+
+
+@pytest.mark.parametrize("N", [16, 4096])
+def test_every_value_with_every_power_of_two(mad, N):
+    """Times 1 and times 2^-100, in both kernels: exact for the exponent bytes 3 to 246."""
+    import torch
+    values = torch.arange(256, dtype=torch.uint8, device="cuda")
+    values = values[(values & 127) != 127]
+    bytes_ = torch.arange(3, 247, dtype=torch.uint8, device="cuda")
+    rows = len(values) * len(bytes_)
+    q, scale = torch.zeros(rows, 16, dtype=torch.uint8, device="cuda"), torch.full((rows, 4), 127, dtype=torch.uint8, device="cuda")
+    q[:, 0] = values.repeat(len(bytes_))
+    scale[:, 0] = bytes_.repeat_interleave(len(values))
+    want = q[:, 0].view(torch.float8_e4m3fn).double() * torch.exp2(scale[:, 0].double() - 127)
+    step = rows if N > 16 else 60
+    for power in (0, -100):
+        b = torch.zeros(N, 16, device="cuda")
+        b[:, 0] = 2.0 ** power
+        B = mad.maddness_quantise_blocks(b)
+        for r in range(0, rows, step):
+            A = mad.BlockMatrix(q[r:r + step].view(torch.float8_e4m3fn), scale[r:r + step])
+            got = mad.maddness_block_product(A, B, out_dtype=torch.float32)
+            assert mad.maddness_last_kernel().startswith("product_tiles_kernel" if N > 16 else "product_few_kernel")
+            exact = (want[r:r + step] * 2.0 ** power).float()
+            assert torch.equal(got[:, 0], exact) and torch.equal(got[:, N - 1], exact)
