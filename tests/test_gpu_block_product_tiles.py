@@ -35,8 +35,12 @@ def bound(A, B, dtype):
 
 
 def check(got, A, B, label):
+    import torch
     want, tol = bound(A, B, got.dtype)
-    worst = float(((got.double() - want).abs() / tol).max())
+    most = torch.finfo(got.dtype).max
+    far = want.abs() + tol > most                          # (beyond the type's largest number, or nearly: infinite, or nearly that)
+    assert (got[far].abs() >= most * (1 - 2.0 ** -7)).all(), f"{label}: small results for large ones"
+    worst = float(torch.where(far, 0, (got.double() - want).abs() / tol).max())
     assert worst <= 1, f"{label}: {worst:.2f} of the bound"
 
 
@@ -134,3 +138,157 @@ def test_every_value_with_every_power_of_two(mad, N):
             assert mad.maddness_last_kernel().startswith("product_tiles_kernel" if N > 16 else "product_few_kernel")
             exact = (want[r:r + step] * 2.0 ** power).float()
             assert torch.equal(got[:, 0], exact) and torch.equal(got[:, N - 1], exact)
+
+
+def matrix(mad, seed, rows, cols, tile):
+    """Rows of unequal size, a tenth of the values 0, the first block of every seventh row (or all of its tile) too; behind the columns NaN
+    bytes and NaN exponents."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(rows, cols, generator=g, device="cuda") * torch.exp2(torch.randint(-4, 3, (rows, 1), generator=g, device="cuda").float())
+    x *= torch.rand(rows, cols, generator=g, device="cuda") > 0.1
+    x[torch.arange(rows, device="cuda") // tile % 7 == 3, :128] = 0
+    made, blocks = mad.maddness_quantise_blocks(x, tile), -(-cols // 128)
+    q = torch.full((rows, cols // 16 * 16 + 48), 127, dtype=torch.uint8, device="cuda")
+    q[:, :cols] = made.q.view(torch.uint8)
+    scale = torch.full((made.scale.shape[0], -(-blocks // 4) * 4 + 4), 255, dtype=torch.uint8, device="cuda")
+    scale[:, :blocks] = made.scale[:, :blocks]
+    return mad.BlockMatrix(q.view(torch.float8_e4m3fn)[:, :cols], scale, tile)
+
+
+def experts(mad, seed, E, rows, cols):
+    import torch
+    parts = [matrix(mad, seed + e, rows, cols, 128) for e in range(E)]
+    q = torch.stack([p.q.as_strided((rows, p.q.stride(0)), (p.q.stride(0), 1)).view(torch.uint8) for p in parts])
+    return mad.BlockMatrix(q.view(torch.float8_e4m3fn)[..., :cols], torch.stack([p.scale for p in parts]), 128)
+
+
+def expert(W, e):
+    return type(W)(W.q[e], W.scale[e], W.tile)
+
+
+def offsets_of(counts, align):
+    return np.concatenate([[0], np.cumsum([-(-c // align) * align for c in counts])]).astype(np.int32)
+
+
+def shape_of(dtype, large):
+    return (128, 128) if not large else (256, 256) if dtype == "bf16" else (256, 128)
+
+
+@pytest.mark.parametrize("M,N,K,large", [(2050, 2050, 700, False), (2177, 1925, 129, False), (4100, 4100, 300, True), (4351, 4225, 1001, True)])
+@pytest.mark.parametrize("tiles", [(1, 128), (128, 1)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_dense(mad, M, N, K, large, tiles, dtype):
+    import torch
+    print("case dense", M, N, K, tiles, dtype, flush=True)
+    A, B = matrix(mad, M, M, K, tiles[0]), matrix(mad, N, N, K, tiles[1])
+    out = torch.full((M, N + 7), 5.0, dtype=dtype_of(dtype), device="cuda")
+    mad.maddness_block_product(A, B, out=out[:, 3:N + 3])
+    assert tiles_of(mad.maddness_last_kernel()) == shape_of(dtype, large)
+    assert (out[:, :3] == 5).all() and (out[:, N + 3:] == 5).all()
+    check(out[:, 3:N + 3], factors(A), factors(B), f"{M} x {N} x {K}")
+
+
+@pytest.mark.parametrize("M,N,large", [(2050, 2050, False), (4100, 4100, True)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_nan_stays_in_its_row_and_column(mad, M, N, large, dtype):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w = torch.randn(M, 300, generator=g, device="cuda"), torch.randn(N, 300, generator=g, device="cuda")
+    x[M - 3, 299], w[N - 2, 17] = float("nan"), float("inf")
+    got = mad.maddness_block_product(mad.maddness_quantise_blocks(x), mad.maddness_quantise_blocks(w, 128), out_dtype=dtype_of(dtype)).isnan()
+    assert tiles_of(mad.maddness_last_kernel()) == shape_of(dtype, large)
+    want = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+    want[M - 3], want[:, N - 2] = True, True
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("counts,N,K,large", [([700, 0, 1290, 1, 130, 129], 600, 520, False), ([5003, 0, 7600], 1300, 200, True)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_by_rows(mad, counts, N, K, large, dtype):
+    import torch
+    print("case by rows", counts, N, K, dtype, flush=True)
+    E, off = len(counts), offsets_of(counts, 1)
+    S = int(off[-1]) + 9                                                   # rows that nobody has
+    A, W = matrix(mad, S, S, K, 1), experts(mad, E, E, N, K)
+    out = torch.full((S, N + 3), 7.0, dtype=dtype_of(dtype), device="cuda")
+    mad.maddness_block_product(A, W, torch.from_numpy(off).cuda(), out=out[:, 1:N + 1])
+    assert tiles_of(mad.maddness_last_kernel()) == shape_of(dtype, large) and "GATHER = false" in mad.maddness_last_kernel()
+    a = factors(A)
+    for e in range(E):
+        rows = slice(off[e], off[e + 1])
+        if counts[e]:
+            check(out[rows, 1:N + 1], tuple(v[rows] for v in a), factors(expert(W, e)), f"expert {e}")
+    assert (out[off[-1]:] == 7).all() and (out[:, 0] == 7).all() and (out[:, N + 1:] == 7).all()
+
+
+@pytest.mark.parametrize("T,counts,k,N,K", [(900, [700, 0, 1290, 1, 130, 129], 3, 600, 520), (3000, [0, 4000, 2100], 2, 520, 1001)])
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16", "e4m3"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_gathered_rows(mad, T, counts, k, N, K, kind, dtype):
+    import torch
+    print("case gathered", T, counts, k, kind, dtype, flush=True)
+    E, off = len(counts), offsets_of(counts, 4)
+    rng = np.random.default_rng(T)
+    S = int(off[-1]) + 3
+    source = rng.integers(-T // 10, T * k + T // 10, S).astype(np.int32)   # some rows have none, on either side
+    if kind == "e4m3":
+        A = x = matrix(mad, T, T, K, 1)
+    else:
+        x = matrix(mad, T, T, K, 1).values().to(dtype_of(kind))            # rounded within the call, to what they are
+        A = mad.maddness_quantise_blocks(x)
+    W = experts(mad, E, E, N, K)
+    out = torch.full((S, N), 7.0, dtype=dtype_of(dtype), device="cuda")
+    mad.maddness_block_product(x, W, torch.from_numpy(off).cuda(), source=torch.from_numpy(source).cuda(), repeat=k, out=out)
+    if kind == "e4m3":                                                     # (else the first kernel of the call is the rounding)
+        assert tiles_of(mad.maddness_last_kernel()) == (128, 128) and "GATHER = true" in mad.maddness_last_kernel()
+    a, written = factors(A), np.zeros(S, bool)
+    for e in range(E):
+        rows = np.arange(off[e], off[e + 1])
+        rows = rows[(source[rows] >= 0) & (source[rows] < T * k)]
+        written[rows] = True
+        if len(rows):
+            at = torch.from_numpy(source[rows] // k).cuda()
+            check(out[torch.from_numpy(rows).cuda()], tuple(v[at] for v in a), factors(expert(W, e)), f"expert {e}")
+    assert written.sum() > S // 2 and (out[torch.from_numpy(~written).cuda()] == 7).all()
+
+
+@pytest.mark.parametrize("counts,M,N,large", [([1024, 4224, 5, 0, 900], 700, 500, False), ([1152, 0, 6000, 300], 2100, 2100, True)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_by_depth(mad, counts, M, N, large, dtype):
+    import torch
+    print("case by depth", counts, M, N, dtype, flush=True)
+    off = offsets_of(counts, 128)
+    S = int(off[-1]) + 50
+    A, B = matrix(mad, M, M, S, 1), matrix(mad, N, N, S, 1)
+    got = mad.maddness_block_product(A, B, torch.from_numpy(off).cuda(), by="depth", out_dtype=dtype_of(dtype))
+    assert tiles_of(mad.maddness_last_kernel()) == shape_of(dtype, large)
+    a, b = factors(A), factors(B)
+    for e in range(len(counts)):
+        part = slice(off[e], off[e + 1])
+        if off[e + 1] > off[e]:
+            check(got[e], tuple(v[:, part] for v in a), tuple(v[:, part] for v in b), f"expert {e}")
+        else:
+            assert (got[e] == 0).all()
+
+
+def test_gradients_against_differences(mad):
+    """The loss sum(dY * (X W^T)) of the rounded dY is linear in X and in W: a difference along a direction is the gradient's sum with it, up to
+    the product's own rounding.  Along the gradient itself that difference is far larger than this, so one of zeros or of the other sign would not pass."""
+    import torch
+    for M, N, K in ((150, 70, 200), (2050, 600, 700)):
+        g = torch.Generator(device="cuda").manual_seed(M)
+        x, w, dy = (torch.randn(*s, generator=g, device="cuda") for s in ((M, K), (N, K), (M, N)))
+        W, Wt = mad.maddness_quantise_blocks(w, 128, both=True)
+        G, Gt = mad.maddness_quantise_blocks(dy, both=True)
+        Xt = mad.maddness_quantise_blocks(x, transposed=True)
+        dx = mad.maddness_block_product(G, Wt, out_dtype=torch.float32).double()
+        dw = mad.maddness_block_product(Gt, Xt, out_dtype=torch.float32).double()
+        v, u = G.values().double() @ W.values().double(), Gt.values().double() @ Xt.values().double().T
+        for got, along, rows, inner, loss in (
+                (dx, v, G.values().double(), W.values().double(), lambda t: (G.values().double() * ((x.double() + t * v) @ W.values().double().T)).sum()),
+                (dw, u, Gt.values().double(), Xt.values().double().T, lambda t: (Gt.values().double().T * (Xt.values().double().T @ (w.double() + t * u).T)).sum())):
+            difference = float(loss(0.5) - loss(-0.5))
+            tol = float(((rows.shape[1] + 9) * 2.0 ** -23 * (along.abs() * (rows.abs() @ inner.abs())).sum()))
+            assert abs(float((got * along).sum()) - difference) <= tol
+            assert abs(difference) > 2 * tol
