@@ -282,6 +282,8 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", so
     need = L.maddness_block_product_workspace(a_rows, K, how, a_dtype) if a_dtype != MADDNESS_E4M3 else 0
     if workspace is None and need:
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace is not None and not workspace.is_contiguous():              # (its size in bytes is then not what it has room for)
+        raise ValueError("workspace must be contiguous")
     _m._check(L.maddness_block_product(C.byref(a), C.byref(B._struct), how, groups, offsets_p, source_p, M, repeat, out.data_ptr(), _code(out, "out"), ldo,
                                        _m._ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(),
                                        _m._stream(None)))

@@ -544,7 +544,7 @@ PyObject *block_product(PyObject *, PyObject *const *a, Py_ssize_t n)
         size_t work_bytes = 0;
         if (a[9] != Py_None) {
             const at::Tensor &w = tensor(a[9]);
-            if (w.scalar_type() != at::kByte || w.device() != device) throw NotUsual();
+            if (w.scalar_type() != at::kByte || !w.is_contiguous() || w.device() != device) throw NotUsual();
             work_p = w.data_ptr();
             work_bytes = (size_t)w.numel();
         } else if ((work_bytes = maddness_block_product_workspace(A.rows, A.cols, by, A.dtype))) {

@@ -292,3 +292,14 @@ def test_gradients_against_differences(mad):
             tol = float(((rows.shape[1] + 9) * 2.0 ** -23 * (along.abs() * (rows.abs() @ inner.abs())).sum()))
             assert abs(float((got * along).sum()) - difference) <= tol
             assert abs(difference) > 2 * tol
+
+
+def test_a_workspace_with_gaps_or_of_one_byte_is_refused(mad):
+    """Its number of elements is not the room that there is."""
+    import torch
+    x, B = torch.ones(300, 512, device="cuda"), mad.maddness_quantise_blocks(torch.ones(40, 512, device="cuda"), 128)
+    need = mad.lib().maddness_block_product_workspace(300, 512, 0, mad.MADDNESS_F32)
+    for work in (torch.empty(1, dtype=torch.uint8, device="cuda").expand(need), torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError, match="contiguous"):
+            mad.maddness_block_product(x, B, workspace=work)
+    assert (mad.maddness_block_product(x, B, workspace=torch.empty(need, dtype=torch.uint8, device="cuda")) == 512).all()
