@@ -207,7 +207,8 @@ def maddness_quantise_blocks(x, tile: int = 1, transposed: bool = False, both: b
 
 
 def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", source=None, repeat: int = 1, out_dtype=None, out=None, workspace=None, stream=None):
-    """A @ B.T.  A: a BlockMatrix or a float tensor [M, K]; B: a BlockMatrix [N, K].
+    """A @ B.T.  A: a BlockMatrix or a float tensor [M, K]; B: a BlockMatrix [N, K].  Sums are fp32, rounded once to ``out_dtype`` (bfloat16); for
+    bfloat16 results of many rows the products of every eight neighbours are cut off at 2^-13 of the largest before, with float32 never.
 
     With ``offsets`` (int32 [experts + 1]) by experts: by="rows" multiplies rows offsets[e] .. offsets[e + 1] - 1 of A with B[e]
     (B [experts, N, K]) into out [M, N], rows that no expert has are left as they are; by="depth" gives out [experts, M, N] from the

@@ -113,11 +113,11 @@ __device__ __forceinline__ int64_t row_of_a(const ProductArgs &p, int64_t m)
 
 // Few rows: 16 MT rows by 16 NT columns to a workgroup; its wavefronts take every WAVES-th block of the sum, DEPTH of them asked for
 // at once, and add up in LDS, in their order.  B comes straight from memory, in pieces of 32 bytes to a lane, and so does an 8-bit A; a floating
-// A is rounded into LDS while the first of B is on its way.  Bound by the way of one piece: 1 x 4096 x 4096 6.7 us (16.8 MB, 2.5 TB/s),
-// 37 x 1000 x 510 8.1.
+// A is rounded into LDS while the first of B is on its way.  Bound by the way of one piece: 1 x 4096 x 4096 6.4 us (16.8 MB, 2.6 TB/s),
+// 37 x 1000 x 510 7.9.
 //
 // CHOICE: of the slots, those whose id is the workgroup's expert, found by going through all ids, 16 MT at a time; no order of them is needed.  The rows of
-// results are the slots themselves.  (24 slots of 64 experts of 1024 x 512: 10.0 us; 7.0 and a launch of 4.5 before it with an order.)
+// results are the slots themselves.  (24 slots of 64 experts of 1024 x 512: 8.4 us; the layer of it, with the choice and the sum, 16 us, 22 with an order.)
 template <int AT, int MT, int NT, int WAVES, int DEPTH, int OUT, bool CHOICE>
 __global__ __launch_bounds__(WAVES * 64) void product_few_kernel(ProductArgs p, uint32_t col_tiles)
 {
@@ -338,9 +338,10 @@ __device__ __forceinline__ f32x4 multiply(i32x8 b, i32x8 a, f32x4 c, int scale_b
 // exchanged by its index, so that the rows that a read of the lanes goes to fall on all banks.  WIDE: the 16-bit instruction.
 //
 // Eight wavefronts are two to a SIMD, and take turns: while one half of them reads its fragments of a block from LDS, the other half multiplies the ones
-// that it has read before.  With all eight reading and then all multiplying the matrix cores were busy 43% of the time (16384 x 4096 x 4096 to bfloat16:
-// 268 us; now 234 us, 2350 TFLOP/s, 0.9 of what the library's product of 8-bit matrices without exponents reaches).  What bounds it now is the way from L2 to LDS: 64 KiB
-// a block, of which one is under way at a time, take 1.0 of the 1.7 us.
+// that it has read before.  16384 x 4096 x 4096 to bfloat16: 268 us with all eight reading and then all multiplying, 229 to 250 in turns (the more the more
+// the operands change from call to call), 2200 to 2400 TFLOP/s, 0.9 of what the library's product of 8-bit matrices without exponents reaches; to binary16, by the
+// 16-bit instruction, 453.  The matrix cores are busy half of the time in either, by their counter; of a block's 1.8 us the rest goes to the way of 64 KiB from
+// L2 to LDS, of which one block is under way at a time.  (The first twenty calls after a pause take up to a quarter longer each, until the clocks are up.)
 template <int BM, int BN, int WM, int WN, bool WIDE, bool GATHER, int OUT>
 __global__ __launch_bounds__(WM * WN * 64, 2) void product_tiles_kernel(ProductArgs p, uint32_t col_tiles)
 {
@@ -616,7 +617,8 @@ int launch_to(const ProductArgs &p, int a_dtype, hipStream_t stream)
     const bool far = std::max(p.lda, p.ldb) > kMostStride || (p.source && p.a_rows * p.lda >= (int64_t)1 << 32);
     // Between the two by what they take, in microseconds, fitted to sizes from 300 x 300 x 300 to 1024 x 4096 x 4096: the few-rows kernel makes more workgroups of
     // a product, and so wins where the other leaves compute units without work (1024 x 512 x 512: 7.0 against 9.0, 128 x 4096 x 4096: 20 against 25,
-    // 256 x 4096 x 4096: 38 against 25).
+    // 256 x 4096 x 4096: 38 against 25).  Experts' rows count as their average, as only the device knows the rest: where one expert has all, the few-rows kernel
+    // takes no longer than with even shares (64 experts of 1024 x 1024, 2048 rows: 43 us and 60; 14 as a dense product), the other neither (12800 rows 38 and 40).
     const double blocks = (double)ceil_div(p.by == MADDNESS_BY_DEPTH ? ceil_div(p.K, groups) : p.K, (int64_t)kBlock);
     const double small = (double)(ceil_div(rows, (int64_t)64) * ceil_div(p.N, (int64_t)32) * groups), tiles = (double)(ceil_div(rows, (int64_t)128) * ceil_div(p.N, (int64_t)128) * groups);
     const double cus = device_info().cus, step = kWide<OUT> ? 0.85 : 0.6;

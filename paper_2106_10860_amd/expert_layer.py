@@ -58,9 +58,9 @@ class ExpertLayer:
 
     def by_choice(self, tokens: int) -> bool:
         """Whether the product finds an expert's slots by itself, without an order of them (a launch less): while an expert has 16 rows
-        or so, which it multiplies at a time.  64 experts of 1024 x 512, 6 to a token: 4 tokens 16.7 us, 22.6 with an order, 85 tokens 21.9 and 25.6;
-        8 of 4096 x 4096, 2 to a token: 64 tokens 59 and 68, 85 tokens 73 and 69.  Where all tokens choose the same experts it costs up to
-        half as much again (85 tokens of the first layer 37 and 26)."""
+        or so, which it multiplies at a time.  64 experts of 1024 x 512, 6 to a token: 4 tokens 16 us, 22 with an order, 85 tokens 22 and 25;
+        8 of 4096 x 4096, 2 to a token: 64 tokens 61 and 70, 85 tokens 73 and 68.  Where all tokens choose the same experts it costs up to
+        half as much again (85 tokens of the first layer 37 and 25)."""
         return tokens * self.k <= min(m.MAX_CHOSEN, 16 * self.experts)
 
     def forward(self, x, logits, training: bool = False):
