@@ -440,6 +440,7 @@ int maddness_order(const int32_t *ids, int64_t slots, int32_t E, int32_t align, 
 /*
  * out[t] = sum_j weights[t][j] y[place[t][j]], j = 0 .. k - 1 in this order, in fp32 and rounded once to out_dtype; a place outside
  * [0, rows) adds nothing.  y [rows][ldy] of y_dtype, place [T][k] or NULL (t k + j, rows >= T k), weights [T][k] fp32 or NULL (1), out [T][ldo]; F32, F16 or BF16.
+ * A y that is infinite or NaN makes the sum NaN also where its weight is 0: results that may pass y_dtype's range are kept in F32.
  * maddness_combine_gradient: weights_gradient[t][j] = sum_n gradient[t][n] y[place[t][j]][n], 0 without a place.  (The
  * gradient of y is the gradient's rows times the weights: source and factors of maddness_quantise_blocks.)
  */
