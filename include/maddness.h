@@ -451,6 +451,114 @@ int maddness_combine_gradient(const void *gradient, int32_t dtype, int64_t ldg, 
                               float *weights_gradient, void *stream);
 
 /*
+ * The exact product in 8-bit integers, and what stands around exact layers and layers of experts: the layer norm before them, the
+ * balance of the experts' tokens, the norm of a training step's gradients.
+ *
+ * An integer matrix is [rows][cols] of signed 8-bit values with one fp32 scale for each row (a token of activations, an output
+ * channel of weights): the value at data[r ld + c] stands for it times scale[r].
+ *   data   16-byte aligned, ld a multiple of 16; what lies between cols and ld does not matter.
+ *   scale  4-byte aligned, [rows].
+ */
+typedef enum { MADDNESS_I8 = 17 } maddness_integer_dtype;
+#define MADDNESS_MAX_INTEGER_DEPTH 131071    /* 2^14 times that still fits the 32-bit sums */
+
+typedef struct {
+    const void *data;
+    int32_t dtype;        /* MADDNESS_I8 (or MADDNESS_F32 / F16 / BF16 where the call says so) */
+    int64_t rows, cols, ld;
+    const float *scale;
+} maddness_integer_matrix;
+
+/*
+ * x [rows][ldx] of `dtype` (F32, F16 or BF16) to an integer matrix: for every row t = its largest |x|, scale = t / 127 rounded to fp32, but at
+ * least 2^-126, and 1 where t = 0; q = x / scale rounded to the nearest integer, ties to even (the quotient itself, not one rounded before).  So
+ * |q| <= 127.  A row with a NaN or an infinity has the scale NaN and q = 0: what is computed of it is NaN.
+ * q [rows][ldq]; bytes from cols up to the next multiple of 16 are set to 0.
+ */
+int maddness_quantise_rows(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t *q, int64_t ldq, float *scale,
+                           void *stream);
+
+/*
+ * out[m][n] = ((float)S A.scale[m]) B.scale[n] + bias[n], S = sum_k A[m][k] B[n][k]: S is exact (32-bit integers), its conversion, the two
+ * products and the sum are rounded to fp32, and the result to out_dtype (F32, F16 or BF16).  It does not depend on anything but the row and the
+ * column.
+ * A       MADDNESS_I8, or F32 / F16 / BF16: then its rows are rounded as maddness_quantise_rows does; data aligned to its element, scale ignored.
+ * B       MADDNESS_I8.
+ * bias    NULL (nothing is added), or [N] fp32.
+ * workspace  maddness_integer_product_workspace(A's rows, K, dtype of A) bytes, 16-byte aligned (NULL where that is 0); contents undefined
+ *         afterwards.
+ * M = 0 and N = 0 are valid; K = 0 gives the bias or zeros; K <= MADDNESS_MAX_INTEGER_DEPTH; M, N < 2^31.
+ */
+size_t maddness_integer_product_workspace(int64_t a_rows, int64_t K, int32_t a_dtype);
+int maddness_integer_product(const maddness_integer_matrix *A, const maddness_integer_matrix *B, const float *bias, void *out, int32_t out_dtype,
+                             int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The layer norm of every row: mu = mean(x), v = mean((x - mu)^2), r = 1 / sqrt(v + eps), y = (x - mu) r weight + bias; all in fp32, the
+ * variance of the centred values.
+ * x       [rows][ldx] of `dtype`; weight, bias [cols] of parameter_dtype, or NULL (1 and 0).  Types: F32, F16 or BF16.
+ * out     [rows][ldo] of out_dtype: y rounded once, scale NULL.  Or MADDNESS_I8: y as an integer matrix with `scale` [rows], as
+ *         maddness_quantise_rows makes of the fp32 y.
+ * mean, rstd  [rows] fp32, mu and r, or both NULL.
+ * cols >= 1; eps >= 0 and finite.
+ *
+ * maddness_layer_norm_gradient: from the gradient g of y, with h = (x - mu) r and u = g weight:
+ *   dx = r (u - mean(u) - h mean(u h)), rounded to x's dtype;  dweight[c] = sum over rows of g h, dbias[c] = sum over rows of g, in fp32 in an order that
+ *   depends on the sizes only.
+ * gradient [rows][ldg] of gradient_dtype.  mean and rstd of the call before.  dx [rows][ldd], or NULL.  dweight and dbias [cols], or both NULL.
+ * Without rows dweight and dbias are 0.
+ * workspace  maddness_layer_norm_gradient_workspace(rows, cols) bytes, 16-byte aligned; not needed (NULL) without dweight and dbias.
+ */
+int maddness_layer_norm(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ldx, const void *weight, const void *bias,
+                        int32_t parameter_dtype, float eps, void *out, int32_t out_dtype, int64_t ldo, float *scale, float *mean, float *rstd,
+                        void *stream);
+size_t maddness_layer_norm_gradient_workspace(int64_t rows, int64_t cols);
+int maddness_layer_norm_gradient(const void *gradient, int32_t gradient_dtype, int64_t ldg, const void *x, int32_t dtype, int64_t rows,
+                                 int64_t cols, int64_t ldx, const float *mean, const float *rstd, const void *weight, int32_t parameter_dtype,
+                                 void *dx, int64_t ldd, float *dweight, float *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * How evenly the tokens fall on the experts.  s are the scores that maddness_route makes of the logits (0 for a masked one), p[t][e] = s[t][e] /
+ * sum_f s[t][f]; a token whose scores are all 0 (padding) counts nowhere.
+ *   counts[e] = how many of `ids` [T][k] are e (those outside [0, E) are none);  n = their sum, L = the tokens that count
+ *   push[e]   = factor E counts[e] / (n L), 0 where n or L is 0
+ *   loss      = sum_e push[e] sum_t p[t][e]: factor where all experts have the same, more the less evenly they have
+ * Sums over tokens are fp32 in an order that depends on the sizes only, and fp64 where those meet.  push is what the gradient takes: the counts have none.
+ * workspace  maddness_balance_workspace(T, E) bytes, 8-byte aligned.
+ *
+ * maddness_balance_gradient: gradient[t][e] of logits [T][ldl], times loss_gradient[0] (NULL: 1), plus add[t][e] ([T][lda] of `dtype`, or NULL;
+ * it may be `gradient` itself): in fp32, rounded once to `dtype`.  0 (plus add) for a masked logit.
+ *   softmax: p[t][e] (push[e] - sum_f p[t][f] push[f]);  sigmoid: the same times 1 - s[t][e]
+ */
+size_t maddness_balance_workspace(int64_t T, int32_t E);
+int maddness_balance(const void *logits, int32_t dtype, int64_t T, int32_t E, int64_t ldl, int32_t scores, const int32_t *ids, int32_t k,
+                     float factor, float *loss, int32_t *counts, float *push, void *workspace, size_t workspace_bytes, void *stream);
+int maddness_balance_gradient(const void *logits, int32_t dtype, int64_t T, int32_t E, int64_t ldl, int32_t scores, const float *push,
+                              const float *loss_gradient, const void *add, int64_t lda, void *gradient, int64_t ldd, void *stream);
+
+/*
+ * The norm over many tensors of any of the types F32, F16 and BF16: norm[0] = sqrt(sum of squares), summed in fp64 and rounded to fp32 once.
+ * `tensors` is a HOST array of n of them, read before the call returns; data and out are device pointers to `count` elements without gaps.
+ *
+ * maddness_clip_gradients: every tensor's out = data times min(1, max_norm / norm[0]), in fp32, rounded to out_dtype; out may be data itself where
+ * the types agree (then nothing is written where the factor is 1), and otherwise overlaps no data or out.  A norm that is not finite leaves the factor 1: the caller sees
+ * it in norm.  max_norm >= 0 (infinity: the factor is 1).  Where norm_given is 0 the norm is that of these tensors, and written to norm; else norm
+ * is read (a norm over the tensors of several processes).
+ * workspace  maddness_gradient_norm_workspace() bytes, 8-byte aligned (NULL where norm_given).
+ */
+typedef struct {
+    const void *data;
+    void *out;            /* not used by maddness_gradient_norm */
+    int64_t count;
+    int32_t dtype, out_dtype;
+} maddness_tensor;
+
+size_t maddness_gradient_norm_workspace(void);
+int maddness_gradient_norm(const maddness_tensor *tensors, int64_t n, float *norm, void *workspace, size_t workspace_bytes, void *stream);
+int maddness_clip_gradients(const maddness_tensor *tensors, int64_t n, float max_norm, float *norm, int32_t norm_given, void *workspace,
+                            size_t workspace_bytes, void *stream);
+
+/*
  * Process-wide switches for tests and measurements (Section 4.4 describes f as table
  * lookups and integer additions; MADDNESS_OPT_KERNELS = 1 keeps the library to kernels
  * of exactly that form).  Normal use needs none of them: every switch starts at 0, "the

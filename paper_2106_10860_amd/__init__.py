@@ -50,6 +50,18 @@ EXPORTS = (
     "maddness_order",
     "maddness_combine",
     "maddness_combine_gradient",
+    "maddness_quantise_rows",
+    "maddness_integer_product_workspace",
+    "maddness_integer_product",
+    "maddness_layer_norm",
+    "maddness_layer_norm_gradient_workspace",
+    "maddness_layer_norm_gradient",
+    "maddness_balance_workspace",
+    "maddness_balance",
+    "maddness_balance_gradient",
+    "maddness_gradient_norm_workspace",
+    "maddness_gradient_norm",
+    "maddness_clip_gradients",
     "maddness_set_option",
     "maddness_get_option",
     "maddness_last_error",
@@ -71,6 +83,14 @@ class _Params(C.Structure):
 class _BlockMatrix(C.Structure):
     _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("tile", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
                 ("ld", C.c_int64), ("stride", C.c_int64), ("scale", C.c_void_p), ("lds", C.c_int64), ("scale_stride", C.c_int64)]
+
+
+class _IntegerMatrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("scale", C.c_void_p)]
+
+
+class _Tensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32), ("out_dtype", C.c_int32)]
 
 
 _lib = None
@@ -120,6 +140,22 @@ def lib() -> C.CDLL:
         L.maddness_order.argtypes = [vp, i64, i32, i32, vp, vp, vp, i64, vp, vp, sz, vp]
         L.maddness_combine.argtypes = [vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, i32, i64, vp]
         L.maddness_combine_gradient.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, vp, i64, i32, vp, vp]
+        L.maddness_quantise_rows.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, vp]
+        L.maddness_integer_product_workspace.argtypes = [i64, i64, i32]
+        L.maddness_integer_product_workspace.restype = sz
+        L.maddness_integer_product.argtypes = [C.POINTER(_IntegerMatrix), C.POINTER(_IntegerMatrix), vp, vp, i32, i64, vp, sz, vp]
+        L.maddness_layer_norm.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, C.c_float, vp, i32, i64, vp, vp, vp, vp]
+        L.maddness_layer_norm_gradient_workspace.argtypes = [i64, i64]
+        L.maddness_layer_norm_gradient_workspace.restype = sz
+        L.maddness_layer_norm_gradient.argtypes = [vp, i32, i64, vp, i32, i64, i64, i64, vp, vp, vp, i32, vp, i64, vp, vp, vp, sz, vp]
+        L.maddness_balance_workspace.argtypes = [i64, i32]
+        L.maddness_balance_workspace.restype = sz
+        L.maddness_balance.argtypes = [vp, i32, i64, i32, i64, i32, vp, i32, C.c_float, vp, vp, vp, vp, sz, vp]
+        L.maddness_balance_gradient.argtypes = [vp, i32, i64, i32, i64, i32, vp, vp, vp, i64, vp, i64, vp]
+        L.maddness_gradient_norm_workspace.argtypes = []
+        L.maddness_gradient_norm_workspace.restype = sz
+        L.maddness_gradient_norm.argtypes = [C.POINTER(_Tensor), i64, vp, vp, sz, vp]
+        L.maddness_clip_gradients.argtypes = [C.POINTER(_Tensor), i64, C.c_float, vp, i32, vp, sz, vp]
         L.maddness_set_option.argtypes = [i32, i32]
         L.maddness_get_option.argtypes = [i32]
         L.maddness_get_option.restype = i32
@@ -147,6 +183,7 @@ class _NotBuilt:
 
     encode = scan = build_luts = encode_scan
     quantise_blocks = block_product = route = route_gradient = order = combine = combine_gradient = encode_scan
+    quantise_rows = integer_product = layer_norm = layer_norm_gradient = balance = balance_gradient = clip_gradients = encode_scan
 
 
 class _NotLoaded:
@@ -545,4 +582,17 @@ from .blocks import (  # noqa: E402
     maddness_quantise_blocks,
     maddness_route,
     maddness_route_gradient,
+)
+
+# What stands around exact layers: 8-bit integers, the layer norm, the balance of experts, the gradients' norm.
+from .layers import (  # noqa: E402
+    IntegerMatrix,
+    maddness_balance,
+    maddness_balance_gradient,
+    maddness_clip_gradients,
+    maddness_gradient_norm,
+    maddness_integer_product,
+    maddness_layer_norm,
+    maddness_layer_norm_gradient,
+    maddness_quantise_rows,
 )

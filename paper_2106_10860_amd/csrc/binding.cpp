@@ -15,6 +15,7 @@
 
 #include <cstdio>
 #include <cstring>
+#include <vector>
 
 #include "maddness.h"
 
@@ -706,6 +707,374 @@ PyObject *combine_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---------------------------------------------------------------- 8-bit integers, layer norm, balance of experts, gradients' norm
+
+// The current stream of the current device, which has to be the tensors' one.
+void *stream_on(const at::Device &device)
+{
+    Ref current(PyObject_CallNoArgs(get_device));
+    if (whole(current.p) != device.index()) throw NotUsual();
+    Ref raw(PyObject_CallOneArg(get_stream, current.p));
+    return reinterpret_cast<void *>(whole(raw.p));
+}
+
+float real(PyObject *o)
+{
+    if (!PyFloat_CheckExact(o)) throw NotUsual();
+    return (float)PyFloat_AS_DOUBLE(o);
+}
+
+template <typename... T>
+PyObject *tuple_of(const T &...t)
+{
+    PyObject *tuple = PyTuple_New(sizeof...(T));
+    Py_ssize_t at = 0;
+    (PyTuple_SET_ITEM(tuple, at++, THPVariable_Wrap(t)), ...);
+    return tuple;
+}
+
+// An IntegerMatrix, as its constructor checked it.
+maddness_integer_matrix integer_matrix(PyObject *o, const at::Device *device, at::Device *own)
+{
+    Ref q_ref(PyObject_GetAttr(o, s_q)), scale_ref(PyObject_GetAttr(o, s_scale));
+    const at::Tensor &q = tensor(q_ref.p), &scale = tensor(scale_ref.p);
+    if (q.dim() != 2 || q.scalar_type() != at::kChar || (device && q.device() != *device)) throw NotUsual();
+    maddness_integer_matrix m{};
+    m.data = q.data_ptr();
+    m.dtype = MADDNESS_I8;
+    m.rows = q.size(0);
+    m.cols = q.size(1);
+    m.ld = m.rows > 1 ? q.stride(0) : up(std::max(m.cols, q.stride(0)), 16);
+    m.scale = static_cast<const float *>(scale.data_ptr());
+    if (own) *own = q.device();
+    return m;
+}
+
+struct NewIntegers {
+    at::Tensor q, scale;
+    int64_t ld;
+};
+
+NewIntegers new_integers(int64_t rows, int64_t cols, const at::Device &device)
+{
+    NewIntegers b;
+    b.ld = up(cols, 16);
+    b.q = at::empty({rows, b.ld}, at::TensorOptions().dtype(at::kChar).device(device));
+    b.scale = at::empty({rows}, at::TensorOptions().dtype(at::kFloat).device(device));
+    if (b.ld != cols) b.q = b.q.narrow(1, 0, cols);
+    return b;
+}
+
+// (x) -> (q, scale)
+PyObject *quantise_rows(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 1) throw NotUsual();
+        const at::Tensor &x = plain(a[0]);
+        const int code = float_code(x.scalar_type());
+        const Rows r = rows_of(x);
+        void *stream = stream_on(x.device());
+        const NewIntegers out = new_integers(r.rows, r.cols, x.device());
+        const void *x_p = x.data_ptr();
+        int8_t *q = static_cast<int8_t *>(out.q.data_ptr());
+        float *scale = static_cast<float *>(out.scale.data_ptr());
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_quantise_rows(x_p, code, r.rows, r.cols, r.ld, q, out.ld, scale, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        return tuple_of(out.q, out.scale);
+    });
+}
+
+// (a_is_integers, A, B, bias, out_dtype, out, workspace) -> out
+PyObject *integer_product(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 7) throw NotUsual();
+        at::Device device(at::kCPU);
+        maddness_integer_matrix A{};
+        if (truth(a[0])) {
+            A = integer_matrix(a[1], nullptr, &device);
+        } else {
+            const at::Tensor &x = plain(a[1]);
+            const Rows r = rows_of(x);
+            A.data = x.data_ptr();
+            A.dtype = float_code(x.scalar_type());
+            A.rows = r.rows;
+            A.cols = r.cols;
+            A.ld = r.ld;
+            device = x.device();
+        }
+        const maddness_integer_matrix B = integer_matrix(a[2], &device, nullptr);
+        if (A.cols != B.cols) throw NotUsual();
+        const float *bias = flat_or_null<const float>(a[3], at::kFloat, {B.rows}, device);
+        const at::ScalarType type = dtype_or(a[4], at::kBFloat16);
+        void *stream = stream_on(device);
+        at::Tensor made, work;
+        void *out;
+        int64_t ldo;
+        int code;
+        if (a[5] == Py_None) {
+            code = float_code(type);
+            made = at::empty({A.rows, B.rows}, at::TensorOptions().dtype(type).device(device));
+            out = made.data_ptr();
+            ldo = B.rows;
+        } else {
+            const at::Tensor &o = plain(a[5]);
+            if (o.device() != device || (a[4] != Py_None && o.scalar_type() != type)) throw NotUsual();
+            const Rows r = rows_of(o);
+            if (r.rows != A.rows || r.cols != B.rows) throw NotUsual();
+            code = float_code(o.scalar_type());
+            out = o.data_ptr();
+            ldo = r.ld;
+        }
+        void *work_p = nullptr;
+        size_t work_bytes = 0;
+        if (a[6] != Py_None) {
+            const at::Tensor &w = tensor(a[6]);
+            if (w.scalar_type() != at::kByte || !w.is_contiguous() || w.device() != device) throw NotUsual();
+            work_p = w.data_ptr();
+            work_bytes = (size_t)w.numel();
+        } else if ((work_bytes = maddness_integer_product_workspace(A.rows, A.cols, A.dtype))) {
+            work = at::empty({(int64_t)work_bytes}, at::TensorOptions().dtype(at::kByte).device(device));
+            work_p = work.data_ptr();
+        }
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_integer_product(&A, &B, bias, out, code, ldo, work_p, work_bytes, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        if (made.defined()) return THPVariable_Wrap(std::move(made));
+        Py_INCREF(a[5]);
+        return a[5];
+    });
+}
+
+// A norm's weight or bias (or nullptr); its type has to be that of the other one.
+const void *parameter(PyObject *o, int64_t cols, const at::Device &device, int *code)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = plain(o);
+    const int c = float_code(t.scalar_type());
+    if (t.dim() != 1 || t.size(0) != cols || !t.is_contiguous() || t.device() != device || (*code >= 0 && c != *code)) throw NotUsual();
+    *code = c;
+    return t.data_ptr();
+}
+
+// (x, weight, bias, eps, training, integer, out_dtype, out) -> out, or (out [or q, scale], mean, rstd), or (q, scale)
+PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 8 || a[7] != Py_None) throw NotUsual();
+        const at::Tensor &x = plain(a[0]);
+        const int code = float_code(x.scalar_type());
+        const Rows r = rows_of(x);
+        int parameters = -1;
+        const void *weight = parameter(a[1], r.cols, x.device(), &parameters), *bias = parameter(a[2], r.cols, x.device(), &parameters);
+        const float eps = real(a[3]);
+        const bool training = truth(a[4]), integer = truth(a[5]);
+        const at::ScalarType type = dtype_or(a[6], x.scalar_type());
+        void *stream = stream_on(x.device());
+        const auto floats = at::TensorOptions().dtype(at::kFloat).device(x.device());
+        at::Tensor y, mean, rstd;
+        NewIntegers q;
+        if (integer) q = new_integers(r.rows, r.cols, x.device());
+        else y = at::empty({r.rows, r.cols}, x.options().dtype(type));
+        const int out_code = integer ? (int)MADDNESS_I8 : float_code(type);
+        if (training) {
+            mean = at::empty({r.rows}, floats);
+            rstd = at::empty({r.rows}, floats);
+        }
+        const void *x_p = x.data_ptr();
+        void *out = integer ? q.q.data_ptr() : y.data_ptr();
+        const int64_t ldo = integer ? q.ld : r.cols;
+        float *scale = integer ? static_cast<float *>(q.scale.data_ptr()) : nullptr;
+        float *mean_p = training ? static_cast<float *>(mean.data_ptr()) : nullptr, *rstd_p = training ? static_cast<float *>(rstd.data_ptr()) : nullptr;
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_layer_norm(x_p, code, r.rows, r.cols, r.ld, weight, bias, std::max(parameters, 0), eps, out, out_code, ldo, scale, mean_p, rstd_p, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        if (integer) return training ? tuple_of(q.q, q.scale, mean, rstd) : tuple_of(q.q, q.scale);
+        return training ? tuple_of(y, mean, rstd) : THPVariable_Wrap(std::move(y));
+    });
+}
+
+// (gradient, x, mean, rstd, weight, parameters) -> (dx, dweight, dbias)
+PyObject *layer_norm_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 6) throw NotUsual();
+        const at::Tensor &g = plain(a[0]), &x = plain(a[1]);
+        const int g_code = float_code(g.scalar_type()), code = float_code(x.scalar_type());
+        const Rows rg = rows_of(g), r = rows_of(x);
+        if (rg.rows != r.rows || rg.cols != r.cols || g.device() != x.device()) throw NotUsual();
+        const float *mean = static_cast<const float *>(flat(a[2], at::kFloat, {r.rows}, x.device()).data_ptr());
+        const float *rstd = static_cast<const float *>(flat(a[3], at::kFloat, {r.rows}, x.device()).data_ptr());
+        int parameter_code = -1;
+        const void *weight = parameter(a[4], r.cols, x.device(), &parameter_code);
+        const bool parameters = truth(a[5]);
+        void *stream = stream_on(x.device());
+        const auto floats = at::TensorOptions().dtype(at::kFloat).device(x.device());
+        at::Tensor dx = at::empty({r.rows, r.cols}, x.options()), dweight, dbias, work;
+        size_t bytes = 0;
+        if (parameters) {
+            dweight = at::empty({r.cols}, floats);
+            dbias = at::empty({r.cols}, floats);
+            bytes = maddness_layer_norm_gradient_workspace(r.rows, r.cols);
+            work = at::empty({(int64_t)bytes}, floats.dtype(at::kByte));
+        }
+        const void *g_p = g.data_ptr(), *x_p = x.data_ptr();
+        void *dx_p = dx.data_ptr(), *work_p = parameters ? work.data_ptr() : nullptr;
+        float *dweight_p = parameters ? static_cast<float *>(dweight.data_ptr()) : nullptr, *dbias_p = parameters ? static_cast<float *>(dbias.data_ptr()) : nullptr;
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_layer_norm_gradient(g_p, g_code, rg.ld, x_p, code, r.rows, r.cols, r.ld, mean, rstd, weight, std::max(parameter_code, 0), dx_p, r.cols,
+                                          dweight_p, dbias_p, work_p, bytes, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        if (parameters) return tuple_of(dx, dweight, dbias);
+        PyObject *tuple = PyTuple_New(3);
+        PyTuple_SET_ITEM(tuple, 0, THPVariable_Wrap(std::move(dx)));
+        for (int i = 1; i < 3; ++i) {
+            Py_INCREF(Py_None);
+            PyTuple_SET_ITEM(tuple, i, Py_None);
+        }
+        return tuple;
+    });
+}
+
+// (logits, ids, sigmoid, factor) -> (loss, counts, push)
+PyObject *balance(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 4) throw NotUsual();
+        const at::Tensor &x = plain(a[0]), &ids = tensor(a[1]);
+        const int code = float_code(x.scalar_type());
+        const Rows r = rows_of(x);
+        if (ids.dim() != 2 || r.cols < 1 || r.cols > MADDNESS_MAX_EXPERTS) throw NotUsual();
+        const int32_t k = narrow(ids.size(1)), E = (int32_t)r.cols;
+        if (k < 1) throw NotUsual();
+        const int32_t *ids_p = flat_or_null<const int32_t>(a[1], at::kInt, {r.rows, k}, x.device());
+        const bool sigmoid = truth(a[2]);
+        const float factor = real(a[3]);
+        void *stream = stream_on(x.device());
+        const auto floats = at::TensorOptions().dtype(at::kFloat).device(x.device());
+        const size_t bytes = maddness_balance_workspace(r.rows, E);
+        at::Tensor loss = at::empty({}, floats), counts = at::empty({E}, floats.dtype(at::kInt)), push = at::empty({E}, floats);
+        at::Tensor work = at::empty({(int64_t)bytes}, floats.dtype(at::kByte));
+        const void *x_p = x.data_ptr();
+        float *loss_p = static_cast<float *>(loss.data_ptr()), *push_p = static_cast<float *>(push.data_ptr());
+        int32_t *counts_p = static_cast<int32_t *>(counts.data_ptr());
+        void *work_p = work.data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_balance(x_p, code, r.rows, E, r.ld, sigmoid ? MADDNESS_SIGMOID : MADDNESS_SOFTMAX, ids_p, k, factor, loss_p, counts_p, push_p, work_p,
+                              bytes, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        return tuple_of(loss, counts, push);
+    });
+}
+
+// (logits, push, sigmoid, loss_gradient, add, out) -> gradient
+PyObject *balance_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 6) throw NotUsual();
+        const at::Tensor &x = plain(a[0]);
+        const int code = float_code(x.scalar_type());
+        const Rows r = rows_of(x);
+        if (r.cols < 1 || r.cols > MADDNESS_MAX_EXPERTS) throw NotUsual();
+        const float *push = static_cast<const float *>(flat(a[1], at::kFloat, {r.cols}, x.device()).data_ptr());
+        const bool sigmoid = truth(a[2]);
+        const float *times = nullptr;
+        if (a[3] != Py_None) {
+            const at::Tensor &t = plain(a[3]);
+            if (t.scalar_type() != at::kFloat || t.numel() != 1 || t.device() != x.device()) throw NotUsual();
+            times = static_cast<const float *>(t.data_ptr());
+        }
+        auto like = [&](PyObject *o, int64_t *ld) -> void * {
+            const at::Tensor &t = plain(o);
+            const Rows rt = rows_of(t);
+            if (t.scalar_type() != x.scalar_type() || rt.rows != r.rows || rt.cols != r.cols || t.device() != x.device()) throw NotUsual();
+            *ld = rt.ld;
+            return t.data_ptr();
+        };
+        int64_t lda = 0, ldd = r.cols;
+        const void *add = a[4] == Py_None ? nullptr : like(a[4], &lda);
+        at::Tensor made;
+        void *out, *stream = stream_on(x.device());
+        if (a[5] == Py_None) {
+            made = at::empty({r.rows, r.cols}, x.options());
+            out = made.data_ptr();
+        } else {
+            out = like(a[5], &ldd);
+        }
+        const void *x_p = x.data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = maddness_balance_gradient(x_p, code, r.rows, (int32_t)r.cols, r.ld, sigmoid ? MADDNESS_SIGMOID : MADDNESS_SOFTMAX, push, times, add, lda, out, ldd, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        if (made.defined()) return THPVariable_Wrap(std::move(made));
+        Py_INCREF(a[5]);
+        return a[5];
+    });
+}
+
+// (tensors, max_norm or None, norm, out) -> norm: scales the tensors where there is a max_norm
+PyObject *clip_gradients(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return usual([&]() -> PyObject * {
+        if (n != 4 || !PyList_CheckExact(a[0]) || (a[3] != Py_None && !PyList_CheckExact(a[3]))) throw NotUsual();
+        const Py_ssize_t count = PyList_GET_SIZE(a[0]);
+        if (count == 0 || (a[3] != Py_None && PyList_GET_SIZE(a[3]) != count)) throw NotUsual();
+        const bool scales = a[1] != Py_None;
+        const float max_norm = scales ? real(a[1]) : 0.0f;
+        std::vector<maddness_tensor> table((size_t)count);
+        const at::Device device = tensor(PyList_GET_ITEM(a[0], 0)).device();
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            const at::Tensor &t = plain(PyList_GET_ITEM(a[0], i));
+            if (t.device() != device || !t.is_non_overlapping_and_dense()) throw NotUsual();
+            maddness_tensor &to = table[(size_t)i];
+            to.data = to.out = t.data_ptr();
+            to.count = t.numel();
+            to.dtype = to.out_dtype = float_code(t.scalar_type());
+            if (!scales || a[3] == Py_None) continue;
+            const at::Tensor &o = plain(PyList_GET_ITEM(a[3], i));
+            if (o.device() != device || o.sizes() != t.sizes() || o.strides() != t.strides()) throw NotUsual();
+            to.out = o.data_ptr();
+            to.out_dtype = float_code(o.scalar_type());
+        }
+        void *stream = stream_on(device);
+        at::Tensor norm, work;
+        const auto floats = at::TensorOptions().dtype(at::kFloat).device(device);
+        const bool given = a[2] != Py_None;
+        size_t bytes = 0;
+        if (given) {
+            norm = plain(a[2]);
+            if (norm.scalar_type() != at::kFloat || norm.numel() != 1 || norm.device() != device) throw NotUsual();
+        } else {
+            norm = at::empty({}, floats);
+            bytes = maddness_gradient_norm_workspace();
+            work = at::empty({(int64_t)bytes}, floats.dtype(at::kByte));
+        }
+        float *norm_p = static_cast<float *>(norm.data_ptr());
+        void *work_p = given ? nullptr : work.data_ptr();
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = scales ? maddness_clip_gradients(table.data(), count, max_norm, norm_p, given, work_p, bytes, stream)
+                    : maddness_gradient_norm(table.data(), count, norm_p, work_p, bytes, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != MADDNESS_OK) return int_status(rc);
+        if (!given) return THPVariable_Wrap(std::move(norm));
+        Py_INCREF(a[2]);
+        return a[2];
+    });
+}
+
 // Tensors are read by the layout of the torch, and objects by that of the Python, that this was built with: with others it is an
 // ImportError, also where every symbol is found.
 bool built_for_these()
@@ -736,6 +1105,13 @@ PyMethodDef methods[] = {
     {"order", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(order)), METH_FASTCALL, nullptr},
     {"combine", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(combine)), METH_FASTCALL, nullptr},
     {"combine_gradient", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(combine_gradient)), METH_FASTCALL, nullptr},
+    {"quantise_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(quantise_rows)), METH_FASTCALL, nullptr},
+    {"integer_product", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(integer_product)), METH_FASTCALL, nullptr},
+    {"layer_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(layer_norm)), METH_FASTCALL, nullptr},
+    {"layer_norm_gradient", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(layer_norm_gradient)), METH_FASTCALL, nullptr},
+    {"balance", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(balance)), METH_FASTCALL, nullptr},
+    {"balance_gradient", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(balance_gradient)), METH_FASTCALL, nullptr},
+    {"clip_gradients", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(clip_gradients)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -1,0 +1,349 @@
+// out[m][n] = A.scale[m] B.scale[n] sum_k A[m][k] B[n][k] + bias[n] of two matrices of 8-bit integers, on the integer matrix cores.
+//
+// The instruction (v_mfma_i32_16x16x64_i8) adds exactly in 32 bits, so results depend on no split of the sum; the scales come in once, at the end.
+// B's rows (the columns of out) are its first operand and A's rows its second, so that a lane's four results are four neighbours in a row of out.
+// Lane l holds 16 values of row l % 16 of an operand (which 16 of the 64 does not matter as long as they are the same ones of both operands), and results
+// n = 4 (l / 16) + i of row m = l % 16.
+#include "layers_common.h"
+#include "tile_loads.h"
+
+namespace maddness {
+namespace {
+
+// A lane's 32 bytes of a row's 128, at group * 32.
+struct Piece {
+    i32x4 lo, hi;
+};
+
+// Reads them, 16 bytes that begin at or beyond column K from the row's last 16 that do not: in bounds, and cut off of one operand.
+__device__ __forceinline__ Piece load_piece(const int8_t *row, int64_t kb, int group, int64_t K)
+{
+    const int64_t k = kb * kBlock + group * 32, last = (K - 1) & ~(int64_t)15;
+    return Piece{*reinterpret_cast<const i32x4 *>(row + min(k, last)), *reinterpret_cast<const i32x4 *>(row + min(k + 16, last))};
+}
+
+__device__ __forceinline__ i32x4 multiply(i32x4 b, i32x4 a, i32x4 c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(b, a, c, 0, 0, 0); }
+
+__device__ __forceinline__ float scaled(int32_t sum, float scale_a, float scale_b, const float *bias, int64_t n)
+{
+    const float v = (float)sum * scale_a * scale_b;
+    return bias ? v + bias[n] : v;
+}
+
+// Whether A's rows are rounded within the few-rows kernel, by every workgroup for itself: while they fill 32 KiB of LDS at most.
+constexpr int64_t kInside = 32768, kInsideRows = 64;
+
+// Few rows: 16 MT rows by 16 NT columns to a workgroup; its wavefronts take every WAVES-th block of 128 of the sum, DEPTH of them asked for
+// at once, and add up in LDS.  B comes straight from memory, in pieces of 32 bytes to a lane, and so does an 8-bit A; a floating A is rounded into
+// LDS while the first of B is on its way.
+template <int AT, int MT, int NT, int WAVES, int DEPTH, int OUT>
+__global__ __launch_bounds__(WAVES * 64) void integer_few_kernel(IntegerArgs p, uint32_t col_tiles)
+{
+    constexpr bool ROUND = AT != kI8;
+    __shared__ i32x4 sums[WAVES][MT * NT][64];
+    __shared__ __attribute__((aligned(16))) int8_t rounded[ROUND ? kInside + kInsideRows * 16 : 16];
+    __shared__ uint32_t tops[kInsideRows];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, r16 = lane % 16, g = lane / 16;
+    const int64_t n0 = (int64_t)(blockIdx.x % col_tiles) * (16 * NT), first = (int64_t)(blockIdx.x / col_tiles) * (16 * MT), last = min(first + 16 * MT, p.M);
+    const int64_t blocks = ceil_div(p.K, (int64_t)kBlock);
+    const int8_t *row_b[NT], *row_a[MT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) row_b[t] = p.b + min(n0 + t * 16 + r16, p.N - 1) * p.ldb;
+    Piece b[DEPTH][NT], a[DEPTH][MT];
+    auto load = [&](int64_t kb0) INLINE_LAMBDA {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) b[d][t] = load_piece(row_b[t], min(kb0 + d * WAVES, blocks - 1), g, p.K);
+    };
+    if (wave < blocks) load(wave);
+
+    const int stride = (int)blocks * kBlock + 16;
+    if constexpr (ROUND) {
+        // sixteen lanes to 128 values of a row: the largest of all first
+        const int units = (int)(p.M * blocks);
+        Raw<AT> kept;
+        auto read = [&](int unit, int &row, int &k) INLINE_LAMBDA {
+            row = unit / (int)blocks;
+            k = unit % (int)blocks * kBlock + r16 * 8;
+            return load_raw<AT>(p.a, row * p.lda, k, p.K);
+        };
+        if ((int)threadIdx.x < kInsideRows) tops[threadIdx.x] = 0;
+        __syncthreads();
+        for (int unit = threadIdx.x / 16; unit < units; unit += WAVES * 4) {
+            int row, k;
+            const Raw<AT> raw = read(unit, row, k);
+            if (unit < WAVES * 4) kept = raw;
+            float v[8];
+            widen<AT>(raw, v);
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);      // (those of a neighbour's piece do no harm)
+            top = row16_max(top);
+            if (r16 == 0) atomicMax(&tops[row], top);
+        }
+        __syncthreads();
+        for (int unit = threadIdx.x / 16; unit < units; unit += WAVES * 4) {
+            int row, k;
+            Raw<AT> raw = read(unit, row, k);
+            if (unit < WAVES * 4) raw = kept;
+            const float s = integer_scale(tops[row]), inv = 1.0f / s;
+            float v[8];
+            widen<AT>(raw, v);
+            *reinterpret_cast<uint2 *>(rounded + row * stride + k) = in_place(pack8_integers(v, s, inv), before_column(k, p.K));
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int64_t m = min(first + t * 16 + r16, p.M - 1);
+        row_a[t] = ROUND ? rounded + m * stride : static_cast<const int8_t *>(p.a) + m * p.lda;
+    }
+    i32x4 acc[MT][NT] = {};
+    for (int64_t kb0 = wave; kb0 < blocks; kb0 += DEPTH * WAVES) {
+        if (kb0 != wave) load(kb0);
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int64_t kb = min(kb0 + d * WAVES, blocks - 1);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                if constexpr (ROUND) {
+                    a[d][t].lo = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32);
+                    a[d][t].hi = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32 + 16);
+                } else {
+                    a[d][t] = load_piece(row_a[t], kb, g, p.K);
+                }
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int64_t kb = kb0 + d * WAVES;
+            if (kb >= blocks) break;
+            if (!ROUND && (kb + 1) * kBlock > p.K) {          // (rounded rows end in zeros)
+                const int64_t k = kb * kBlock + g * 32;
+#pragma unroll
+                for (int t = 0; t < MT; ++t) a[d][t] = Piece{first_bytes(a[d][t].lo, p.K - k), first_bytes(a[d][t].hi, p.K - k - 16)};
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = multiply(b[d][j].lo, a[d][i].lo, acc[i][j]);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = multiply(b[d][j].hi, a[d][i].hi, acc[i][j]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int o = threadIdx.x; o < MT * NT * 256; o += WAVES * 64) {
+        const int m = o / (16 * NT), n = o % (16 * NT);
+        if (first + m >= last || n0 + n >= p.N) continue;
+        const int tile = m / 16 * NT + n / 16, at = m % 16 + n % 16 / 4 * 16;
+        int32_t s = 0;
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) s += sums[k][tile][at][n % 4];
+        const float scale_a = ROUND ? integer_scale(tops[first + m]) : p.K ? p.scale_a[first + m] : 1.0f;
+        store_as<OUT>(p.out, (first + m) * p.ldo + n0 + n, scaled(s, scale_a, p.scale_b[n0 + n], p.bias, n0 + n));
+    }
+}
+
+// Many rows: BM x BN results to a workgroup of WM x WN wavefronts, each with (BM / WM) x (BN / WN) of them in registers.  Blocks of 128 values
+// of the BM + BN rows go to LDS without passing registers, the next ones while this one is multiplied.  A row's eight pieces of 16 bytes lie
+// exchanged by its index, so that the rows that a read of the lanes goes to fall on all banks.
+//
+// Eight wavefronts are two to a SIMD, and take turns: while one half of them reads its fragments of a block from LDS, the other half multiplies the ones
+// that it has read before.
+template <int BM, int BN, int WM, int WN, int OUT>
+__global__ __launch_bounds__(WM * WN * 64, 2) void integer_tiles_kernel(IntegerArgs p, uint32_t col_tiles)
+{
+    constexpr int WAVES = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16, LOADS_A = BM / 8 / WAVES, LOADS_B = BN / 8 / WAVES, LOADS = LOADS_A + LOADS_B;
+    constexpr bool TURNS = WAVES == 8;
+    static_assert(WAVES % 2 == 0 && LOADS_A * 8 * WAVES == BM && LOADS_B * 8 * WAVES == BN, "a wavefront loads whole groups of 8 rows, all at even or all at odd places");
+    __shared__ __attribute__((aligned(128))) uint8_t tiles[2][(BM + BN) * kBlock];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r16 = lane % 16, g = lane / 16;
+
+    // four pieces by all columns, then the next four: what a die works on at a time shares rows of both operands
+    const uint32_t pieces = (uint32_t)ceil_div(p.M, (int64_t)BM), at = by_die(blockIdx.x, pieces * col_tiles);
+    const uint32_t band = at / (4 * col_tiles), in_band = at % (4 * col_tiles), height = min(4u, pieces - band * 4);
+    const int64_t n0 = (int64_t)(in_band / height) * BN, m0 = (int64_t)(band * 4 + in_band % height) * BM;
+
+    // Rows are addressed by 32-bit offsets within the tile (the launcher keeps row strides to kMostStride).  What lies beyond the tile's last
+    // row is out of the buffers' range; what lies beyond column K is cut off from A's fragments.
+    const uint32_t lda = (uint32_t)p.lda, ldb = (uint32_t)p.ldb, blocks = (uint32_t)ceil_div(p.K, (int64_t)kBlock);
+    const uint32_t rows = (uint32_t)min((int64_t)BM, p.M - m0), cols = (uint32_t)min((int64_t)BN, p.N - n0), width = round_up((uint32_t)p.K, 16u);
+    const i32x4 mem_a = buffer_of(static_cast<const uint8_t *>(p.a) + m0 * p.lda, (rows - 1) * lda + width);
+    const i32x4 mem_b = buffer_of(reinterpret_cast<const uint8_t *>(p.b) + n0 * p.ldb, (cols - 1) * ldb + width);
+    const uint32_t chunk = (uint32_t)((lane % 8) ^ (lane / 8)) * 16, row0 = wave * 8 + lane / 8;
+    const uint32_t at_a = row0 * lda + chunk, at_b = row0 * ldb + chunk;
+    // (keeps the compiler from holding every sum of this and a multiple of a stride in a register of its own)
+    auto again = [](uint32_t x) INLINE_LAMBDA { asm volatile("" : "+v"(x)); return x; };
+    const uint32_t tiles_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)tiles[0] + wave * 1024;
+    auto load_one = [&](int i, uint32_t stage, uint32_t kb, uint32_t wanted, auto always) INLINE_LAMBDA {
+        const uint32_t to = tiles_at + stage * ((BM + BN) * kBlock) + (i < LOADS_A ? i * WAVES * 1024 : BM * kBlock + (i - LOADS_A) * WAVES * 1024);
+        const uint32_t from = i < LOADS_A ? again(at_a) + ((i * WAVES * 8) * lda + kb * kBlock) : again(at_b) + (((i - LOADS_A) * WAVES * 8) * ldb + kb * kBlock);
+        if constexpr (decltype(always)::value) load_to_lds(i < LOADS_A ? mem_a : mem_b, from, to);
+        else load_to_lds_if(wanted, i < LOADS_A ? mem_a : mem_b, from, to);
+    };
+    auto load = [&](uint32_t stage, uint32_t kb) INLINE_LAMBDA {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load_one(i, stage, kb, 1, std::true_type{});
+    };
+    const int wm = wave / WN, wn = wave % WN;
+    i32x4 acc[MT][NT] = {};
+    // A lane's 32 values of a row are pieces g and g + 4: the same ones of both operands.
+    const int half0 = r16 * kBlock + ((g ^ (r16 % 8)) * 16), half1 = half0 ^ 64;
+    if (blocks) {
+        const bool second = TURNS && wave >= WAVES / 2;      // the half that reads while the first multiplies
+        load(0, 0);
+        wait_for_loads();
+        meet();
+        uint32_t stage = 0;
+        if (second) {
+            if (1 < blocks) load(1, 1);
+            meet();
+        }
+        for (uint32_t kb = 0;; ++kb) {
+            if (!second && kb + 1 < blocks) load(stage ^ 1, kb + 1);
+            const uint8_t *tile = tiles[stage];
+            i32x4 b[NT][2], a[MT][2];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                b[j][0] = *reinterpret_cast<const i32x4 *>(tile + (BM + (wn * NT + j) * 16) * kBlock + half0);
+                b[j][1] = *reinterpret_cast<const i32x4 *>(tile + (BM + (wn * NT + j) * 16) * kBlock + half1);
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                a[i][0] = *reinterpret_cast<const i32x4 *>(tile + (wm * MT + i) * 16 * kBlock + half0);
+                a[i][1] = *reinterpret_cast<const i32x4 *>(tile + (wm * MT + i) * 16 * kBlock + half1);
+            }
+            if (kb + 1 == blocks && p.K % kBlock) {
+                const int64_t keep = p.K % kBlock - g * 16;
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    a[i][0] = first_bytes(a[i][0], keep);
+                    a[i][1] = first_bytes(a[i][1], keep - 64);
+                }
+            }
+            if constexpr (TURNS) {
+                // (the next block has to have come when the first half reads it, which is when the second half has done so with this one)
+                if (second) wait_for_loads();
+                else wait_for_reads();
+                meet();
+                __builtin_amdgcn_s_setprio(1);               // (the half that multiplies before the one that reads)
+            }
+            const uint32_t more = __builtin_amdgcn_readfirstlane(TURNS && second && kb + 2 < blocks);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = multiply(b[j][h], a[i][h], acc[i][j]);
+                // the second half's loads among its products, as each takes some time to get away
+                if constexpr (TURNS) {
+#pragma unroll
+                    for (int l = i * LOADS / MT; l < (i + 1) * LOADS / MT; ++l) load_one(l, stage, kb + 2, more, std::false_type{});
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if constexpr (TURNS) __builtin_amdgcn_s_setprio(0);
+            if (kb + 1 >= blocks) break;
+            if (!second) wait_for_loads();
+            meet();
+            stage ^= 1;
+        }
+        if (TURNS && !second) meet();                        // (the second half is one behind)
+    }
+    float scale_b[NT][4], bias[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t n = min(n0 + (wn * NT + j) * 16 + 4 * g + k, p.N - 1);
+            scale_b[j][k] = p.scale_b[n];
+            bias[j][k] = p.bias ? p.bias[n] : 0.0f;
+        }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const int64_t m = m0 + (wm * MT + i) * 16 + r16;
+        if (m >= p.M) continue;
+        const float scale_a = p.scale_a[m];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int64_t n = n0 + (wn * NT + j) * 16 + 4 * g, to = m * p.ldo + n;
+            float four[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                four[k] = (float)acc[i][j][k] * scale_a * scale_b[j][k];
+                if (p.bias) four[k] += bias[j][k];
+            }
+            if (n + 4 <= p.N) {
+                store_run<OUT>(p.out, to, four);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    if (n + k < p.N) store_as<OUT>(p.out, to + k, four[k]);
+            }
+        }
+    }
+}
+
+template <int BM, int BN, int WM, int WN, int OUT>
+int launch_tiles(const IntegerArgs &p, hipStream_t stream)
+{
+    const int64_t col_tiles = ceil_div(p.N, (int64_t)BN), pieces = ceil_div(p.M, (int64_t)BM);
+    if (col_tiles * pieces * WM * WN * 64 > kMostThreads) return fail(MADDNESS_E_UNSUPPORTED, "integer product: %lld x %lld results are too many", (long long)p.M, (long long)p.N);
+    note_kernel("integer_tiles_kernel", __PRETTY_FUNCTION__);
+    hipLaunchKernelGGL((integer_tiles_kernel<BM, BN, WM, WN, OUT>), dim3((unsigned)(col_tiles * pieces)), dim3(WM * WN * 64), 0, stream, p, (uint32_t)col_tiles);
+    return check_hip(hipGetLastError(), "launch integer_tiles_kernel");
+}
+
+template <int AT, int OUT, int MT, int NT, int DEPTH>
+int launch_few_as(const IntegerArgs &p, hipStream_t stream)
+{
+    constexpr int WAVES = 8;
+    const int64_t col_tiles = ceil_div(p.N, (int64_t)(16 * NT)), pieces = ceil_div(p.M, (int64_t)(16 * MT));
+    if (col_tiles * pieces * WAVES * 64 > kMostThreads) return fail(MADDNESS_E_UNSUPPORTED, "integer product: %lld x %lld results are too many", (long long)p.M, (long long)p.N);
+    note_kernel("integer_few_kernel", __PRETTY_FUNCTION__);
+    hipLaunchKernelGGL((integer_few_kernel<AT, MT, NT, WAVES, DEPTH, OUT>), dim3((unsigned)(col_tiles * pieces)), dim3(WAVES * 64), 0, stream, p, (uint32_t)col_tiles);
+    return check_hip(hipGetLastError(), "launch integer_few_kernel");
+}
+
+template <int AT, int OUT>
+int launch_few(const IntegerArgs &p, hipStream_t stream)
+{
+    if (p.M > 16) return launch_few_as<AT, OUT, 4, 2, 2>(p, stream);
+    // a wavefront's share of the sum is one block: more columns to a workgroup instead
+    return p.K <= 8 * kBlock ? launch_few_as<AT, OUT, 1, 4, 1>(p, stream) : launch_few_as<AT, OUT, 1, 1, 4>(p, stream);
+}
+
+template <int OUT>
+int launch_to(const IntegerArgs &p, int a_dtype, hipStream_t stream)
+{
+    if (a_dtype == MADDNESS_F32) return launch_few<kF32, OUT>(p, stream);
+    if (a_dtype == MADDNESS_F16) return launch_few<kF16, OUT>(p, stream);
+    if (a_dtype == MADDNESS_BF16) return launch_few<kBF16, OUT>(p, stream);
+    const bool far = std::max(p.lda, p.ldb) > kMostStride;
+    if (far || p.M <= 64 || p.K == 0) return launch_few<kI8, OUT>(p, stream);
+    if (ceil_div(p.M, (int64_t)256) * ceil_div(p.N, (int64_t)256) >= device_info().cus) return launch_tiles<256, 256, 2, 4, OUT>(p, stream);
+    return launch_tiles<128, 128, 2, 2, OUT>(p, stream);
+}
+
+}  // namespace
+
+bool integer_rounds_inside(int64_t M, int64_t K)
+{
+    return M <= kInsideRows && K >= 8 && M * round_up(K, (int64_t)kBlock) <= kInside;
+}
+
+int launch_integer_product(const IntegerArgs &p, int a_dtype, int out_dtype, hipStream_t stream)
+{
+    if (out_dtype == MADDNESS_F32) return launch_to<kF32>(p, a_dtype, stream);
+    if (out_dtype == MADDNESS_F16) return launch_to<kF16>(p, a_dtype, stream);
+    return launch_to<kBF16>(p, a_dtype, stream);
+}
+
+}  // namespace maddness
