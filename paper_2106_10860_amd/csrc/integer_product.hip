@@ -152,18 +152,19 @@ __global__ __launch_bounds__(WAVES * 64) void integer_few_kernel(IntegerArgs p, 
 }
 
 // Many rows: BM x BN results to a workgroup of WM x WN wavefronts, each with (BM / WM) x (BN / WN) of them in registers.  Blocks of 128 values
-// of the BM + BN rows go to LDS without passing registers, the next ones while this one is multiplied.  A row's eight pieces of 16 bytes lie
-// exchanged by its index, so that the rows that a read of the lanes goes to fall on all banks.
+// of the BM + BN rows go to LDS without passing registers: whole lines of memory, as the way from L2 takes one at a time (of half lines it brings half the bytes).  There two blocks
+// of A and three of B have a place, and a block is multiplied in two halves: the fragments of one are read while those of the other are multiplied.  So the wavefronts meet
+// once in a block, when the last of it is in registers and the next has come; then A's place is free for the block after that one.
 //
-// Eight wavefronts are two to a SIMD, and take turns: while one half of them reads its fragments of a block from LDS, the other half multiplies the ones
-// that it has read before.
+// A row's eight pieces of 16 bytes lie exchanged by its index, so that the rows that a read of the lanes goes to fall on all banks.
 template <int BM, int BN, int WM, int WN, int OUT>
 __global__ __launch_bounds__(WM * WN * 64, 2) void integer_tiles_kernel(IntegerArgs p, uint32_t col_tiles)
 {
-    constexpr int WAVES = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16, LOADS_A = BM / 8 / WAVES, LOADS_B = BN / 8 / WAVES, LOADS = LOADS_A + LOADS_B;
-    constexpr bool TURNS = WAVES == 8;
+    constexpr int WAVES = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16, LOADS_A = BM / 8 / WAVES, LOADS_B = BN / 8 / WAVES;
+    constexpr uint32_t PLACE_A = BM * kBlock, PLACE_B = BN * kBlock;
     static_assert(WAVES % 2 == 0 && LOADS_A * 8 * WAVES == BM && LOADS_B * 8 * WAVES == BN, "a wavefront loads whole groups of 8 rows, all at even or all at odd places");
-    __shared__ __attribute__((aligned(128))) uint8_t tiles[2][(BM + BN) * kBlock];
+    static_assert(MT >= LOADS_A && MT >= LOADS_B, "a load to each row of products at most");
+    __shared__ __attribute__((aligned(128))) uint8_t tile[2 * PLACE_A + 3 * PLACE_B];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r16 = lane % 16, g = lane / 16;
 
     // four pieces by all columns, then the next four: what a die works on at a time shares rows of both operands
@@ -171,8 +172,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void integer_tiles_kernel(IntegerA
     const uint32_t band = at / (4 * col_tiles), in_band = at % (4 * col_tiles), height = min(4u, pieces - band * 4);
     const int64_t n0 = (int64_t)(in_band / height) * BN, m0 = (int64_t)(band * 4 + in_band % height) * BM;
 
-    // Rows are addressed by 32-bit offsets within the tile (the launcher keeps row strides to kMostStride).  What lies beyond the tile's last
-    // row is out of the buffers' range; what lies beyond column K is cut off from A's fragments.
+    // Rows are addressed by 32-bit offsets within the tile (the launcher keeps row strides to kMostStride, so these are below 2^31).  What lies beyond the tile's last
+    // row, and beyond the last block, is out of the buffers' range; what lies beyond column K is cut off from A's fragments.
     const uint32_t lda = (uint32_t)p.lda, ldb = (uint32_t)p.ldb, blocks = (uint32_t)ceil_div(p.K, (int64_t)kBlock);
     const uint32_t rows = (uint32_t)min((int64_t)BM, p.M - m0), cols = (uint32_t)min((int64_t)BN, p.N - n0), width = round_up((uint32_t)p.K, 16u);
     const i32x4 mem_a = buffer_of(static_cast<const uint8_t *>(p.a) + m0 * p.lda, (rows - 1) * lda + width);
@@ -181,113 +182,131 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void integer_tiles_kernel(IntegerA
     const uint32_t at_a = row0 * lda + chunk, at_b = row0 * ldb + chunk;
     // (keeps the compiler from holding every sum of this and a multiple of a stride in a register of its own)
     auto again = [](uint32_t x) INLINE_LAMBDA { asm volatile("" : "+v"(x)); return x; };
-    const uint32_t tiles_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)tiles[0] + wave * 1024;
-    auto load_one = [&](int i, uint32_t stage, uint32_t kb, uint32_t wanted, auto always) INLINE_LAMBDA {
-        const uint32_t to = tiles_at + stage * ((BM + BN) * kBlock) + (i < LOADS_A ? i * WAVES * 1024 : BM * kBlock + (i - LOADS_A) * WAVES * 1024);
-        const uint32_t from = i < LOADS_A ? again(at_a) + ((i * WAVES * 8) * lda + kb * kBlock) : again(at_b) + (((i - LOADS_A) * WAVES * 8) * ldb + kb * kBlock);
-        if constexpr (decltype(always)::value) load_to_lds(i < LOADS_A ? mem_a : mem_b, from, to);
-        else load_to_lds_if(wanted, i < LOADS_A ? mem_a : mem_b, from, to);
+    const uint32_t tile_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)tile + wave * 1024;
+    auto column = [&](uint32_t kb) INLINE_LAMBDA { return kb < blocks ? kb * kBlock : 0x80000000u; };
+    auto load_a = [&](int i, uint32_t place, uint32_t kb) INLINE_LAMBDA {
+        load_to_lds(mem_a, again(at_a) + ((i * WAVES * 8) * lda + column(kb)), tile_at + place + i * WAVES * 1024);
     };
-    auto load = [&](uint32_t stage, uint32_t kb) INLINE_LAMBDA {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) load_one(i, stage, kb, 1, std::true_type{});
+    auto load_b = [&](int i, uint32_t place, uint32_t kb) INLINE_LAMBDA {
+        load_to_lds(mem_b, again(at_b) + ((i * WAVES * 8) * ldb + column(kb)), tile_at + 2 * PLACE_A + place + i * WAVES * 1024);
     };
-    const int wm = wave / WN, wn = wave % WN;
+    const int wm = wave / WN, wn = wave % WN, tail = (int)(p.K % kBlock);
+    const uint32_t from = r16 * kBlock + ((g ^ (r16 % 8)) * 16), from_a = from + wm * MT * 16 * kBlock, from_b = from + 2 * PLACE_A + wn * NT * 16 * kBlock;
     i32x4 acc[MT][NT] = {};
-    // A lane's 32 values of a row are pieces g and g + 4: the same ones of both operands.
-    const int half0 = r16 * kBlock + ((g ^ (r16 % 8)) * 16), half1 = half0 ^ 64;
+    struct Fragments {
+        i32x4 a[MT], b[NT];
+    } first, second;
+    // The r-th of a half's fragments, B's first; the halves of a row's pieces differ in one bit of their place.
+    auto read_one = [&](int r, int half, uint32_t place_a, uint32_t place_b, Fragments &f) INLINE_LAMBDA {
+        if (r < NT) f.b[r] = *reinterpret_cast<const i32x4 *>(tile + place_b + (from_b ^ (half * 64)) + r * 16 * kBlock);
+        else f.a[r - NT] = *reinterpret_cast<const i32x4 *>(tile + place_a + (from_a ^ (half * 64)) + (r - NT) * 16 * kBlock);
+    };
+    auto cut = [&](Fragments &f, int keep) INLINE_LAMBDA {
+        i32x4 mask;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int bytes = min(max(keep - g * 16 - k * 4, 0), 4);
+            mask[k] = bytes == 4 ? -1 : (int)((1u << (8 * bytes)) - 1);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) f.a[i] &= mask;
+    };
+    auto multiply_and = [&](const Fragments &f, auto beside) INLINE_LAMBDA {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            beside(i);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = multiply(f.b[j], f.a[i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
     if (blocks) {
-        const bool second = TURNS && wave >= WAVES / 2;      // the half that reads while the first multiplies
-        load(0, 0);
-        wait_for_loads();
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int i = 0; i < LOADS_A; ++i) load_a(i, s * PLACE_A, s);
+#pragma unroll
+            for (int i = 0; i < LOADS_B; ++i) load_b(i, s * PLACE_B, s);
+        }
+        wait_for_loads_but<LOADS_A + LOADS_B>();
         meet();
-        uint32_t stage = 0;
-        if (second) {
-            if (1 < blocks) load(1, 1);
+#pragma unroll
+        for (int r = 0; r < MT + NT; ++r) read_one(r, 0, 0, 0, first);
+        uint32_t place_a = 0, place_b = 0, far_b = 2 * PLACE_B;           // of this block, and of B's block after the next
+        for (uint32_t kb = 0; kb < blocks; ++kb) {
+            const bool last = kb + 1 == blocks && tail;
+            if (last) cut(first, tail);
+            multiply_and(first, [&](int i) INLINE_LAMBDA {
+#pragma unroll
+                for (int r = i * (MT + NT) / MT; r < (i + 1) * (MT + NT) / MT; ++r) read_one(r, 1, place_a, place_b, second);
+                if (i < LOADS_B) load_b(i, far_b, kb + 2);
+            });
+            wait_for_loads_but<LOADS_B>();
             meet();
+            if (last) cut(second, tail - 64);
+            const uint32_t free_a = place_a;
+            place_a ^= PLACE_A;
+            far_b = place_b;
+            place_b = place_b == 2 * PLACE_B ? 0 : place_b + PLACE_B;
+            multiply_and(second, [&](int i) INLINE_LAMBDA {
+#pragma unroll
+                for (int r = i * (MT + NT) / MT; r < (i + 1) * (MT + NT) / MT; ++r) read_one(r, 0, place_a, place_b, first);
+                if (i < LOADS_A) load_a(i, free_a, kb + 2);
+            });
         }
-        for (uint32_t kb = 0;; ++kb) {
-            if (!second && kb + 1 < blocks) load(stage ^ 1, kb + 1);
-            const uint8_t *tile = tiles[stage];
-            i32x4 b[NT][2], a[MT][2];
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                b[j][0] = *reinterpret_cast<const i32x4 *>(tile + (BM + (wn * NT + j) * 16) * kBlock + half0);
-                b[j][1] = *reinterpret_cast<const i32x4 *>(tile + (BM + (wn * NT + j) * 16) * kBlock + half1);
-            }
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                a[i][0] = *reinterpret_cast<const i32x4 *>(tile + (wm * MT + i) * 16 * kBlock + half0);
-                a[i][1] = *reinterpret_cast<const i32x4 *>(tile + (wm * MT + i) * 16 * kBlock + half1);
-            }
-            if (kb + 1 == blocks && p.K % kBlock) {
-                const int64_t keep = p.K % kBlock - g * 16;
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    a[i][0] = first_bytes(a[i][0], keep);
-                    a[i][1] = first_bytes(a[i][1], keep - 64);
-                }
-            }
-            if constexpr (TURNS) {
-                // (the next block has to have come when the first half reads it, which is when the second half has done so with this one)
-                if (second) wait_for_loads();
-                else wait_for_reads();
-                meet();
-                __builtin_amdgcn_s_setprio(1);               // (the half that multiplies before the one that reads)
-            }
-            const uint32_t more = __builtin_amdgcn_readfirstlane(TURNS && second && kb + 2 < blocks);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][j] = multiply(b[j][h], a[i][h], acc[i][j]);
-                // the second half's loads among its products, as each takes some time to get away
-                if constexpr (TURNS) {
-#pragma unroll
-                    for (int l = i * LOADS / MT; l < (i + 1) * LOADS / MT; ++l) load_one(l, stage, kb + 2, more, std::false_type{});
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-            if constexpr (TURNS) __builtin_amdgcn_s_setprio(0);
-            if (kb + 1 >= blocks) break;
-            if (!second) wait_for_loads();
-            meet();
-            stage ^= 1;
-        }
-        if (TURNS && !second) meet();                        // (the second half is one behind)
+        wait_for_loads();                                    // (its place in LDS is another's from here on)
+        meet();
     }
-    float scale_b[NT][4], bias[NT][4];
+    // A wavefront's results go through its part of LDS, half of its rows at a time, so that they are stored in whole lines: lanes hold four neighbours
+    // of sixteen rows each, pieces of 8 or 16 bytes (8192 x 4096 x 128 to bfloat16: 34 us with those, see below with lines).
+    constexpr int ROWS = MT * 8, COLS = NT * 16, RUN = 16 / elem_size(OUT), LINE = COLS * elem_size(OUT) + 16;
+    static_assert(ROWS * LINE * WAVES <= (int)sizeof(tile), "the wavefronts' results fit LDS");
+    uint8_t *const mine = tile + wave * ROWS * LINE;
+    const int64_t col0 = n0 + wn * COLS + lane % (COLS / RUN) * RUN;
+    float scale_b[NT][4];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int64_t n = min(n0 + (wn * NT + j) * 16 + 4 * g + k, p.N - 1);
-            scale_b[j][k] = p.scale_b[n];
-            bias[j][k] = p.bias ? p.bias[n] : 0.0f;
-        }
+        for (int k = 0; k < 4; ++k) scale_b[j][k] = p.scale_b[min(n0 + (wn * NT + j) * 16 + 4 * g + k, p.N - 1)];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int64_t m = m0 + (wm * MT + i) * 16 + r16;
-        if (m >= p.M) continue;
-        const float scale_a = p.scale_a[m];
+    for (int half = 0; half < 2; ++half) {
+        const int64_t row0 = m0 + wm * MT * 16 + half * ROWS;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const int64_t n = n0 + (wn * NT + j) * 16 + 4 * g, to = m * p.ldo + n;
-            float four[4];
+        for (int i = 0; i < MT / 2; ++i) {
+            const float scale_a = p.scale_a[min(row0 + i * 16 + r16, p.M - 1)];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                four[k] = (float)acc[i][j][k] * scale_a * scale_b[j][k];
-                if (p.bias) four[k] += bias[j][k];
+            for (int j = 0; j < NT; ++j) {
+                const i32x4 sum = acc[half * (MT / 2) + i][j];
+                float four[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) four[k] = (float)sum[k] * scale_a * scale_b[j][k];
+                if (p.bias) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) four[k] += p.bias[min(n0 + (wn * NT + j) * 16 + 4 * g + k, p.N - 1)];
+                }
+                store_run<OUT>(mine + (i * 16 + r16) * LINE, j * 16 + 4 * g, four);
             }
-            if (n + 4 <= p.N) {
-                store_run<OUT>(p.out, to, four);
+        }
+        wave_lds_fence();
+#pragma unroll
+        for (int q = 0; q < ROWS * COLS / RUN / 64; ++q) {
+            const int row = q * (64 * RUN / COLS) + lane / (COLS / RUN);
+            const i32x4 run = *reinterpret_cast<const i32x4 *>(mine + row * LINE + lane % (COLS / RUN) * 16);
+            if (row0 + row >= p.M) continue;
+            const int64_t to = (row0 + row) * p.ldo + col0;
+            if (col0 + RUN <= p.N) {
+                struct __attribute__((packed, aligned(elem_size(OUT)))) Words { i32x4 w; };
+                reinterpret_cast<Words *>(static_cast<char *>(p.out) + to * elem_size(OUT))->w = run;
             } else {
 #pragma unroll
-                for (int k = 0; k < 3; ++k)
-                    if (n + k < p.N) store_as<OUT>(p.out, to + k, four[k]);
+                for (int k = 0; k < RUN - 1; ++k)
+                    if (col0 + k < p.N) {
+                        if constexpr (OUT == kF32) static_cast<int32_t *>(p.out)[to + k] = run[k];
+                        else static_cast<uint16_t *>(p.out)[to + k] = (uint16_t)((uint32_t)run[k / 2] >> (k % 2 * 16));
+                    }
             }
         }
+        wave_lds_fence();
     }
 }
 

@@ -46,6 +46,10 @@ __device__ __forceinline__ void load_to_lds_if(uint32_t wanted, i32x4 buffer, ui
 // Waits until this wavefront's loads have come and its reads of LDS are done.
 __device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
+// Waits until all but the last N loads of this wavefront have come and its reads of LDS are done.
+template <int N>
+__device__ __forceinline__ void wait_for_loads_but() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
+
 __device__ __forceinline__ void wait_for_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // Waits for the workgroup's other wavefronts.
