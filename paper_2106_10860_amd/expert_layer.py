@@ -4,7 +4,8 @@
     out, saved = layer.forward(x, logits, training=True)
     dx, dW, dlogits = layer.backward(saved, grad)
 
-Run as a module it trains such a layer on a task that wants different matrices for different tokens, and prints the loss.
+Run as a module it trains such a layer on a task that wants different matrices for different tokens, and prints the loss; ``--norm`` puts a layer
+norm before it, ``--balance`` adds the loss that keeps the experts' tokens alike, ``--clip`` scales the gradients down to a norm.
 """
 from __future__ import annotations
 
@@ -25,6 +26,9 @@ class Saved:
     x_t: object = None
     y: object = None
     tokens: int = 0
+    balance_loss: object = None        # with ``balance``: the loss, the experts' tokens and what the gradient takes
+    counts: object = None
+    push: object = None
 
 
 class ExpertLayer:
@@ -34,10 +38,13 @@ class ExpertLayer:
     ``slot_dtype`` is what a token's k results are held in between their products and the weighted sum (and those of the backward pass).  In
     fp32, the default, out and the gradients are rounded once, to the types that they are returned in.  A narrower type halves the bytes of
     that step and rounds every one of the k; float16 makes a result beyond 65504 infinite, also where its weight is 0 or the sum would be in
-    range."""
+    range.
+
+    ``balance``: the factor of the loss of ``maddness_balance``, or 0 for none.  In training it is in ``Saved.balance_loss`` (an fp32 scalar tensor, to be added to the
+    model's own loss), beside the experts' tokens in ``Saved.counts``, and its gradient is part of that of the logits."""
 
     def __init__(self, W: "m.BlockMatrix", Wt=None, k: int = 1, scores: str = "softmax", bias=None, groups: int = 1, kept_groups: int = 1,
-                 renormalise: bool = True, factor: float = 1.0, slot_dtype=None):
+                 renormalise: bool = True, factor: float = 1.0, slot_dtype=None, balance: float = 0.0):
         if len(W.shape) != 3:
             raise ValueError("W must be [experts, outputs, inputs]")
         if Wt is not None and Wt.shape != (W.shape[0], W.shape[2], W.shape[1]):
@@ -48,6 +55,7 @@ class ExpertLayer:
         m.blocks._float_code(slot_dtype, "slot_dtype")
         self.W, self.Wt, self.experts, self.k, self.slot_dtype = W, Wt, W.shape[0], k, slot_dtype
         self.choice = {"scores": scores, "renormalise": renormalise, "factor": factor}
+        self.balance = float(balance)
         self.groups = {"bias": bias, "groups": groups, "kept_groups": kept_groups}
 
     @classmethod
@@ -81,11 +89,14 @@ class ExpertLayer:
         if not training:
             return out, Saved(ids, weights)
         # (a copy: the caller may write to its logits before the backward pass)
-        return out, Saved(ids, weights, logits.clone(), offsets, source, place, x_t, y, x.shape[0])
+        saved = Saved(ids, weights, logits.clone(), offsets, source, place, x_t, y, x.shape[0])
+        if self.balance:
+            saved.balance_loss, saved.counts, saved.push = m.maddness_balance(logits, ids, scores=self.choice["scores"], factor=self.balance)
+        return out, saved
 
-    def backward(self, saved: Saved, grad, weight_dtype=None):
+    def backward(self, saved: Saved, grad, weight_dtype=None, balance_gradient=None):
         """The gradient of out [T, outputs] -> those of x, of the matrices [experts, outputs, inputs] (of ``weight_dtype``, or grad's
-        dtype) and of logits."""
+        dtype) and of logits.  ``balance_gradient``: that of the balance's loss, an fp32 tensor of one element (1: what a loss is scaled by)."""
         if saved.y is None:
             raise ValueError("saved is of a forward pass without training=True")
         if tuple(grad.shape) != (saved.tokens, self.W.shape[1]):
@@ -94,13 +105,16 @@ class ExpertLayer:
             grad = grad.contiguous()
         dweights = m.maddness_combine_gradient(grad, saved.y, saved.place)
         dlogits = m.maddness_route_gradient(saved.logits, saved.ids, dweights, **self.choice)
+        if saved.push is not None:
+            m.maddness_balance_gradient(saved.logits, saved.push, scores=self.choice["scores"], loss_gradient=balance_gradient, add=dlogits, out=dlogits)
         dy, dy_t = m.maddness_quantise_blocks(grad, both=True, source=saved.source, repeat=self.k, factors=saved.weights)
         dx = m.maddness_combine(m.maddness_block_product(dy, self.Wt, saved.offsets, out_dtype=self.slot_dtype), saved.place, out_dtype=grad.dtype)
         dW = m.maddness_block_product(dy_t, saved.x_t, saved.offsets, by="depth", out_dtype=weight_dtype or grad.dtype)
         return dx, dW, dlogits
 
 
-def train_example(steps: int = 60, tokens: int = 2048, inputs: int = 256, outputs: int = 192, experts: int = 8, k: int = 2, seed: int = 0):
+def train_example(steps: int = 60, tokens: int = 2048, inputs: int = 256, outputs: int = 192, experts: int = 8, k: int = 2, seed: int = 0, norm: bool = False,
+                  balance: float = 0.0, clip=None):
     """Tokens of several kinds, each with a matrix of its own; a gate and a layer of experts learn them.  Returns the losses."""
     import torch
     g = torch.Generator(device="cuda").manual_seed(seed)
@@ -110,20 +124,38 @@ def train_example(steps: int = 60, tokens: int = 2048, inputs: int = 256, output
 
     kinds, truth = normal(experts, inputs), normal(experts, outputs, inputs) / inputs ** 0.5
     weight, gate = normal(experts, outputs, inputs) * (0.3 / inputs ** 0.5), 0.3 * normal(experts, inputs)
+    scale, shift = torch.ones(inputs, device="cuda"), torch.zeros(inputs, device="cuda")
     losses = []
     for step in range(steps):
         kind = torch.randint(experts, (tokens,), generator=g, device="cuda")
         x = kinds[kind] + 0.5 * normal(tokens, inputs)
         want = torch.bmm(truth[kind], x.unsqueeze(2)).squeeze(2)
-        layer = ExpertLayer.from_weights(weight, k)
-        out, saved = layer.forward(x, x @ gate.T, training=True)
+        h = x
+        if norm:
+            h, mean, rstd = m.maddness_layer_norm(x, scale, shift, training=True)
+        layer = ExpertLayer.from_weights(weight, k, balance=balance)
+        out, saved = layer.forward(h, h @ gate.T, training=True)
         losses.append(float(((out - want) ** 2).mean()))
-        dx, dW, dlogits = layer.backward(saved, 2 * (out - want) / out.numel())
-        weight -= 4.0 * dW
-        gate -= 0.05 * (dlogits.T @ x)
+        dh, dW, dlogits = layer.backward(saved, 2 * (out - want) / out.numel())
+        gradients = [dW, dlogits.T @ h]
+        if norm:
+            gradients += m.maddness_layer_norm_gradient(dh + dlogits @ gate, x, mean, rstd, scale)[1:]
+        if clip is not None:
+            m.maddness_clip_gradients(gradients, clip)
+        weight -= 4.0 * gradients[0]
+        gate -= 0.05 * gradients[1]
+        if norm:
+            scale -= 0.05 * gradients[2]
+            shift -= 0.05 * gradients[3]
     return losses
 
 
 if __name__ == "__main__":
-    curve = train_example()
+    import argparse
+    parser = argparse.ArgumentParser(description="Trains a layer of experts.")
+    parser.add_argument("--norm", action="store_true", help="a layer norm before the layer")
+    parser.add_argument("--balance", type=float, default=0.0, help="factor of the loss that keeps the experts' tokens alike")
+    parser.add_argument("--clip", type=float, default=None, help="largest norm of a step's gradients")
+    chosen = parser.parse_args()
+    curve = train_example(norm=chosen.norm, balance=chosen.balance, clip=chosen.clip)
     print("mean squared error, every tenth step: " + " ".join(f"{v:.4f}" for v in curve[::10] + curve[-1:]))
