@@ -5,10 +5,47 @@
 namespace maddness {
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64;
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kGradientWaves = 4;
 constexpr float kTop = 3.402823466e38f;
 
 constexpr auto larger = [](float a, float b) INLINE_LAMBDA { return fmaxf(a, b); };
+
+// f over the LANES lanes that share a token, in all of them.
+template <int LANES, typename T, typename F>
+__device__ __forceinline__ T over_token(T x, F f)
+{
+    if constexpr (LANES == 4) {
+        x = f(x, __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0xb1, 0xf, 0xf, true)));       // lane l ^ 1
+        return f(x, __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x4e, 0xf, 0xf, true)));    // lane l ^ 2
+    } else {
+        return over_lanes<LANES>(x, f);
+    }
+}
+
+// The sum over the lanes of the wavefront's tokens that have the same experts, in all of them.
+template <int LANES, typename T>
+__device__ __forceinline__ T over_tokens(T x)
+{
+    if constexpr (LANES == 4) {
+        x += from_lane<8>(x);
+        x += from_lane<4>(x);
+    }
+    if constexpr (LANES <= 16) {
+        x += from_lane<16>(x);
+        x += from_lane<32>(x);
+    }
+    return x;
+}
+
+// e^x by the 2^x instruction, whose argument's rounding is put back: to 2 steps of fp32 (x kept to +-128; results below 2^-126 are 0).  The library's function
+// takes twice the operations.
+__device__ __forceinline__ float exponential(float x)
+{
+    constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f, kLn2 = 0.693147182f;
+    x = __builtin_amdgcn_fmed3f(x, -128.0f, 128.0f);
+    const float t = x * kLog2e, e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e, kLn2 * __builtin_fmaf(x, kLog2eRest, __builtin_fmaf(x, kLog2e, -t)), e);
+}
 
 // The four neighbours of every 4 LANES experts that a lane has: i of its R.
 template <int LANES>
@@ -19,11 +56,10 @@ struct alignas(4 * elem_size(DT)) Four {
     char bytes[4 * elem_size(DT)];
 };
 
-// A token's scores over LANES lanes, R to a lane, and their sum; 0 for masked ones and beyond E.
+// A lane's logits of a token.
 template <int DT, int LANES, int R>
-__device__ __forceinline__ float load_scores(const BalanceArgs &a, bool pieces, int64_t t, int lane, float (&s)[R], uint32_t &seen)
+__device__ __forceinline__ void load_logits(const BalanceArgs &a, bool pieces, int64_t t, int lane, float (&x)[R])
 {
-    float x[R];
 #pragma unroll
     for (int q = 0; q < R / 4; ++q) {
         const int e = expert_at<LANES>(lane, 4 * q);
@@ -37,6 +73,12 @@ __device__ __forceinline__ float load_scores(const BalanceArgs &a, bool pieces, 
             for (int i = 0; i < 4; ++i) x[4 * q + i] = widen_at<DT>(a.logits, t * a.ldl + min(e + i, a.E - 1));
         }
     }
+}
+
+// A token's scores over LANES lanes, R to a lane, and their sum; 0 for masked ones and beyond E.
+template <int LANES, int R>
+__device__ __forceinline__ float scores_of(const BalanceArgs &a, int lane, float (&x)[R], float (&s)[R], uint32_t &seen)
+{
     seen = 0;
     float top = -kTop;
 #pragma unroll
@@ -47,14 +89,14 @@ __device__ __forceinline__ float load_scores(const BalanceArgs &a, bool pieces, 
         top = fmaxf(top, x[i]);
     }
     float sum = 0.0f;
-    if (a.softmax) top = over_lanes<LANES>(top, larger);
+    if (a.softmax) top = over_token<LANES>(top, larger);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-        const float v = a.softmax ? expf(x[i] - top) : 1.0f / (1.0f + expf(-x[i]));
+        const float v = a.softmax ? exponential(x[i] - top) : __builtin_amdgcn_rcpf(1.0f + exponential(-x[i]));
         s[i] = seen >> i & 1 ? v : 0.0f;
         sum += s[i];
     }
-    return over_lanes<LANES>(sum, plus);
+    return over_token<LANES>(sum, plus);
 }
 
 // Where the workgroups leave their sums.
@@ -80,17 +122,24 @@ __host__ __device__ inline Workspace workspace_of(void *base, int64_t groups, in
     return w;
 }
 
-// Every workgroup's share: its tokens' p added up for each expert, and its part of the ids counted.
-template <int DT, int LANES, int R>
+__device__ __forceinline__ float push_of(const BalanceArgs &a, int64_t count, int64_t chosen, int64_t live)
+{
+    return live && chosen ? (float)((double)a.factor * a.E * (double)count / ((double)chosen * (double)live)) : 0.0f;
+}
+
+// Every workgroup's share: its tokens' p added up for each expert, and its part of the ids counted.  Four tokens of a lane are asked for at a time, and their sums over the lanes go on
+// beside each other.  ALL: the only workgroup, which gives the results (few tokens: a launch less).
+template <int DT, int LANES, int R, bool ALL>
 __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a, void *base, bool pieces)
 {
-    constexpr int TOKENS = 64 / LANES;                         // of a wavefront at a time
+    constexpr int TOKENS = 64 / LANES, ONCE = R <= 4 ? 4 : 1;  // of a wavefront side by side, and in turn
     __shared__ int32_t counts[R * LANES];
     __shared__ float mass[kWaves][R * LANES];
     __shared__ int32_t lives[kWaves];
+    __shared__ double parts[kWaves];
     const Workspace w = workspace_of(base, gridDim.x, a.E);
     const int wave = threadIdx.x / 64, lane = threadIdx.x % LANES, part = threadIdx.x % 64 / LANES;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *w.ticket = 0;
+    if (!ALL && blockIdx.x == 0 && threadIdx.x == 0) *w.ticket = 0;
     for (int e = threadIdx.x; e < a.E; e += kThreads) counts[e] = 0;
     __syncthreads();
     const int64_t ids = a.T * a.k;
@@ -100,46 +149,66 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a, void *
     }
     float sum[R] = {};
     int live = 0;
-    for (int64_t t = ((int64_t)blockIdx.x * kWaves + wave) * TOKENS + part; t < a.T; t += (int64_t)gridDim.x * kWaves * TOKENS) {
-        float s[R];
-        uint32_t seen;
-        const float all = load_scores<DT, LANES, R>(a, pieces, t, lane, s, seen);
-        if (all > 0.0f) {
-            ++live;
-            const float scale = 1.0f / all;
+    const int64_t step = (int64_t)gridDim.x * kWaves * TOKENS;
+    for (int64_t t = ((int64_t)blockIdx.x * kWaves + wave) * TOKENS + part; t < a.T; t += ONCE * step) {
+        float x[ONCE][R], s[R];
+#pragma unroll
+        for (int u = 0; u < ONCE; ++u) load_logits<DT, LANES, R>(a, pieces, min(t + u * step, a.T - 1), lane, x[u]);
+#pragma unroll
+        for (int u = 0; u < ONCE; ++u) {
+            uint32_t seen;
+            const float all = scores_of<LANES, R>(a, lane, x[u], s, seen);
+            const bool here = all > 0.0f && t + u * step < a.T;
+            live += here;
+            const float scale = here ? 1.0f / all : 0.0f;
 #pragma unroll
             for (int i = 0; i < R; ++i) sum[i] += s[i] * scale;
         }
     }
-    if constexpr (LANES == 16) {
-        live += (int)from_lane<16>((uint32_t)live);
-        live += (int)from_lane<32>((uint32_t)live);
+    live = (int)over_tokens<LANES>((uint32_t)live);
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            sum[i] += from_lane<16>(sum[i]);
-            sum[i] += from_lane<32>(sum[i]);
-        }
-    }
+    for (int i = 0; i < R; ++i) sum[i] = over_tokens<LANES>(sum[i]);
     if (part == 0) {
 #pragma unroll
         for (int i = 0; i < R; ++i) mass[wave][expert_at<LANES>(lane, i)] = sum[i];
         if (lane == 0) lives[wave] = live;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < a.E; e += kThreads) {
-        float m = mass[0][e];
+    uint32_t chosen = 0;
+    int all = 0;
+    if (ALL || threadIdx.x < 64) {
+        for (int e = threadIdx.x % 64; e < a.E; e += 64) chosen += (uint32_t)counts[e];
+        chosen = over_lanes<64>(chosen, plus);
+        for (int v = 0; v < kWaves; ++v) all += lives[v];
+    }
+    const int e = threadIdx.x;                                 // (E <= kThreads)
+    float m = 0.0f;
+    if (e < a.E) {
+        m = mass[0][e];
 #pragma unroll
         for (int v = 1; v < kWaves; ++v) m += mass[v][e];
-        w.mass[(int64_t)blockIdx.x * a.E + e] = m;
-        w.counts[(int64_t)blockIdx.x * a.E + e] = counts[e];
     }
-    if (threadIdx.x < 64) {
-        uint32_t chosen = 0;
-        for (int e = threadIdx.x; e < a.E; e += 64) chosen += (uint32_t)counts[e];
-        chosen = over_lanes<64>(chosen, plus);
+    if constexpr (ALL) {
+        double loss = 0.0;
+        if (e < a.E) {
+            const float push = push_of(a, counts[e], chosen, all);
+            a.counts[e] = counts[e];
+            a.push[e] = push;
+            loss = (double)push * m;
+        }
+        loss = over_lanes<64>(loss, plus);
+        if (threadIdx.x % 64 == 0) parts[wave] = loss;
+        __syncthreads();
         if (threadIdx.x == 0) {
-            int all = 0;
-            for (int v = 0; v < kWaves; ++v) all += lives[v];
+            for (int v = 1; v < kWaves; ++v) loss += parts[v];
+            *a.loss = (float)loss;
+        }
+    } else {
+        if (e < a.E) {
+            w.mass[(int64_t)blockIdx.x * a.E + e] = m;
+            w.counts[(int64_t)blockIdx.x * a.E + e] = counts[e];
+        }
+        if (threadIdx.x == 0) {
             w.live[blockIdx.x] = all;
             w.chosen[blockIdx.x] = (int32_t)chosen;
         }
@@ -150,51 +219,49 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a, void *
 // experts' parts of the loss up, in their order.
 __global__ __launch_bounds__(1024) void balance_sum_kernel(BalanceArgs a, void *base, int groups)
 {
-    __shared__ double masses[64][kSlice];
-    __shared__ int32_t counts[64][kSlice];
-    __shared__ int64_t lives[16], chosens[16];
+    __shared__ double masses[16][kSlice];
+    __shared__ uint32_t counts[16][kSlice];
+    __shared__ uint32_t lives[16], chosens[16];
     const Workspace w = workspace_of(base, groups, a.E);
-    const int column = threadIdx.x % kSlice, run = threadIdx.x / kSlice, e = blockIdx.x * kSlice + column;
-    int64_t live = 0, chosen = 0;
-    for (int g = threadIdx.x; g < groups; g += 1024) {
-        live += w.live[g];
-        chosen += w.chosen[g];
-    }
+    const int column = threadIdx.x % kSlice, run = threadIdx.x / kSlice, wave = threadIdx.x / 64, e = blockIdx.x * kSlice + column;
+    uint32_t live = 0, chosen = 0, count = 0;                  // (all below 2^31)
     double mass = 0.0;
-    int32_t count = 0;
+    for (int g = threadIdx.x; g < groups; g += 1024) {
+        live += (uint32_t)w.live[g];
+        chosen += (uint32_t)w.chosen[g];
+    }
+#pragma unroll 4
     for (int g = run; g < groups; g += 64) {
         mass += (double)w.mass[(int64_t)g * a.E + min(e, a.E - 1)];
-        count += w.counts[(int64_t)g * a.E + min(e, a.E - 1)];
+        count += (uint32_t)w.counts[(int64_t)g * a.E + min(e, a.E - 1)];
     }
-    masses[run][column] = mass;
-    counts[run][column] = count;
-#pragma unroll
-    for (int d = 32; d; d /= 2) {
-        live += __shfl_xor(live, d);
-        chosen += __shfl_xor(chosen, d);
-    }
-    if (threadIdx.x % 64 == 0) {
-        lives[threadIdx.x / 64] = live;
-        chosens[threadIdx.x / 64] = chosen;
+    live = over_lanes<64>(live, plus);
+    chosen = over_lanes<64>(chosen, plus);
+    mass += from_lane<16>(mass);
+    mass += from_lane<32>(mass);
+    count += from_lane<16>(count);
+    count += from_lane<32>(count);
+    if (threadIdx.x % 64 < kSlice) {
+        masses[wave][column] = mass;
+        counts[wave][column] = count;
+        lives[wave] = live;
+        chosens[wave] = chosen;
     }
     __syncthreads();
     if (threadIdx.x >= 64) return;
-    double part = 0.0;
-    live = chosen = 0;
+    mass = 0.0;
+    live = chosen = count = 0;
+#pragma unroll
     for (int v = 0; v < 16; ++v) {
+        mass += masses[v][column];
+        count += counts[v][column];
         live += lives[v];
         chosen += chosens[v];
     }
+    double part = 0.0;
     if (threadIdx.x < kSlice && e < a.E) {
-        mass = 0.0;
-        count = 0;
-#pragma unroll 8
-        for (int r = 0; r < 64; ++r) {
-            mass += masses[r][column];
-            count += counts[r][column];
-        }
-        const float push = live && chosen ? (float)((double)a.factor * a.E * count / ((double)chosen * (double)live)) : 0.0f;
-        a.counts[e] = count;
+        const float push = push_of(a, count, chosen, live);
+        a.counts[e] = (int32_t)count;
         a.push[e] = push;
         part = push * mass;
     }
@@ -214,9 +281,9 @@ __global__ __launch_bounds__(1024) void balance_sum_kernel(BalanceArgs a, void *
 }
 
 template <int DT, int LANES, int R>
-__global__ __launch_bounds__(kThreads) void balance_gradient_kernel(BalanceArgs a, bool pieces, bool add_pieces)
+__global__ __launch_bounds__(kGradientWaves * 64) void balance_gradient_kernel(BalanceArgs a, bool pieces, bool add_pieces)
 {
-    constexpr int TOKENS = 64 / LANES;
+    constexpr int TOKENS = 64 / LANES, ONCE = R <= 4 ? 2 : 1;
     const int wave = threadIdx.x / 64, lane = threadIdx.x % LANES, part = threadIdx.x % 64 / LANES;
     const float times = a.loss_gradient ? *a.loss_gradient : 1.0f;
     float push[R];
@@ -225,44 +292,58 @@ __global__ __launch_bounds__(kThreads) void balance_gradient_kernel(BalanceArgs 
         const int e = expert_at<LANES>(lane, i);
         push[i] = e < a.E ? a.push[e] : 0.0f;
     }
-    for (int64_t t = ((int64_t)blockIdx.x * kWaves + wave) * TOKENS + part; t < a.T; t += (int64_t)gridDim.x * kWaves * TOKENS) {
-        float s[R];
-        uint32_t seen;
-        const float all = load_scores<DT, LANES, R>(a, pieces, t, lane, s, seen), scale = all > 0.0f ? 1.0f / all : 0.0f;
-        float dot = 0.0f;
+    const int64_t step = (int64_t)gridDim.x * kGradientWaves * TOKENS;
+    for (int64_t t0 = ((int64_t)blockIdx.x * kGradientWaves + wave) * TOKENS + part; t0 < a.T; t0 += ONCE * step) {
+        float x[ONCE][R];
 #pragma unroll
-        for (int i = 0; i < R; ++i) dot += s[i] * scale * push[i];
-        dot = over_lanes<LANES>(dot, plus);
+        for (int u = 0; u < ONCE; ++u) load_logits<DT, LANES, R>(a, pieces, min(t0 + u * step, a.T - 1), lane, x[u]);
 #pragma unroll
-        for (int q = 0; q < R / 4; ++q) {
-            const int e = expert_at<LANES>(lane, 4 * q);
-            float d[4];
+        for (int u = 0; u < ONCE; ++u) {
+            const int64_t t = t0 + u * step;
+            float s[R];
+            uint32_t seen;
+            const float all = scores_of<LANES, R>(a, lane, x[u], s, seen), scale = all > 0.0f ? 1.0f / all : 0.0f;
+            float dot = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int j = 4 * q + i;
-                d[i] = seen >> j & 1 ? times * (s[j] * scale * (push[j] - dot) * (a.softmax ? 1.0f : 1.0f - s[j])) : 0.0f;
-            }
-            if (add_pieces) {
-                if (e >= a.E) continue;
-                if (a.add) {
-                    const Four<DT> four = *reinterpret_cast<const Four<DT> *>(static_cast<const char *>(a.add) + (t * a.lda + e) * elem_size(DT));
+            for (int i = 0; i < R; ++i) dot += s[i] * scale * push[i];
+            dot = over_token<LANES>(dot, plus);
+            if (t >= a.T) continue;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) d[i] += widen_at<DT>(four.bytes, i);
+            for (int q = 0; q < R / 4; ++q) {
+                const int e = expert_at<LANES>(lane, 4 * q);
+                float d[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = 4 * q + i;
+                    d[i] = seen >> j & 1 ? times * (s[j] * scale * (push[j] - dot) * (a.softmax ? 1.0f : 1.0f - s[j])) : 0.0f;
                 }
-                store_run<DT>(a.gradient, t * a.ldd + e, d);
-            } else {
+                if (add_pieces) {
+                    if (e >= a.E) continue;
+                    if (a.add) {
+                        const Four<DT> four = *reinterpret_cast<const Four<DT> *>(static_cast<const char *>(a.add) + (t * a.lda + e) * elem_size(DT));
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (e + i < a.E) store_as<DT>(a.gradient, t * a.ldd + e + i, a.add ? d[i] + widen_at<DT>(a.add, t * a.lda + e + i) : d[i]);
+                        for (int i = 0; i < 4; ++i) d[i] += widen_at<DT>(four.bytes, i);
+                    }
+                    store_run<DT>(a.gradient, t * a.ldd + e, d);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (e + i < a.E) store_as<DT>(a.gradient, t * a.ldd + e + i, a.add ? d[i] + widen_at<DT>(a.add, t * a.lda + e + i) : d[i]);
+                }
             }
         }
     }
 }
 
+// Lanes that share a token, and how many experts they have room for.
+constexpr int lanes_of(int E) { return E <= 16 ? 4 : E <= 64 ? 16 : 64; }
+constexpr int slots_of(int E) { return E <= 16 ? 16 : E <= 64 ? 64 : E <= 256 ? 256 : 1024; }
+
+// One workgroup while that has 32 experts' places to a thread or fewer (512 tokens of 8 experts: see the table of measurements).
 int64_t groups_of(int64_t T, int E)
 {
-    const int64_t tokens = kWaves * (E <= 64 ? 4 : 1);
-    return std::min(std::max(ceil_div(T, tokens), (int64_t)1), (int64_t)device_info().cus);
+    if (T * slots_of(E) <= 32 * kThreads) return 1;
+    return std::min(ceil_div(T, (int64_t)(kWaves * (64 / lanes_of(E)))), (int64_t)device_info().cus);
 }
 
 // Rows that can be read and written four at a time.
@@ -276,15 +357,19 @@ int launch_as(const BalanceArgs &a, void *workspace, hipStream_t stream)
 {
     const bool pieces = fours(a.logits, a.ldl, a.E, DT);
     if (a.gradient) {
-        const int64_t groups = std::min(ceil_div(a.T, (int64_t)(kWaves * (64 / LANES))), (int64_t)device_info().cus * 4);
+        const int64_t groups = std::min(ceil_div(a.T, (int64_t)(kGradientWaves * (64 / LANES))), (int64_t)device_info().cus * 8);
         note_kernel("balance_gradient_kernel", __PRETTY_FUNCTION__);
-        hipLaunchKernelGGL((balance_gradient_kernel<DT, LANES, R>), dim3((unsigned)groups), dim3(kThreads), 0, stream, a, pieces,
+        hipLaunchKernelGGL((balance_gradient_kernel<DT, LANES, R>), dim3((unsigned)groups), dim3(kGradientWaves * 64), 0, stream, a, pieces,
                            a.E % 4 == 0 && (!a.add || fours(a.add, a.lda, a.E, DT)));
         return check_hip(hipGetLastError(), "launch balance_gradient_kernel");
     }
     const int64_t groups = groups_of(a.T, a.E);
     note_kernel("balance_kernel", __PRETTY_FUNCTION__);
-    hipLaunchKernelGGL((balance_kernel<DT, LANES, R>), dim3((unsigned)groups), dim3(kThreads), 0, stream, a, workspace, pieces);
+    if (groups == 1) {
+        hipLaunchKernelGGL((balance_kernel<DT, LANES, R, true>), dim3(1), dim3(kThreads), 0, stream, a, workspace, pieces);
+        return check_hip(hipGetLastError(), "launch balance_kernel");
+    }
+    hipLaunchKernelGGL((balance_kernel<DT, LANES, R, false>), dim3((unsigned)groups), dim3(kThreads), 0, stream, a, workspace, pieces);
     hipLaunchKernelGGL(balance_sum_kernel, dim3((unsigned)ceil_div(a.E, kSlice)), dim3(1024), 0, stream, a, workspace, (int)groups);
     return check_hip(hipGetLastError(), "launch balance_kernel");
 }
@@ -292,6 +377,7 @@ int launch_as(const BalanceArgs &a, void *workspace, hipStream_t stream)
 template <int DT>
 int launch_of(const BalanceArgs &a, void *workspace, hipStream_t stream)
 {
+    if (a.E <= 16) return launch_as<DT, 4, 4>(a, workspace, stream);
     if (a.E <= 64) return launch_as<DT, 16, 4>(a, workspace, stream);
     if (a.E <= 256) return launch_as<DT, 64, 4>(a, workspace, stream);
     return launch_as<DT, 64, 16>(a, workspace, stream);

@@ -56,24 +56,25 @@ __global__ __launch_bounds__(WAVES * 64) void integer_few_kernel(IntegerArgs p, 
 #pragma unroll
             for (int t = 0; t < NT; ++t) b[d][t] = load_piece(row_b[t], min(kb0 + d * WAVES, blocks - 1), g, p.K);
     };
-    if (wave < blocks) load(wave);
-
     const int stride = (int)blocks * kBlock + 16;
     if constexpr (ROUND) {
-        // sixteen lanes to 128 values of a row: the largest of all first
+        // Sixteen lanes to 128 values of a row.  All of A is asked for at once, before B, which then comes while A is rounded.
+        constexpr int ONCE = kInside / kBlock / (WAVES * 4);          // turns of the workgroup, of which few rows need few
         const int units = (int)(p.M * blocks);
-        Raw<AT> kept;
         auto read = [&](int unit, int &row, int &k) INLINE_LAMBDA {
             row = unit / (int)blocks;
             k = unit % (int)blocks * kBlock + r16 * 8;
             return load_raw<AT>(p.a, row * p.lda, k, p.K);
         };
+        Raw<AT> kept[ONCE];
+        int rows[ONCE], ks[ONCE];
+#pragma unroll
+        for (int u = 0; u < ONCE; ++u)
+            if (u * WAVES * 4 < units) kept[u] = read(min((int)threadIdx.x / 16 + u * WAVES * 4, units - 1), rows[u], ks[u]);
         if ((int)threadIdx.x < kInsideRows) tops[threadIdx.x] = 0;
+        if (wave < blocks) load(wave);
         __syncthreads();
-        for (int unit = threadIdx.x / 16; unit < units; unit += WAVES * 4) {
-            int row, k;
-            const Raw<AT> raw = read(unit, row, k);
-            if (unit < WAVES * 4) kept = raw;
+        auto largest = [&](const Raw<AT> &raw, int row) INLINE_LAMBDA {
             float v[8];
             widen<AT>(raw, v);
             uint32_t top = 0;
@@ -81,18 +82,23 @@ __global__ __launch_bounds__(WAVES * 64) void integer_few_kernel(IntegerArgs p, 
             for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);      // (those of a neighbour's piece do no harm)
             top = row16_max(top);
             if (r16 == 0) atomicMax(&tops[row], top);
-        }
-        __syncthreads();
-        for (int unit = threadIdx.x / 16; unit < units; unit += WAVES * 4) {
-            int row, k;
-            Raw<AT> raw = read(unit, row, k);
-            if (unit < WAVES * 4) raw = kept;
+        };
+        auto round = [&](const Raw<AT> &raw, int row, int k) INLINE_LAMBDA {
             const float s = integer_scale(tops[row]), inv = 1.0f / s;
             float v[8];
             widen<AT>(raw, v);
             *reinterpret_cast<uint2 *>(rounded + row * stride + k) = in_place(pack8_integers(v, s, inv), before_column(k, p.K));
-        }
+        };
+#pragma unroll
+        for (int u = 0; u < ONCE; ++u)
+            if (u * WAVES * 4 < units && (int)threadIdx.x / 16 + u * WAVES * 4 < units) largest(kept[u], rows[u]);
         __syncthreads();
+#pragma unroll
+        for (int u = 0; u < ONCE; ++u)
+            if (u * WAVES * 4 < units && (int)threadIdx.x / 16 + u * WAVES * 4 < units) round(kept[u], rows[u], ks[u]);
+        __syncthreads();
+    } else {
+        if (wave < blocks) load(wave);
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) {

@@ -56,8 +56,12 @@ __device__ __forceinline__ void load_parameters(const void *p, int dtype, int at
 constexpr int rows_at_once(int waves) { return waves == 1 ? 4 : 1; }      // rows to a workgroup
 constexpr int threads_of(int waves) { return waves == 1 ? 256 : waves * 64; }
 
+// Whether element i of a piece is counted here and not by a neighbour.  WHOLE: rows are whole pieces, of which all or none is (16 operations fewer to a piece).
+template <bool WHOLE>
+__device__ __forceinline__ bool counts(const Place &p, int i) { return WHOLE ? p.skip == 0 : i >= p.skip; }
+
 // NORM: normalised; else as they are (to integers).  Rows of 8 to WAVES * PER * 512 elements.
-template <int XT, int OT, bool NORM, int WAVES, int PER>
+template <int XT, int OT, bool NORM, int WAVES, int PER, bool WHOLE>
 __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
 {
     __shared__ float sums[2][WAVES];
@@ -90,7 +94,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
 #pragma unroll
             for (int p = 0; p < PER; ++p)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += i >= place[p].skip ? v[p][i] : 0.0f;
+                for (int i = 0; i < 8; ++i) sum += counts<WHOLE>(place[p], i) ? v[p][i] : 0.0f;
             const float mean = over_row<WAVES>(sum, sums[0], plus) / (float)n;
             float squares = 0.0f;
 #pragma unroll
@@ -98,7 +102,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     v[p][i] -= mean;
-                    squares += i >= place[p].skip ? v[p][i] * v[p][i] : 0.0f;
+                    squares += counts<WHOLE>(place[p], i) ? v[p][i] * v[p][i] : 0.0f;
                 }
             const float rstd = 1.0f / sqrtf(over_row<WAVES>(squares, sums[1], plus) / (float)n + a.eps);
             if (a.mean && threadIdx.x % (WAVES * 64) == 0) {
@@ -183,9 +187,12 @@ __global__ __launch_bounds__(1024) void rows_any_kernel(RowsArgs a)
 template <int XT, int OT, bool NORM, int WAVES, int PER>
 int launch_rows_as(const RowsArgs &a, hipStream_t stream)
 {
+    const bool whole = NORM && a.n % 8 == 0;
     const int64_t groups = ceil_div(a.rows, (int64_t)rows_at_once(WAVES)), most = (int64_t)device_info().cus * (WAVES == 1 ? 8 : 32 / WAVES);
     note_kernel("rows_kernel", __PRETTY_FUNCTION__);
-    hipLaunchKernelGGL((rows_kernel<XT, OT, NORM, WAVES, PER>), dim3((unsigned)std::min(groups, most)), dim3(threads_of(WAVES)), 0, stream, a);
+    const dim3 grid((unsigned)std::min(groups, most)), block(threads_of(WAVES));
+    if (whole) hipLaunchKernelGGL((rows_kernel<XT, OT, NORM, WAVES, PER, NORM>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((rows_kernel<XT, OT, NORM, WAVES, PER, false>), grid, block, 0, stream, a);
     return check_hip(hipGetLastError(), "launch rows_kernel");
 }
 
@@ -208,7 +215,7 @@ int launch_rows(const RowsArgs &a, hipStream_t stream)
 // --------------------------------------------------------------------------------------------------------------- the gradient
 
 // dx row by row, and of all rows that a workgroup takes the sums of g h and g for its lanes' columns; partial is [2][gridDim.x][n].
-template <int GT, int XT, int WAVES, int PER, bool SUMS>
+template <int GT, int XT, int WAVES, int PER, bool SUMS, bool WHOLE>
 __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGradientArgs a)
 {
     constexpr int ROWS = rows_at_once(WAVES);
@@ -235,9 +242,12 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGr
             raw_g[p] = load_raw<GT>(a.g, row * a.ldg, place[p].at, n);
         }
     };
-    if (first < a.rows) load(first);
+    // (4 pieces to a lane leave no registers for the next row beside them)
+    constexpr bool AHEAD = PER < 4;
+    if (AHEAD && first < a.rows) load(first);
     int turn = 0;
     for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
+        if constexpr (!AHEAD) load(row);
         float h[PER][8], g[PER][8];
         const float r = rstd;
         float su = 0.0f, suh = 0.0f;
@@ -253,12 +263,11 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGr
                     dbias[p][i] += g[p][i];
                 }
                 g[p][i] *= weight[p][i];
-                const float u = i >= place[p].skip ? g[p][i] : 0.0f;
-                su += u;
-                suh += i >= place[p].skip ? u * h[p][i] : 0.0f;
+                su += counts<WHOLE>(place[p], i) ? g[p][i] : 0.0f;
+                suh += counts<WHOLE>(place[p], i) ? g[p][i] * h[p][i] : 0.0f;
             }
         }
-        if (row + step < a.rows) load(row + step);
+        if (AHEAD && row + step < a.rows) load(row + step);
         if (!a.dx) continue;
         su = over_lanes<64>(su, plus);
         suh = over_lanes<64>(suh, plus);
@@ -354,21 +363,23 @@ __global__ __launch_bounds__(256) void norm_sums_any_kernel(NormGradientArgs a)
     a.partial[(gridDim.y + blockIdx.y) * a.n + c] = dbias;
 }
 
-// Sums of `parts` rows of partial sums (none: 0): 64 columns to a workgroup, its 16 wavefronts take every 16th row.  blockIdx.y: weight or bias.
+// Sums of `parts` rows of partial sums (none: 0): 32 columns to a workgroup, its 32 runs of 32 lanes take every 32nd row.  blockIdx.y: weight or bias.
 __global__ __launch_bounds__(1024) void column_sums_kernel(const float *partial, int64_t parts, int64_t n, float *dweight, float *dbias)
 {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    __shared__ float sums[16][32];
+    const int column = threadIdx.x % 32, run = threadIdx.x / 32;
+    const int64_t c = (int64_t)blockIdx.x * 32 + column;
     const float *from = partial + blockIdx.y * parts * n + min(c, n - 1);
     float s = 0.0f;
-#pragma unroll 4
-    for (int64_t p = wave; p < parts; p += 16) s += from[p * n];
-    sums[wave][lane] = s;
+#pragma unroll 8
+    for (int64_t p = run; p < parts; p += 32) s += from[p * n];
+    s += from_lane<32>(s);
+    if (threadIdx.x % 64 < 32) sums[threadIdx.x / 64][column] = s;
     __syncthreads();
-    if (wave == 0 && c < n) {
+    if (threadIdx.x < 32 && c < n) {
+        s = sums[0][column];
 #pragma unroll
-        for (int w = 1; w < 16; ++w) s += sums[w][lane];
+        for (int w = 1; w < 16; ++w) s += sums[w][column];
         (blockIdx.y ? dbias : dweight)[c] = s;
     }
 }
@@ -389,8 +400,9 @@ int launch_gradient_as(const NormGradientArgs &a, hipStream_t stream)
 {
     const dim3 grid((unsigned)parts_of(a.rows, a.n)), block(threads_of(WAVES));
     note_kernel("norm_gradient_kernel", __PRETTY_FUNCTION__);
-    if (a.dweight) hipLaunchKernelGGL((norm_gradient_kernel<GT, XT, WAVES, PER, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((norm_gradient_kernel<GT, XT, WAVES, PER, false>), grid, block, 0, stream, a);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
+    if (a.n % 8) a.dweight ? launch(norm_gradient_kernel<GT, XT, WAVES, PER, true, false>) : launch(norm_gradient_kernel<GT, XT, WAVES, PER, false, false>);
+    else a.dweight ? launch(norm_gradient_kernel<GT, XT, WAVES, PER, true, true>) : launch(norm_gradient_kernel<GT, XT, WAVES, PER, false, true>);
     return check_hip(hipGetLastError(), "launch norm_gradient_kernel");
 }
 
@@ -462,7 +474,7 @@ int launch_layer_norm_gradient(const NormGradientArgs &a, int gradient_dtype, in
     if (rc != MADDNESS_OK || !a.dweight) return rc;
     const int64_t parts = a.rows > 0 ? parts_of(a.rows, a.n) : 0;
     note_kernel("column_sums_kernel", nullptr);
-    hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)ceil_div(a.n, (int64_t)64), 2), dim3(1024), 0, stream, a.partial, parts, a.n, a.dweight, a.dbias);
+    hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)ceil_div(a.n, (int64_t)32), 2), dim3(1024), 0, stream, a.partial, parts, a.n, a.dweight, a.dbias);
     return check_hip(hipGetLastError(), "launch column_sums_kernel");
 }
 
