@@ -524,7 +524,7 @@ int maddness_layer_norm_gradient(const void *gradient, int32_t gradient_dtype, i
  *   push[e]   = factor E counts[e] / (n L), 0 where n or L is 0
  *   loss      = sum_e push[e] sum_t p[t][e]: factor where all experts have the same, more the less evenly they have
  * Sums over tokens are fp32 in an order that depends on the sizes only, and fp64 where those meet.  push is what the gradient takes: the counts have none.
- * workspace  maddness_balance_workspace(T, E) bytes, 8-byte aligned.
+ * workspace  maddness_balance_workspace(T, E) bytes, 8-byte aligned (NULL where that is 0).
  *
  * maddness_balance_gradient: gradient[t][e] of logits [T][ldl], times loss_gradient[0] (NULL: 1), plus add[t][e] ([T][lda] of `dtype`, or NULL;
  * it may be `gradient` itself): in fp32, rounded once to `dtype`.  0 (plus add) for a masked logit.

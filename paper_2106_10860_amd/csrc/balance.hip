@@ -395,6 +395,7 @@ int launch(const BalanceArgs &a, int dtype, void *workspace, hipStream_t stream)
 size_t balance_workspace_bytes(int64_t T, int E)
 {
     const int64_t groups = groups_of(T, E);
+    if (groups == 1) return 0;
     return (size_t)(kMostSlices * 8 + 8 + groups * 8 + groups * E * 8);
 }
 

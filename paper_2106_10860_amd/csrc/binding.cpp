@@ -963,11 +963,12 @@ PyObject *balance(PyObject *, PyObject *const *a, Py_ssize_t n)
         const auto floats = at::TensorOptions().dtype(at::kFloat).device(x.device());
         const size_t bytes = maddness_balance_workspace(r.rows, E);
         at::Tensor loss = at::empty({}, floats), counts = at::empty({E}, floats.dtype(at::kInt)), push = at::empty({E}, floats);
-        at::Tensor work = at::empty({(int64_t)bytes}, floats.dtype(at::kByte));
+        at::Tensor work;
+        if (bytes) work = at::empty({(int64_t)bytes}, floats.dtype(at::kByte));
         const void *x_p = x.data_ptr();
         float *loss_p = static_cast<float *>(loss.data_ptr()), *push_p = static_cast<float *>(push.data_ptr());
         int32_t *counts_p = static_cast<int32_t *>(counts.data_ptr());
-        void *work_p = work.data_ptr();
+        void *work_p = bytes ? work.data_ptr() : nullptr;
         int rc;
         Py_BEGIN_ALLOW_THREADS
         rc = maddness_balance(x_p, code, r.rows, E, r.ld, sigmoid ? MADDNESS_SIGMOID : MADDNESS_SOFTMAX, ids_p, k, factor, loss_p, counts_p, push_p, work_p,

@@ -7,33 +7,66 @@
 namespace maddness {
 namespace {
 
-constexpr int kTensors = 96, kThreads = 256;
+constexpr int kThreads = 256;
+// Tensors to a launch: a table of them is read anew by every launch, entry after entry of a search where it is long; a short one comes at once.
+constexpr int kFewTensors = 8, kManyTensors = 96;
 // Elements that a workgroup takes at a time: eight pieces of 8 to a thread, or one where the elements would otherwise leave compute units without work (a
 // million in 4 tensors: norm and scaling 4.1 and 6.2 us with eight, 3.6 and 5.3 with one).
 constexpr int kMany = 8;
 constexpr int chunk_of(int pieces) { return kThreads * 8 * pieces; }
 
+template <int N>
 struct Table {
-    const void *data[kTensors];
-    void *out[kTensors];
-    int64_t count[kTensors];
-    uint32_t end[kTensors];             // chunks of the tensors up to and with this one
-    uint8_t types[kTensors];            // of data + 4 times that of out
-    int n;
+    const void *data[N];
+    void *out[N];
+    int64_t count[N];
+    uint32_t end[N];                    // chunks of the tensors up to and with this one; of those that are not there, of all
+    uint8_t types[N];                   // of data + 4 times that of out
+    uint32_t chunks;
 };
 
-// The tensor that a chunk belongs to, and the chunk's first element.
-template <int PIECES>
-__device__ __forceinline__ int tensor_of(const Table &t, uint32_t chunk, int64_t &first)
+// The tensor that a chunk belongs to.
+struct Entry {
+    const void *data;
+    void *out;
+    int64_t count, first;               // its elements, and the chunk's first one
+    int types;
+};
+
+template <int PIECES, int N>
+__device__ __forceinline__ Entry entry_of(const Table<N> &t, uint32_t chunk)
 {
-    int lo = 0, hi = t.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (chunk < t.end[mid]) hi = mid;
-        else lo = mid + 1;
+    Entry e;
+    uint32_t before;
+    if constexpr (N == kFewTensors) {
+        // (all of it in registers: no load waits for another)
+        e = Entry{t.data[0], t.out[0], t.count[0], 0, t.types[0]};
+        before = 0;
+#pragma unroll
+        for (int i = 1; i < N; ++i) {
+            const bool later = chunk >= t.end[i - 1];
+            const void *data = t.data[i];
+            void *out = t.out[i];
+            const int64_t count = t.count[i];
+            const int types = t.types[i];
+            e.data = later ? data : e.data;
+            e.out = later ? out : e.out;
+            e.count = later ? count : e.count;
+            e.types = later ? types : e.types;
+            before = later ? t.end[i - 1] : before;
+        }
+    } else {
+        int lo = 0, hi = N - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (chunk < t.end[mid]) hi = mid;
+            else lo = mid + 1;
+        }
+        e = Entry{t.data[lo], t.out[lo], t.count[lo], 0, t.types[lo]};
+        before = lo ? t.end[lo - 1] : 0;
     }
-    first = (int64_t)(chunk - (lo ? t.end[lo - 1] : 0)) * chunk_of(PIECES);
-    return lo;
+    e.first = (int64_t)(chunk - before) * chunk_of(PIECES);
+    return e;
 }
 
 // The sum over the workgroup's threads, in all of them.
@@ -72,19 +105,17 @@ __device__ __forceinline__ void add_squares(const void *data, int64_t first, int
 }
 
 // Sums of squares of a launch's tensors: to partials[workgroup], or in addition to what is there.
-template <int PIECES>
-__global__ __launch_bounds__(kThreads) void squares_kernel(Table t, double *partials, bool add)
+template <int PIECES, int N>
+__global__ __launch_bounds__(kThreads) void squares_kernel(Table<N> t, double *partials, bool add)
 {
     __shared__ double slots[kThreads / 64];
     double sums[2] = {};
-    const uint32_t chunks = t.n ? t.end[t.n - 1] : 0;
-    for (uint32_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
-        int64_t first;
-        const int i = tensor_of<PIECES>(t, chunk, first);
-        switch (t.types[i] & 3) {
-        case kF32: add_squares<kF32, PIECES>(t.data[i], first, t.count[i], sums); break;
-        case kF16: add_squares<kF16, PIECES>(t.data[i], first, t.count[i], sums); break;
-        default: add_squares<kBF16, PIECES>(t.data[i], first, t.count[i], sums);
+    for (uint32_t chunk = blockIdx.x; chunk < t.chunks; chunk += gridDim.x) {
+        const Entry e = entry_of<PIECES>(t, chunk);
+        switch (e.types & 3) {
+        case kF32: add_squares<kF32, PIECES>(e.data, e.first, e.count, sums); break;
+        case kF16: add_squares<kF16, PIECES>(e.data, e.first, e.count, sums); break;
+        default: add_squares<kBF16, PIECES>(e.data, e.first, e.count, sums);
         }
     }
     const double sum = group_sum(sums[0] + sums[1], slots);
@@ -105,81 +136,71 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const double *partials, 
     if (threadIdx.x == 0) *norm = all;
 }
 
-// A whole chunk's pieces as they are in memory.
-template <int PIECES>
-struct Chunk {
-    uint32_t w[PIECES][8];
+// Eight elements as they are in memory, of a narrow type in the first half.
+struct Piece {
+    i32x4 lo, hi;
 };
 
-template <int DT, int PIECES>
-__device__ __forceinline__ void load_chunk(const void *data, int64_t first, int64_t count, Chunk<PIECES> &c)
+template <int DT>
+__device__ __forceinline__ Piece load_piece(const void *data, int64_t at)
 {
-#pragma unroll
-    for (int p = 0; p < PIECES; ++p) {
-        const Raw<DT> raw = load_raw<DT>(data, first, (int64_t)(p * kThreads + threadIdx.x) * 8, count);
-#pragma unroll
-        for (int i = 0; i < 2 * elem_size(DT); ++i) c.w[p][i] = raw.w[i];
-    }
+    using words = __attribute__((ext_vector_type(4), aligned(elem_size(DT)))) int;
+    const words *from = reinterpret_cast<const words *>(static_cast<const char *>(data) + at * elem_size(DT));
+    if constexpr (DT == kF32) return Piece{from[0], from[1]};
+    else return Piece{from[0], i32x4{}};
 }
 
-// (One piece has been asked for before the norm was known; of more the first to come is scaled while the others do.)
+template <int DT, int OT>
+__device__ __forceinline__ void scale_piece(const Piece &piece, void *out, int64_t at, float factor)
+{
+    Raw<DT> raw;
+#pragma unroll
+    for (int i = 0; i < 2 * elem_size(DT); ++i) raw.w[i] = (uint32_t)(i < 4 ? piece.lo[i] : piece.hi[i % 4]);
+    float v[8];
+    widen<DT>(raw, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= factor;
+    store_run<OT>(out, at, v);
+}
+
+// (One piece has been asked for before the norm was known.)
 template <int DT, int OT, int PIECES>
-__device__ __forceinline__ void scale_chunk(const Chunk<PIECES> &asked, bool whole, const void *data, void *out, int64_t first, int64_t count, float factor)
+__device__ __forceinline__ void scale_chunk(const Piece &asked, bool whole, const Entry &e, float factor)
 {
     if (whole) {
-        Chunk<PIECES> c = asked;
-        if constexpr (PIECES > 1) load_chunk<DT>(data, first, count, c);
+        const int64_t at = e.first + (int64_t)threadIdx.x * 8;
+        if constexpr (PIECES == 1) {
+            scale_piece<DT, OT>(asked, e.out, at, factor);
+        } else {
+            Piece pieces[PIECES];
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            Raw<DT> raw;
+            for (int p = 0; p < PIECES; ++p) pieces[p] = load_piece<DT>(e.data, at + p * kThreads * 8);
 #pragma unroll
-            for (int i = 0; i < 2 * elem_size(DT); ++i) raw.w[i] = c.w[p][i];
-            float v[8];
-            widen<DT>(raw, v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= factor;
-            const int64_t at = first + (int64_t)(p * kThreads + threadIdx.x) * 8;
-            store_run<OT>(out, at, v);
+            for (int p = 0; p < PIECES; ++p) scale_piece<DT, OT>(pieces[p], e.out, at + p * kThreads * 8, factor);
         }
     } else {
-        for (int64_t i = first + threadIdx.x; i < count; i += kThreads) store_as<OT>(out, i, widen_at<DT>(data, i) * factor);
+        for (int64_t i = e.first + threadIdx.x; i < e.count; i += kThreads) store_as<OT>(e.out, i, widen_at<DT>(e.data, i) * factor);
     }
-}
-
-// The chunk that a workgroup is at.
-template <int PIECES>
-struct Asked {
-    Chunk<PIECES> pieces;
-    int tensor;
-    int64_t first, count;
-    bool whole;
-};
-
-template <int PIECES>
-__device__ __forceinline__ Asked<PIECES> ask(const Table &t, uint32_t chunk)
-{
-    Asked<PIECES> a;
-    a.tensor = tensor_of<PIECES>(t, chunk, a.first);
-    a.count = t.count[a.tensor];
-    a.whole = a.first + chunk_of(PIECES) <= a.count;
-    if (PIECES == 1 && a.whole) {
-        switch (t.types[a.tensor] & 3) {
-        case kF32: load_chunk<kF32>(t.data[a.tensor], a.first, a.count, a.pieces); break;
-        case kF16: load_chunk<kF16>(t.data[a.tensor], a.first, a.count, a.pieces); break;
-        default: load_chunk<kBF16>(t.data[a.tensor], a.first, a.count, a.pieces);
-        }
-    }
-    return a;
 }
 
 // Scales a launch's tensors; the norm is that of the sums of squares, which every workgroup adds up for itself (16 KiB from L2) while its first chunk comes, or given.
-template <int PIECES>
-__global__ __launch_bounds__(kThreads) void clip_kernel(Table t, const double *partials, int parts, float *norm, bool given, float max_norm)
+template <int PIECES, int N>
+__global__ __launch_bounds__(kThreads) void clip_kernel(Table<N> t, const double *partials, int parts, float *norm, bool given, float max_norm)
 {
     __shared__ double slots[kThreads / 64];
-    const uint32_t chunks = t.n ? t.end[t.n - 1] : 0;
-    Asked<PIECES> now{};
-    if (blockIdx.x < chunks) now = ask<PIECES>(t, chunks - 1 - blockIdx.x);      // (from the end: what the sums read last may still be in the memory-side cache)
+    Piece asked{};
+    Entry now{};
+    bool whole = false;
+    auto turn_to = [&](uint32_t chunk) INLINE_LAMBDA {
+        now = entry_of<PIECES>(t, chunk);
+        whole = now.first + chunk_of(PIECES) <= now.count;
+        if (PIECES == 1 && whole) {
+            const int64_t at = now.first + (int64_t)threadIdx.x * 8;
+            if ((now.types & 3) == kF32) asked = load_piece<kF32>(now.data, at);
+            else asked = load_piece<kF16>(now.data, at);      // (bits, of either narrow type)
+        }
+    };
+    if (blockIdx.x < t.chunks) turn_to(blockIdx.x);
     float all;
     if (given) {
         all = *norm;
@@ -188,54 +209,57 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(Table t, const double *p
         if (blockIdx.x == 0 && threadIdx.x == 0) *norm = all;
     }
     const float factor = all > max_norm && all <= 3.402823466e38f ? (float)((double)max_norm / (double)all) : 1.0f;
-    for (uint32_t turn = blockIdx.x; turn < chunks;) {
-        const void *data = t.data[now.tensor];
-        void *out = t.out[now.tensor];
-        if (data != out || factor != 1.0f) {
-            switch (t.types[now.tensor]) {
-            case kF32 + 4 * kF32: scale_chunk<kF32, kF32>(now.pieces, now.whole, data, out, now.first, now.count, factor); break;
-            case kF32 + 4 * kF16: scale_chunk<kF32, kF16>(now.pieces, now.whole, data, out, now.first, now.count, factor); break;
-            case kF32 + 4 * kBF16: scale_chunk<kF32, kBF16>(now.pieces, now.whole, data, out, now.first, now.count, factor); break;
-            case kF16 + 4 * kF32: scale_chunk<kF16, kF32>(now.pieces, now.whole, data, out, now.first, now.count, factor); break;
-            case kF16 + 4 * kF16: scale_chunk<kF16, kF16>(now.pieces, now.whole, data, out, now.first, now.count, factor); break;
-            case kF16 + 4 * kBF16: scale_chunk<kF16, kBF16>(now.pieces, now.whole, data, out, now.first, now.count, factor); break;
-            case kBF16 + 4 * kF32: scale_chunk<kBF16, kF32>(now.pieces, now.whole, data, out, now.first, now.count, factor); break;
-            case kBF16 + 4 * kF16: scale_chunk<kBF16, kF16>(now.pieces, now.whole, data, out, now.first, now.count, factor); break;
-            default: scale_chunk<kBF16, kBF16>(now.pieces, now.whole, data, out, now.first, now.count, factor);
+    for (uint32_t chunk = blockIdx.x; chunk < t.chunks;) {
+        if (now.data != now.out || factor != 1.0f) {
+            switch (now.types) {
+            case kF32 + 4 * kF32: scale_chunk<kF32, kF32, PIECES>(asked, whole, now, factor); break;
+            case kF32 + 4 * kF16: scale_chunk<kF32, kF16, PIECES>(asked, whole, now, factor); break;
+            case kF32 + 4 * kBF16: scale_chunk<kF32, kBF16, PIECES>(asked, whole, now, factor); break;
+            case kF16 + 4 * kF32: scale_chunk<kF16, kF32, PIECES>(asked, whole, now, factor); break;
+            case kF16 + 4 * kF16: scale_chunk<kF16, kF16, PIECES>(asked, whole, now, factor); break;
+            case kF16 + 4 * kBF16: scale_chunk<kF16, kBF16, PIECES>(asked, whole, now, factor); break;
+            case kBF16 + 4 * kF32: scale_chunk<kBF16, kF32, PIECES>(asked, whole, now, factor); break;
+            case kBF16 + 4 * kF16: scale_chunk<kBF16, kF16, PIECES>(asked, whole, now, factor); break;
+            default: scale_chunk<kBF16, kBF16, PIECES>(asked, whole, now, factor);
             }
         }
-        turn += gridDim.x;
-        if (turn < chunks) now = ask<PIECES>(t, chunks - 1 - turn);
+        chunk += gridDim.x;
+        if (chunk < t.chunks) turn_to(chunk);
     }
 }
 
-// The next tensors from `from` on that have elements, up to a launch's number of them and 2^32 - 1 chunks.
-Table next_table(const maddness_tensor *tensors, int64_t n, int64_t chunk, int64_t &from, bool outs)
+// The next tensors from `from` on that have elements, up to a table's number of them and 2^32 - 1 chunks.
+template <int N>
+Table<N> next_table(const maddness_tensor *tensors, int64_t n, int64_t chunk, int64_t &from, bool outs)
 {
-    Table t;
-    t.n = 0;
+    Table<N> t{};
     uint64_t chunks = 0;
-    for (; from < n && t.n < kTensors; ++from) {
+    int entries = 0;
+    for (; from < n && entries < N; ++from) {
         const maddness_tensor &one = tensors[from];
         if (one.count == 0) continue;
-        chunks += (uint64_t)ceil_div(one.count, chunk);
-        if (chunks > 0xffffffffu) break;
-        t.data[t.n] = one.data;
-        t.out[t.n] = outs ? one.out : nullptr;
-        t.count[t.n] = one.count;
-        t.end[t.n] = (uint32_t)chunks;
-        t.types[t.n] = (uint8_t)(one.dtype + 4 * (outs ? one.out_dtype : 0));
-        ++t.n;
+        const uint64_t more = (uint64_t)ceil_div(one.count, chunk);
+        if (chunks + more > 0xffffffffu) break;
+        chunks += more;
+        t.data[entries] = one.data;
+        t.out[entries] = outs ? one.out : nullptr;
+        t.count[entries] = one.count;
+        t.end[entries] = (uint32_t)chunks;
+        t.types[entries] = (uint8_t)(one.dtype + 4 * (outs ? one.out_dtype : 0));
+        ++entries;
     }
+    for (; entries < N; ++entries) t.end[entries] = (uint32_t)chunks;
+    t.chunks = (uint32_t)chunks;
     return t;
 }
 
 unsigned groups_of(uint64_t chunks) { return (unsigned)std::max<uint64_t>(1, std::min<uint64_t>(chunks, kNormPartials)); }
 
-// How the tensors are cut: pieces to a thread, and chunks of that size in all.
+// How the tensors are cut: pieces to a thread, chunks of that size in all, and whether a short table holds them.
 struct Cut {
     int pieces;
     uint64_t chunks;
+    bool few_tensors;
     Cut(const maddness_tensor *tensors, int64_t n)
     {
         uint64_t few = 0, many = 0;
@@ -245,24 +269,53 @@ struct Cut {
         }
         pieces = few <= kNormPartials ? 1 : kMany;
         chunks = pieces == 1 ? few : many;
+        few_tensors = n <= kFewTensors;
     }
 };
+
+// Launches f with a table after the other: at least once.
+template <int N, typename F>
+int for_tables(const maddness_tensor *tensors, int64_t n, int pieces, bool outs, F f)
+{
+    int64_t from = 0;
+    do {
+        const Table<N> t = next_table<N>(tensors, n, chunk_of(pieces), from, outs);
+        f(t);
+        const int rc = check_hip(hipGetLastError(), outs ? "launch clip_kernel" : "launch squares_kernel");
+        if (rc != MADDNESS_OK) return rc;
+    } while (from < n);
+    return MADDNESS_OK;
+}
+
+template <int PIECES, int N>
+int launch_squares_as(const maddness_tensor *tensors, int64_t n, double *partials, int parts, hipStream_t stream)
+{
+    bool add = false;
+    return for_tables<N>(tensors, n, PIECES, false, [&](const Table<N> &t) {
+        hipLaunchKernelGGL((squares_kernel<PIECES, N>), dim3((unsigned)parts), dim3(kThreads), 0, stream, t, partials, add);
+        add = true;
+    });
+}
+
+template <int PIECES, int N>
+int launch_clip_as(const maddness_tensor *tensors, int64_t n, const double *partials, int parts, float *norm, bool given, float max_norm, hipStream_t stream)
+{
+    return for_tables<N>(tensors, n, PIECES, true, [&](const Table<N> &t) {
+        if (t.chunks == 0 && given) return;
+        hipLaunchKernelGGL((clip_kernel<PIECES, N>), dim3(groups_of(t.chunks)), dim3(kThreads), 0, stream, t, partials, parts, norm, given, max_norm);
+    });
+}
 
 // All sums of squares; how many of the partials hold them.
 int launch_squares(const maddness_tensor *tensors, int64_t n, const Cut &cut, double *partials, int &parts, hipStream_t stream)
 {
     parts = (int)groups_of(cut.chunks);
-    int64_t from = 0;
-    bool add = false;
-    do {
-        const Table t = next_table(tensors, n, chunk_of(cut.pieces), from, false);
-        const auto kernel = cut.pieces == 1 ? squares_kernel<1> : squares_kernel<kMany>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)parts), dim3(kThreads), 0, stream, t, partials, add);
-        const int rc = check_hip(hipGetLastError(), "launch squares_kernel");
-        if (rc != MADDNESS_OK) return rc;
-        add = true;
-    } while (from < n);
-    return MADDNESS_OK;
+    if (cut.few_tensors) {
+        if (cut.pieces == 1) return launch_squares_as<1, kFewTensors>(tensors, n, partials, parts, stream);
+        return launch_squares_as<kMany, kFewTensors>(tensors, n, partials, parts, stream);
+    }
+    if (cut.pieces == 1) return launch_squares_as<1, kManyTensors>(tensors, n, partials, parts, stream);
+    return launch_squares_as<kMany, kManyTensors>(tensors, n, partials, parts, stream);
 }
 
 }  // namespace
@@ -283,15 +336,12 @@ int launch_clip(const maddness_tensor *tensors, int64_t n, float max_norm, float
     int parts = 0, rc;
     note_kernel(given ? "clip_kernel" : "squares_kernel", nullptr);
     if (!given && (rc = launch_squares(tensors, n, cut, partials, parts, stream)) != MADDNESS_OK) return rc;
-    int64_t from = 0;
-    do {
-        const Table t = next_table(tensors, n, chunk_of(cut.pieces), from, true);
-        if (t.n == 0 && given) break;
-        const auto kernel = cut.pieces == 1 ? clip_kernel<1> : clip_kernel<kMany>;
-        hipLaunchKernelGGL(kernel, dim3(groups_of(t.n ? t.end[t.n - 1] : 0)), dim3(kThreads), 0, stream, t, partials, parts, norm, given, max_norm);
-        if ((rc = check_hip(hipGetLastError(), "launch clip_kernel")) != MADDNESS_OK) return rc;
-    } while (from < n);
-    return MADDNESS_OK;
+    if (cut.few_tensors) {
+        if (cut.pieces == 1) return launch_clip_as<1, kFewTensors>(tensors, n, partials, parts, norm, given, max_norm, stream);
+        return launch_clip_as<kMany, kFewTensors>(tensors, n, partials, parts, norm, given, max_norm, stream);
+    }
+    if (cut.pieces == 1) return launch_clip_as<1, kManyTensors>(tensors, n, partials, parts, norm, given, max_norm, stream);
+    return launch_clip_as<kMany, kManyTensors>(tensors, n, partials, parts, norm, given, max_norm, stream);
 }
 
 }  // namespace maddness

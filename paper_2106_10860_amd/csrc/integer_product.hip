@@ -30,48 +30,52 @@ __device__ __forceinline__ float scaled(int32_t sum, float scale_a, float scale_
     return bias ? v + bias[n] : v;
 }
 
-// Whether A's rows are rounded within the few-rows kernel, by every workgroup for itself: while they fill 32 KiB of LDS at most.
-constexpr int64_t kInside = 32768, kInsideRows = 64;
+// Whether A's rows are rounded within the few-rows kernel, by every workgroup for its own 32 at most: while they fill 16 KiB of LDS, which costs 1 us (one row of
+// 4096) to 3.7 (16 of 1024); a launch of its own costs 3.9 (8 rows of 4096: 6.5 within the kernel).
+constexpr int64_t kInside = 16384, kInsideRows = 32, kMostInside = 64;
 
-// Few rows: 16 MT rows by 16 NT columns to a workgroup; its wavefronts take every WAVES-th block of 128 of the sum, DEPTH of them asked for
+// Few rows: 16 MT rows by 16 NT columns to a workgroup; its wavefronts take every WAVES-th block of 128 of the sum, up to DEPTH of them asked for
 // at once, and add up in LDS.  B comes straight from memory, in pieces of 32 bytes to a lane, and so does an 8-bit A; a floating A is rounded into
-// LDS while the first of B is on its way.
+// LDS while the first of B is on its way.  (One row through 4096 x 4096, other matrices from call to call: 6.2 us with four blocks at once, 6.7 with one.)
 template <int AT, int MT, int NT, int WAVES, int DEPTH, int OUT>
 __global__ __launch_bounds__(WAVES * 64) void integer_few_kernel(IntegerArgs p, uint32_t col_tiles)
 {
     constexpr bool ROUND = AT != kI8;
     __shared__ i32x4 sums[WAVES][MT * NT][64];
     __shared__ __attribute__((aligned(16))) int8_t rounded[ROUND ? kInside + kInsideRows * 16 : 16];
-    __shared__ uint32_t tops[kInsideRows];
+    __shared__ uint32_t tops[MT * 16];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, r16 = lane % 16, g = lane / 16;
     const int64_t n0 = (int64_t)(blockIdx.x % col_tiles) * (16 * NT), first = (int64_t)(blockIdx.x / col_tiles) * (16 * MT), last = min(first + 16 * MT, p.M);
     const int64_t blocks = ceil_div(p.K, (int64_t)kBlock);
     const int8_t *row_b[NT], *row_a[MT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) row_b[t] = p.b + min(n0 + t * 16 + r16, p.N - 1) * p.ldb;
-    Piece b[DEPTH][NT], a[DEPTH][MT];
+    Piece b[DEPTH][NT];
     auto load = [&](int64_t kb0) INLINE_LAMBDA {
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d)
+        for (int d = 0; d < DEPTH; ++d) {
+            if (kb0 + d * WAVES >= blocks) break;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) b[d][t] = load_piece(row_b[t], min(kb0 + d * WAVES, blocks - 1), g, p.K);
+            for (int t = 0; t < NT; ++t) b[d][t] = load_piece(row_b[t], kb0 + d * WAVES, g, p.K);
+        }
     };
+
     const int stride = (int)blocks * kBlock + 16;
     if constexpr (ROUND) {
         // Sixteen lanes to 128 values of a row.  All of A is asked for at once, before B, which then comes while A is rounded.
         constexpr int ONCE = kInside / kBlock / (WAVES * 4);          // turns of the workgroup, of which few rows need few
-        const int units = (int)(p.M * blocks);
+        const int units = (int)((last - first) * blocks);
         auto read = [&](int unit, int &row, int &k) INLINE_LAMBDA {
             row = unit / (int)blocks;
             k = unit % (int)blocks * kBlock + r16 * 8;
-            return load_raw<AT>(p.a, row * p.lda, k, p.K);
+            return load_raw<AT>(p.a, (first + row) * p.lda, k, p.K);
         };
         Raw<AT> kept[ONCE];
         int rows[ONCE], ks[ONCE];
 #pragma unroll
         for (int u = 0; u < ONCE; ++u)
             if (u * WAVES * 4 < units) kept[u] = read(min((int)threadIdx.x / 16 + u * WAVES * 4, units - 1), rows[u], ks[u]);
-        if ((int)threadIdx.x < kInsideRows) tops[threadIdx.x] = 0;
+        if ((int)threadIdx.x < MT * 16) tops[threadIdx.x] = 0;
         if (wave < blocks) load(wave);
         __syncthreads();
         auto largest = [&](const Raw<AT> &raw, int row) INLINE_LAMBDA {
@@ -102,42 +106,39 @@ __global__ __launch_bounds__(WAVES * 64) void integer_few_kernel(IntegerArgs p, 
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        const int64_t m = min(first + t * 16 + r16, p.M - 1);
-        row_a[t] = ROUND ? rounded + m * stride : static_cast<const int8_t *>(p.a) + m * p.lda;
+        const int64_t m = min(t * 16 + r16, (int)(last - first) - 1);
+        row_a[t] = ROUND ? rounded + m * stride : static_cast<const int8_t *>(p.a) + (first + m) * p.lda;
     }
     i32x4 acc[MT][NT] = {};
     for (int64_t kb0 = wave; kb0 < blocks; kb0 += DEPTH * WAVES) {
         if (kb0 != wave) load(kb0);
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
-            const int64_t kb = min(kb0 + d * WAVES, blocks - 1);
+            const int64_t kb = kb0 + d * WAVES;
+            if (kb >= blocks) break;
+            Piece a[MT];
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 if constexpr (ROUND) {
-                    a[d][t].lo = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32);
-                    a[d][t].hi = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32 + 16);
+                    a[t].lo = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32);
+                    a[t].hi = *reinterpret_cast<const i32x4 *>(row_a[t] + kb * kBlock + g * 32 + 16);
                 } else {
-                    a[d][t] = load_piece(row_a[t], kb, g, p.K);
+                    a[t] = load_piece(row_a[t], kb, g, p.K);
                 }
             }
-        }
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            const int64_t kb = kb0 + d * WAVES;
-            if (kb >= blocks) break;
             if (!ROUND && (kb + 1) * kBlock > p.K) {          // (rounded rows end in zeros)
                 const int64_t k = kb * kBlock + g * 32;
 #pragma unroll
-                for (int t = 0; t < MT; ++t) a[d][t] = Piece{first_bytes(a[d][t].lo, p.K - k), first_bytes(a[d][t].hi, p.K - k - 16)};
+                for (int t = 0; t < MT; ++t) a[t] = Piece{first_bytes(a[t].lo, p.K - k), first_bytes(a[t].hi, p.K - k - 16)};
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = multiply(b[d][j].lo, a[d][i].lo, acc[i][j]);
+                for (int j = 0; j < NT; ++j) acc[i][j] = multiply(b[d][j].lo, a[i].lo, acc[i][j]);
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = multiply(b[d][j].hi, a[d][i].hi, acc[i][j]);
+                for (int j = 0; j < NT; ++j) acc[i][j] = multiply(b[d][j].hi, a[i].hi, acc[i][j]);
         }
     }
 #pragma unroll
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(WAVES * 64) void integer_few_kernel(IntegerArgs p, 
         int32_t s = 0;
 #pragma unroll
         for (int k = 0; k < WAVES; ++k) s += sums[k][tile][at][n % 4];
-        const float scale_a = ROUND ? integer_scale(tops[first + m]) : p.K ? p.scale_a[first + m] : 1.0f;
+        const float scale_a = ROUND ? integer_scale(tops[m]) : p.K ? p.scale_a[first + m] : 1.0f;
         store_as<OUT>(p.out, (first + m) * p.ldo + n0 + n, scaled(s, scale_a, p.scale_b[n0 + n], p.bias, n0 + n));
     }
 }
@@ -337,12 +338,17 @@ int launch_few_as(const IntegerArgs &p, hipStream_t stream)
     return check_hip(hipGetLastError(), "launch integer_few_kernel");
 }
 
+int64_t tiles_of(const IntegerArgs &p, int64_t rows, int64_t cols) { return ceil_div(p.M, rows) * ceil_div(p.N, cols); }
+
+// The smallest pieces that one workgroup to a compute unit is enough for: 32 x 4096 x 4096 by 16 x 16, 32 x 16 and 32 x 32 results 9.5, 8.1 and 10.0 us, 32 x 1024 x 4096 5.7, 7.4 and
+// 9.7, 64 x 4096 x 4096 16.6, 13.0 and 10.1.
 template <int AT, int OUT>
 int launch_few(const IntegerArgs &p, hipStream_t stream)
 {
-    if (p.M > 16) return launch_few_as<AT, OUT, 4, 2, 2>(p, stream);
-    // a wavefront's share of the sum is one block: more columns to a workgroup instead
-    return p.K <= 8 * kBlock ? launch_few_as<AT, OUT, 1, 4, 1>(p, stream) : launch_few_as<AT, OUT, 1, 1, 4>(p, stream);
+    const int64_t cus = device_info().cus;
+    if (tiles_of(p, 16, 16) <= cus || p.M <= 16) return launch_few_as<AT, OUT, 1, 1, 4>(p, stream);
+    if (tiles_of(p, 32, 16) <= cus) return launch_few_as<AT, OUT, 2, 1, 4>(p, stream);
+    return launch_few_as<AT, OUT, 2, 2, 2>(p, stream);
 }
 
 template <int OUT>
@@ -351,9 +357,14 @@ int launch_to(const IntegerArgs &p, int a_dtype, hipStream_t stream)
     if (a_dtype == MADDNESS_F32) return launch_few<kF32, OUT>(p, stream);
     if (a_dtype == MADDNESS_F16) return launch_few<kF16, OUT>(p, stream);
     if (a_dtype == MADDNESS_BF16) return launch_few<kBF16, OUT>(p, stream);
+    const int64_t cus = device_info().cus;
     const bool far = std::max(p.lda, p.ldb) > kMostStride;
-    if (far || p.M <= 64 || p.K == 0) return launch_few<kI8, OUT>(p, stream);
-    if (ceil_div(p.M, (int64_t)256) * ceil_div(p.N, (int64_t)256) >= device_info().cus) return launch_tiles<256, 256, 2, 4, OUT>(p, stream);
+    if (far || p.K == 0 || p.M <= 16 || tiles_of(p, 32, 32) <= cus) return launch_few<kI8, OUT>(p, stream);
+    // Larger tiles have less to read for each product, but need enough of them for every compute unit, and depth for their beginning and end: by 64 x 128, 128 x 128 and
+    // 256 x 256 results 512 x 4096 x 4096 takes 17.0, 19.6 and 41.6 us, 2048 x 4096 x 4096 45.9, 37.1 and 49.2, 4096 x 4096 x 4096 94, 68 and 64; 1024 x 4096 x 512 7.0, 7.5 and 14.0,
+    // 1024 x 4096 x 1024 13.3, 9.2 and 17.9; 4096 x 4096 x 256 18.1, 15.7 and 16.2, 4096 x 4096 x 1024 35.8, 32.1 and 26.0, 32768 x 1024 x 512 - , 32.2 and 35.
+    if (tiles_of(p, 64, 128) <= (p.K <= 512 ? 2 : 1) * cus) return launch_tiles<64, 128, 1, 4, OUT>(p, stream);
+    if (tiles_of(p, 256, 256) >= cus && p.K >= 1024) return launch_tiles<256, 256, 2, 4, OUT>(p, stream);
     return launch_tiles<128, 128, 2, 2, OUT>(p, stream);
 }
 
@@ -361,7 +372,7 @@ int launch_to(const IntegerArgs &p, int a_dtype, hipStream_t stream)
 
 bool integer_rounds_inside(int64_t M, int64_t K)
 {
-    return M <= kInsideRows && K >= 8 && M * round_up(K, (int64_t)kBlock) <= kInside;
+    return M <= kMostInside && K >= 8 && std::min(M, kInsideRows) * round_up(K, (int64_t)kBlock) <= kInside;
 }
 
 int launch_integer_product(const IntegerArgs &p, int a_dtype, int out_dtype, hipStream_t stream)

@@ -180,18 +180,37 @@ def test_float_rows_are_rounded_within_the_call(mad, size, dtype):
 
 
 def test_results_do_not_depend_on_other_rows(lib):
-    """The sums are exact: whatever kernel the number of rows selects, the same bits."""
+    """The sums are exact: whatever kernel the number of rows selects, the same bits, of every form that the products are built in."""
     import torch
     rng = np.random.default_rng(5)
-    A, qa, sa = integers(lib, rng, 4200, 300)
-    B, qb, sb = integers(lib, rng, 4100, 300)
-    whole = lib.maddness_integer_product(A, B)
-    kernels = {lib.maddness_last_kernel()}
-    for rows in (1, 16, 40, 64, 65, 500):
-        part = lib.maddness_integer_product(lib.IntegerMatrix(A.q[:rows], A.scale[:rows]), B)
+    A, qa, sa = integers(lib, rng, 4200, 1030)
+    B, qb, sb = integers(lib, rng, 4096, 1030)
+    for dtype in DTYPES:
+        whole = lib.maddness_integer_product(A, B, out_dtype=torch_type(dtype))
+        kernels = {lib.maddness_last_kernel()}
+        for rows in (1, 16, 32, 64, 65, 500, 1000, 2000):
+            print("case rows", rows, dtype, flush=True)
+            part = lib.maddness_integer_product(lib.IntegerMatrix(A.q[:rows], A.scale[:rows]), B, out_dtype=torch_type(dtype))
+            kernels.add(lib.maddness_last_kernel())
+            assert torch.equal(part, whole[:rows]), rows
+        assert len(kernels) == 6, kernels
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_rounded_in_every_form(lib, dtype):
+    """Rows that the few-rows kernel rounds by itself, in each of its forms, with a depth that ends inside a piece."""
+    import torch
+    rng = np.random.default_rng(6)
+    B, qb, sb = integers(lib, rng, 4096, 500)
+    x_d = dev(activations(rng, 64, 500), dtype, pad=1)
+    kernels = set()
+    for rows in (1, 16, 32, 33, 64):
+        got = lib.maddness_integer_product(x_d[:rows], B, out_dtype=torch.float32)
         kernels.add(lib.maddness_last_kernel())
-        assert torch.equal(part, whole[:rows]), rows
-    assert len(kernels) >= 4, kernels
+        q, s = ref.quantise(host(x_d[:rows]))
+        want, bound = ref.product(q, s, qb, sb)
+        check(got, want, bound, "f32", (rows, dtype))
+    assert len(kernels) == 3 and all("integer_few_kernel" in k for k in kernels), kernels
 
 
 def test_extreme_values(mad):

@@ -98,7 +98,7 @@ def test_layer_norm_refuses(mad):
 
 def test_balance_refuses(mad):
     L = mad.lib()
-    base = dict(logits=FAKE, dtype=0, T=5, E=64, ldl=64, scores=0, ids=FAKE, k=2, factor=1.0, loss=FAKE, counts=FAKE, push=FAKE, work=FAKE, size=1 << 24, stream=None)
+    base = dict(logits=FAKE, dtype=0, T=5000, E=64, ldl=64, scores=0, ids=FAKE, k=2, factor=1.0, loss=FAKE, counts=FAKE, push=FAKE, work=FAKE, size=1 << 24, stream=None)
 
     def call(**kw):
         return L.maddness_balance(*{**base, **kw}.values())
@@ -107,7 +107,7 @@ def test_balance_refuses(mad):
           (dict(dtype=3), "inval", "dtype"), (dict(ldl=63), "inval", "logits"), (dict(logits=FAKE + 2), "align", "logits"), (dict(k=0), "inval", "k"),
           (dict(T=1 << 30, k=4), "unsupported", "T k"), (dict(ids=None), "inval", "NULL"), (dict(loss=None), "inval", "NULL"), (dict(counts=FAKE + 1), "align", "counts"),
           (dict(push=FAKE + 2), "align", "push"), (dict(work=None), "unsupported", "workspace"), (dict(work=FAKE + 4), "align", "workspace"),
-          (dict(size=L.maddness_balance_workspace(5, 64) - 1), "unsupported", "workspace"))
+          (dict(size=L.maddness_balance_workspace(5000, 64) - 1), "unsupported", "workspace"))
     assert L.maddness_balance_workspace(-1, 64) == 0 and L.maddness_balance_workspace(5, 0) == 0 and L.maddness_balance_workspace(5, 2000) == 0
     base2 = dict(logits=FAKE, dtype=0, T=5, E=64, ldl=64, scores=0, push=FAKE, times=None, add=None, lda=0, out=FAKE, ldd=64, stream=None)
 
