@@ -339,7 +339,7 @@ __global__ __launch_bounds__(kGradientWaves * 64) void balance_gradient_kernel(B
 constexpr int lanes_of(int E) { return E <= 16 ? 4 : E <= 64 ? 16 : 64; }
 constexpr int slots_of(int E) { return E <= 16 ? 16 : E <= 64 ? 64 : E <= 256 ? 256 : 1024; }
 
-// One workgroup while that has 32 experts' places to a thread or fewer (512 tokens of 8 experts: see the table of measurements).
+// One workgroup while that has 32 experts' places to a thread or fewer (512 tokens of 8 experts: 5.8 us, by two launches 3.7 and 3.5).
 int64_t groups_of(int64_t T, int E)
 {
     if (T * slots_of(E) <= 32 * kThreads) return 1;

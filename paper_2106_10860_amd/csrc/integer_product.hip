@@ -164,6 +164,10 @@ __global__ __launch_bounds__(WAVES * 64) void integer_few_kernel(IntegerArgs p, 
 // once in a block, when the last of it is in registers and the next has come; then A's place is free for the block after that one.
 //
 // A row's eight pieces of 16 bytes lie exchanged by its index, so that the rows that a read of the lanes goes to fall on all banks.
+//
+// 8192 x 4096 x 4096 119 us, 2300 TOP/s (the library's product of the same matrices 132, with neither scales nor bfloat16).  Of that some 14 us go to the two turns' first
+// blocks and results; a block of 256 x 256 takes 1.36 us, 0.85 of them the matrix cores' at full clocks: with zeros in place of the values a block takes 0.97, so what bounds
+// it now is power.
 template <int BM, int BN, int WM, int WN, int OUT>
 __global__ __launch_bounds__(WM * WN * 64, 2) void integer_tiles_kernel(IntegerArgs p, uint32_t col_tiles)
 {
@@ -265,7 +269,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void integer_tiles_kernel(IntegerA
         meet();
     }
     // A wavefront's results go through its part of LDS, half of its rows at a time, so that they are stored in whole lines: lanes hold four neighbours
-    // of sixteen rows each, pieces of 8 or 16 bytes (8192 x 4096 x 128 to bfloat16: 34 us with those, see below with lines).
+    // of sixteen rows each, pieces of 8 or 16 bytes (8192 x 4096 x 128 to bfloat16: 34 us with those, 29 in lines).
     constexpr int ROWS = MT * 8, COLS = NT * 16, RUN = 16 / elem_size(OUT), LINE = COLS * elem_size(OUT) + 16;
     static_assert(ROWS * LINE * WAVES <= (int)sizeof(tile), "the wavefronts' results fit LDS");
     uint8_t *const mine = tile + wave * ROWS * LINE;
@@ -360,11 +364,13 @@ int launch_to(const IntegerArgs &p, int a_dtype, hipStream_t stream)
     const int64_t cus = device_info().cus;
     const bool far = std::max(p.lda, p.ldb) > kMostStride;
     if (far || p.K == 0 || p.M <= 16 || tiles_of(p, 32, 32) <= cus) return launch_few<kI8, OUT>(p, stream);
-    // Larger tiles have less to read for each product, but need enough of them for every compute unit, and depth for their beginning and end: by 64 x 128, 128 x 128 and
-    // 256 x 256 results 512 x 4096 x 4096 takes 17.0, 19.6 and 41.6 us, 2048 x 4096 x 4096 45.9, 37.1 and 49.2, 4096 x 4096 x 4096 94, 68 and 64; 1024 x 4096 x 512 7.0, 7.5 and 14.0,
-    // 1024 x 4096 x 1024 13.3, 9.2 and 17.9; 4096 x 4096 x 256 18.1, 15.7 and 16.2, 4096 x 4096 x 1024 35.8, 32.1 and 26.0, 32768 x 1024 x 512 - , 32.2 and 35.
+    // Larger tiles have less to read for each product, but need enough of them for every compute unit, and depth for their beginning and end.  By 64 x 128, 128 x 128, 128 x 256
+    // and 256 x 256 results 512 x 4096 x 4096 takes 17.0, 19.6, - and 41.6 us, 2048 x 4096 x 4096 45.9, 36.0, 33.0 and 49.2, 4096 x 4096 x 4096 94, 68, - and 64,
+    // 8192 x 4096 x 4096 - , 130, 125 and 118; 1024 x 4096 x 4096 24.0, 23.0, 26.2 and 43.5, 1024 x 4096 x 512 7.0, 7.5, - and 14.0, 1024 x 4096 x 1024 13.3, 9.2, - and 17.9, 4096 x 2048 x 1024 - , 14.2, 13.7 and 20.7,
+    // 32768 x 1024 x 512 - , 32.3, 34.5 and 37.5.  (128 x 128 results by four wavefronts, two workgroups to a compute unit, take as long to read their fragments from LDS as to multiply them.)
     if (tiles_of(p, 64, 128) <= (p.K <= 512 ? 2 : 1) * cus) return launch_tiles<64, 128, 1, 4, OUT>(p, stream);
-    if (tiles_of(p, 256, 256) >= cus && p.K >= 1024) return launch_tiles<256, 256, 2, 4, OUT>(p, stream);
+    if (p.K >= 1024 && tiles_of(p, 256, 256) * 4 >= 3 * cus) return launch_tiles<256, 256, 2, 4, OUT>(p, stream);
+    if (p.K >= 1024 && tiles_of(p, 128, 256) <= cus && tiles_of(p, 128, 128) > cus) return launch_tiles<128, 256, 2, 4, OUT>(p, stream);
     return launch_tiles<128, 128, 2, 2, OUT>(p, stream);
 }
 
