@@ -216,7 +216,7 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a, void *
 }
 
 // The workgroups' shares together: 16 experts to a workgroup, its 64 runs of 16 lanes take every 64th share.  The workgroup that is done last adds the
-// experts' parts of the loss up, in their order.
+// experts' parts of the loss up, a lane to each.
 __global__ __launch_bounds__(1024) void balance_sum_kernel(BalanceArgs a, void *base, int groups)
 {
     __shared__ double masses[16][kSlice];
@@ -266,18 +266,20 @@ __global__ __launch_bounds__(1024) void balance_sum_kernel(BalanceArgs a, void *
         part = push * mass;
     }
     part = over_lanes<16>(part, plus);
-    if (threadIdx.x != 0) return;
     if (gridDim.x == 1) {
-        *a.loss = (float)part;
+        if (threadIdx.x == 0) *a.loss = (float)part;
         return;
     }
-    __hip_atomic_store(&w.losses[blockIdx.x], part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const uint32_t before = __hip_atomic_fetch_add(w.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-    if (before + 1 != gridDim.x) return;
-    part = 0.0;
-#pragma unroll 1
-    for (uint32_t i = 0; i < gridDim.x; ++i) part += __hip_atomic_load(&w.losses[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    *a.loss = (float)part;
+    uint32_t before = 0;
+    if (threadIdx.x == 0) {
+        __hip_atomic_store(&w.losses[blockIdx.x], part, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        before = __hip_atomic_fetch_add(w.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if ((uint32_t)__builtin_amdgcn_readfirstlane((int)before) + 1 != gridDim.x) return;
+    static_assert(kMostSlices <= 64, "a lane to each part");
+    part = threadIdx.x < gridDim.x ? __hip_atomic_load(&w.losses[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+    part = over_lanes<64>(part, plus);
+    if (threadIdx.x == 0) *a.loss = (float)part;
 }
 
 template <int DT, int LANES, int R>

@@ -158,6 +158,27 @@ __global__ __launch_bounds__(WAVES * 64) void integer_few_kernel(IntegerArgs p, 
     }
 }
 
+// 16 bytes of results from LDS to row m of out, from column n on, as far as they are there.
+template <int OUT>
+__device__ __forceinline__ void store_line(const uint8_t *from, const IntegerArgs &p, int64_t m, int64_t n)
+{
+    constexpr int RUN = 16 / elem_size(OUT);
+    const i32x4 run = *reinterpret_cast<const i32x4 *>(from);
+    if (m >= p.M) return;
+    const int64_t to = m * p.ldo + n;
+    if (n + RUN <= p.N) {
+        struct __attribute__((packed, aligned(elem_size(OUT)))) Words { i32x4 w; };
+        reinterpret_cast<Words *>(static_cast<char *>(p.out) + to * elem_size(OUT))->w = run;
+    } else {
+#pragma unroll
+        for (int k = 0; k < RUN - 1; ++k)
+            if (n + k < p.N) {
+                if constexpr (OUT == kF32) static_cast<int32_t *>(p.out)[to + k] = run[k];
+                else static_cast<uint16_t *>(p.out)[to + k] = (uint16_t)((uint32_t)run[k / 2] >> (k % 2 * 16));
+            }
+    }
+}
+
 // Many rows: BM x BN results to a workgroup of WM x WN wavefronts, each with (BM / WM) x (BN / WN) of them in registers.  Blocks of 128 values
 // of the BM + BN rows go to LDS without passing registers: whole lines of memory, as the way from L2 takes one at a time (of half lines it brings half the bytes).  There two blocks
 // of A and three of B have a place, and a block is multiplied in two halves: the fragments of one are read while those of the other are multiplied.  So the wavefronts meet
@@ -302,20 +323,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void integer_tiles_kernel(IntegerA
 #pragma unroll
         for (int q = 0; q < ROWS * COLS / RUN / 64; ++q) {
             const int row = q * (64 * RUN / COLS) + lane / (COLS / RUN);
-            const i32x4 run = *reinterpret_cast<const i32x4 *>(mine + row * LINE + lane % (COLS / RUN) * 16);
-            if (row0 + row >= p.M) continue;
-            const int64_t to = (row0 + row) * p.ldo + col0;
-            if (col0 + RUN <= p.N) {
-                struct __attribute__((packed, aligned(elem_size(OUT)))) Words { i32x4 w; };
-                reinterpret_cast<Words *>(static_cast<char *>(p.out) + to * elem_size(OUT))->w = run;
-            } else {
-#pragma unroll
-                for (int k = 0; k < RUN - 1; ++k)
-                    if (col0 + k < p.N) {
-                        if constexpr (OUT == kF32) static_cast<int32_t *>(p.out)[to + k] = run[k];
-                        else static_cast<uint16_t *>(p.out)[to + k] = (uint16_t)((uint32_t)run[k / 2] >> (k % 2 * 16));
-                    }
-            }
+            store_line<OUT>(mine + row * LINE + lane % (COLS / RUN) * 16, p, row0 + row, col0);
         }
         wave_lds_fence();
     }
