@@ -56,9 +56,14 @@ __device__ __forceinline__ void load_parameters(const void *p, int dtype, int at
 constexpr int rows_at_once(int waves) { return waves == 1 ? 4 : 1; }      // rows to a workgroup
 constexpr int threads_of(int waves) { return waves == 1 ? 256 : waves * 64; }
 
-// Whether element i of a piece is counted here and not by a neighbour.  WHOLE: rows are whole pieces, of which all or none is (16 operations fewer to a piece).
+// Whether a piece, and element i of it, are counted here and not by a neighbour.  WHOLE: rows are whole pieces, of which all or none is.
 template <bool WHOLE>
-__device__ __forceinline__ bool counts(const Place &p, int i) { return WHOLE ? p.skip == 0 : i >= p.skip; }
+__device__ __forceinline__ bool counts(const Place &p) { return !WHOLE || p.skip == 0; }
+template <bool WHOLE>
+__device__ __forceinline__ bool counts(const Place &p, int i) { return WHOLE || i >= p.skip; }
+
+// 1 / sqrt(x) to a step of fp32 (the instruction takes numbers below 2^-126 for 0).
+__device__ __forceinline__ float inverse_root(float x) { return x < 1e-30f ? 1.0f / sqrtf(x) : __builtin_amdgcn_rsqf(x); }
 
 // NORM: normalised; else as they are (to integers).  Rows of 8 to WAVES * PER * 512 elements.
 template <int XT, int OT, bool NORM, int WAVES, int PER, bool WHOLE>
@@ -67,6 +72,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
     __shared__ float sums[2][WAVES];
     __shared__ uint32_t tops[WAVES];
     const int n = (int)a.n;
+    const float each = 1.0f / (float)n;
     const int64_t first = (int64_t)blockIdx.x * rows_at_once(WAVES) + (WAVES == 1 ? threadIdx.x / 64 : 0), step = (int64_t)gridDim.x * rows_at_once(WAVES);
     Place place[PER];
     float weight[NORM ? PER : 1][8], bias[NORM ? PER : 1][8];
@@ -92,19 +98,22 @@ __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
         if constexpr (NORM) {
             float sum = 0.0f;
 #pragma unroll
-            for (int p = 0; p < PER; ++p)
+            for (int p = 0; p < PER; ++p) {
+                if (!counts<WHOLE>(place[p])) continue;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum += counts<WHOLE>(place[p], i) ? v[p][i] : 0.0f;
-            const float mean = over_row<WAVES>(sum, sums[0], plus) / (float)n;
+            }
+            const float mean = over_row<WAVES>(sum, sums[0], plus) * each;
             float squares = 0.0f;
 #pragma unroll
-            for (int p = 0; p < PER; ++p)
+            for (int p = 0; p < PER; ++p) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    v[p][i] -= mean;
-                    squares += counts<WHOLE>(place[p], i) ? v[p][i] * v[p][i] : 0.0f;
-                }
-            const float rstd = 1.0f / sqrtf(over_row<WAVES>(squares, sums[1], plus) / (float)n + a.eps);
+                for (int i = 0; i < 8; ++i) v[p][i] -= mean;
+                if (!counts<WHOLE>(place[p])) continue;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) squares += counts<WHOLE>(place[p], i) ? v[p][i] * v[p][i] : 0.0f;
+            }
+            const float rstd = inverse_root(over_row<WAVES>(squares, sums[1], plus) * each + a.eps);
             if (a.mean && threadIdx.x % (WAVES * 64) == 0) {
                 a.mean[row] = mean;
                 a.rstd[row] = rstd;
@@ -222,6 +231,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGr
     __shared__ float sums[2][2][WAVES];
     __shared__ float gathered[WAVES == 1 && SUMS ? ROWS : 1][WAVES == 1 && SUMS ? PER * 512 : 1];
     const int n = (int)a.n;
+    const float each = 1.0f / (float)n;
     const int64_t first = (int64_t)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x / 64 : 0), step = (int64_t)gridDim.x * ROWS;
     Place place[PER];
     float weight[PER][8], dweight[SUMS ? PER : 1][8] = {}, dbias[SUMS ? PER : 1][8] = {};
@@ -263,6 +273,10 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGr
                     dbias[p][i] += g[p][i];
                 }
                 g[p][i] *= weight[p][i];
+            }
+            if (!counts<WHOLE>(place[p])) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
                 su += counts<WHOLE>(place[p], i) ? g[p][i] : 0.0f;
                 suh += counts<WHOLE>(place[p], i) ? g[p][i] * h[p][i] : 0.0f;
             }
@@ -284,8 +298,8 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGr
                 suh += sums[turn][1][w];
             }
         }
-        su /= (float)n;
-        suh /= (float)n;
+        su *= each;
+        suh *= each;
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
 #pragma unroll
