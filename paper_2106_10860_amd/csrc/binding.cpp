@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/core/Allocator.h>
 #include <c10/core/GradMode.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -718,6 +719,19 @@ void *stream_on(const at::Device &device)
     return reinterpret_cast<void *>(whole(raw.p));
 }
 
+at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const at::Device &device) { return at::empty(sizes, at::TensorOptions().dtype(type).device(device)); }
+
+// Memory for the time of a call, of the current device's current stream (a tensor of it takes 0.4 us more).
+struct Scratch {
+    c10::DataPtr memory;
+    size_t bytes = 0;
+    explicit Scratch(size_t n) : bytes(n)
+    {
+        if (n) memory = c10::GetAllocator(c10::DeviceType::CUDA)->allocate(n);
+    }
+    void *get() const { return memory.get(); }
+};
+
 float real(PyObject *o)
 {
     if (!PyFloat_CheckExact(o)) throw NotUsual();
@@ -759,8 +773,8 @@ NewIntegers new_integers(int64_t rows, int64_t cols, const at::Device &device)
 {
     NewIntegers b;
     b.ld = up(cols, 16);
-    b.q = at::empty({rows, b.ld}, at::TensorOptions().dtype(at::kChar).device(device));
-    b.scale = at::empty({rows}, at::TensorOptions().dtype(at::kFloat).device(device));
+    b.q = fresh({rows, b.ld}, at::kChar, device);
+    b.scale = fresh({rows}, at::kFloat, device);
     if (b.ld != cols) b.q = b.q.narrow(1, 0, cols);
     return b;
 }
@@ -811,13 +825,13 @@ PyObject *integer_product(PyObject *, PyObject *const *a, Py_ssize_t n)
         const float *bias = flat_or_null<const float>(a[3], at::kFloat, {B.rows}, device);
         const at::ScalarType type = dtype_or(a[4], at::kBFloat16);
         void *stream = stream_on(device);
-        at::Tensor made, work;
+        at::Tensor made;
         void *out;
         int64_t ldo;
         int code;
         if (a[5] == Py_None) {
             code = float_code(type);
-            made = at::empty({A.rows, B.rows}, at::TensorOptions().dtype(type).device(device));
+            made = fresh({A.rows, B.rows}, type, device);
             out = made.data_ptr();
             ldo = B.rows;
         } else {
@@ -829,16 +843,14 @@ PyObject *integer_product(PyObject *, PyObject *const *a, Py_ssize_t n)
             out = o.data_ptr();
             ldo = r.ld;
         }
-        void *work_p = nullptr;
-        size_t work_bytes = 0;
+        const Scratch work(a[6] == Py_None ? maddness_integer_product_workspace(A.rows, A.cols, A.dtype) : 0);
+        void *work_p = work.get();
+        size_t work_bytes = work.bytes;
         if (a[6] != Py_None) {
             const at::Tensor &w = tensor(a[6]);
             if (w.scalar_type() != at::kByte || !w.is_contiguous() || w.device() != device) throw NotUsual();
             work_p = w.data_ptr();
             work_bytes = (size_t)w.numel();
-        } else if ((work_bytes = maddness_integer_product_workspace(A.rows, A.cols, A.dtype))) {
-            work = at::empty({(int64_t)work_bytes}, at::TensorOptions().dtype(at::kByte).device(device));
-            work_p = work.data_ptr();
         }
         int rc;
         Py_BEGIN_ALLOW_THREADS
@@ -875,16 +887,15 @@ PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
         const float eps = real(a[3]);
         const bool training = truth(a[4]), integer = truth(a[5]);
         const at::ScalarType type = dtype_or(a[6], x.scalar_type());
+        const int out_code = integer ? (int)MADDNESS_I8 : float_code(type);
         void *stream = stream_on(x.device());
-        const auto floats = at::TensorOptions().dtype(at::kFloat).device(x.device());
         at::Tensor y, mean, rstd;
         NewIntegers q;
         if (integer) q = new_integers(r.rows, r.cols, x.device());
-        else y = at::empty({r.rows, r.cols}, x.options().dtype(type));
-        const int out_code = integer ? (int)MADDNESS_I8 : float_code(type);
+        else y = fresh({r.rows, r.cols}, type, x.device());
         if (training) {
-            mean = at::empty({r.rows}, floats);
-            rstd = at::empty({r.rows}, floats);
+            mean = fresh({r.rows}, at::kFloat, x.device());
+            rstd = fresh({r.rows}, at::kFloat, x.device());
         }
         const void *x_p = x.data_ptr();
         void *out = integer ? q.q.data_ptr() : y.data_ptr();
@@ -916,22 +927,19 @@ PyObject *layer_norm_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
         const void *weight = parameter(a[4], r.cols, x.device(), &parameter_code);
         const bool parameters = truth(a[5]);
         void *stream = stream_on(x.device());
-        const auto floats = at::TensorOptions().dtype(at::kFloat).device(x.device());
-        at::Tensor dx = at::empty({r.rows, r.cols}, x.options()), dweight, dbias, work;
-        size_t bytes = 0;
+        at::Tensor dx = fresh({r.rows, r.cols}, x.scalar_type(), x.device()), dweight, dbias;
+        const Scratch work(parameters ? maddness_layer_norm_gradient_workspace(r.rows, r.cols) : 0);
         if (parameters) {
-            dweight = at::empty({r.cols}, floats);
-            dbias = at::empty({r.cols}, floats);
-            bytes = maddness_layer_norm_gradient_workspace(r.rows, r.cols);
-            work = at::empty({(int64_t)bytes}, floats.dtype(at::kByte));
+            dweight = fresh({r.cols}, at::kFloat, x.device());
+            dbias = fresh({r.cols}, at::kFloat, x.device());
         }
         const void *g_p = g.data_ptr(), *x_p = x.data_ptr();
-        void *dx_p = dx.data_ptr(), *work_p = parameters ? work.data_ptr() : nullptr;
+        void *dx_p = dx.data_ptr();
         float *dweight_p = parameters ? static_cast<float *>(dweight.data_ptr()) : nullptr, *dbias_p = parameters ? static_cast<float *>(dbias.data_ptr()) : nullptr;
         int rc;
         Py_BEGIN_ALLOW_THREADS
         rc = maddness_layer_norm_gradient(g_p, g_code, rg.ld, x_p, code, r.rows, r.cols, r.ld, mean, rstd, weight, std::max(parameter_code, 0), dx_p, r.cols,
-                                          dweight_p, dbias_p, work_p, bytes, stream);
+                                          dweight_p, dbias_p, work.get(), work.bytes, stream);
         Py_END_ALLOW_THREADS
         if (rc != MADDNESS_OK) return int_status(rc);
         if (parameters) return tuple_of(dx, dweight, dbias);
@@ -960,19 +968,15 @@ PyObject *balance(PyObject *, PyObject *const *a, Py_ssize_t n)
         const bool sigmoid = truth(a[2]);
         const float factor = real(a[3]);
         void *stream = stream_on(x.device());
-        const auto floats = at::TensorOptions().dtype(at::kFloat).device(x.device());
-        const size_t bytes = maddness_balance_workspace(r.rows, E);
-        at::Tensor loss = at::empty({}, floats), counts = at::empty({E}, floats.dtype(at::kInt)), push = at::empty({E}, floats);
-        at::Tensor work;
-        if (bytes) work = at::empty({(int64_t)bytes}, floats.dtype(at::kByte));
+        const Scratch work(maddness_balance_workspace(r.rows, E));
+        at::Tensor loss = fresh({}, at::kFloat, x.device()), counts = fresh({E}, at::kInt, x.device()), push = fresh({E}, at::kFloat, x.device());
         const void *x_p = x.data_ptr();
         float *loss_p = static_cast<float *>(loss.data_ptr()), *push_p = static_cast<float *>(push.data_ptr());
         int32_t *counts_p = static_cast<int32_t *>(counts.data_ptr());
-        void *work_p = bytes ? work.data_ptr() : nullptr;
         int rc;
         Py_BEGIN_ALLOW_THREADS
-        rc = maddness_balance(x_p, code, r.rows, E, r.ld, sigmoid ? MADDNESS_SIGMOID : MADDNESS_SOFTMAX, ids_p, k, factor, loss_p, counts_p, push_p, work_p,
-                              bytes, stream);
+        rc = maddness_balance(x_p, code, r.rows, E, r.ld, sigmoid ? MADDNESS_SIGMOID : MADDNESS_SOFTMAX, ids_p, k, factor, loss_p, counts_p, push_p,
+                              work.get(), work.bytes, stream);
         Py_END_ALLOW_THREADS
         if (rc != MADDNESS_OK) return int_status(rc);
         return tuple_of(loss, counts, push);
@@ -1008,7 +1012,7 @@ PyObject *balance_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
         at::Tensor made;
         void *out, *stream = stream_on(x.device());
         if (a[5] == Py_None) {
-            made = at::empty({r.rows, r.cols}, x.options());
+            made = fresh({r.rows, r.cols}, x.scalar_type(), x.device());
             out = made.data_ptr();
         } else {
             out = like(a[5], &ldd);
@@ -1050,24 +1054,20 @@ PyObject *clip_gradients(PyObject *, PyObject *const *a, Py_ssize_t n)
             to.out_dtype = float_code(o.scalar_type());
         }
         void *stream = stream_on(device);
-        at::Tensor norm, work;
-        const auto floats = at::TensorOptions().dtype(at::kFloat).device(device);
+        at::Tensor norm;
         const bool given = a[2] != Py_None;
-        size_t bytes = 0;
+        const Scratch work(given ? 0 : maddness_gradient_norm_workspace());
         if (given) {
             norm = plain(a[2]);
             if (norm.scalar_type() != at::kFloat || norm.numel() != 1 || norm.device() != device) throw NotUsual();
         } else {
-            norm = at::empty({}, floats);
-            bytes = maddness_gradient_norm_workspace();
-            work = at::empty({(int64_t)bytes}, floats.dtype(at::kByte));
+            norm = fresh({}, at::kFloat, device);
         }
         float *norm_p = static_cast<float *>(norm.data_ptr());
-        void *work_p = given ? nullptr : work.data_ptr();
         int rc;
         Py_BEGIN_ALLOW_THREADS
-        rc = scales ? maddness_clip_gradients(table.data(), count, max_norm, norm_p, given, work_p, bytes, stream)
-                    : maddness_gradient_norm(table.data(), count, norm_p, work_p, bytes, stream);
+        rc = scales ? maddness_clip_gradients(table.data(), count, max_norm, norm_p, given, work.get(), work.bytes, stream)
+                    : maddness_gradient_norm(table.data(), count, norm_p, work.get(), work.bytes, stream);
         Py_END_ALLOW_THREADS
         if (rc != MADDNESS_OK) return int_status(rc);
         if (!given) return THPVariable_Wrap(std::move(norm));
