@@ -174,7 +174,7 @@ def maddness_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, training: 
     weight_p, bias_p, parameter_code = _parameters(weight, bias, cols)
     _same_device(x, weight, bias, out)
     _here(x)
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device) if training else (None, None)
+    mean, rstd = (torch.empty(rows, dtype=torch.float32, device=x.device) for _ in range(2)) if training else (None, None)
     if integer:
         y = IntegerMatrix.empty(rows, cols, x.device)
         s = y._struct
@@ -214,7 +214,7 @@ def maddness_layer_norm_gradient(gradient, x, mean, rstd, weight=None, parameter
     dweight = dbias = workspace = None
     need, L = 0, _m.lib()
     if parameters:
-        dweight, dbias = torch.empty((2, cols), dtype=torch.float32, device=x.device)
+        dweight, dbias = (torch.empty(cols, dtype=torch.float32, device=x.device) for _ in range(2))
         need = L.maddness_layer_norm_gradient_workspace(rows, cols)
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
     _m._check(L.maddness_layer_norm_gradient(

@@ -269,3 +269,32 @@ def test_a_function_of_torchs_own(mad):
     dx, dw, db, e_dx, e_dw, e_db = ref.norm_gradient(host(grad), host(x.detach()), mean, r, host(w.detach()), 53, 60)
     # (the statistics are fp32 here: a few parts in 10^6 of each term)
     assert (np.abs(host(x.grad) - dx) <= e_dx + 2e-5).all() and (np.abs(host(w.grad) - dw) <= e_dw + 2e-4).all() and (np.abs(host(b.grad) - db) <= e_db + 1e-6).all()
+
+
+@pytest.mark.parametrize("how", ["native", "python"])
+def test_results_are_tensors_as_any(mad, monkeypatch, how):
+    """Small results of one call may share an allocation: writing to one leaves the others, each can be saved, used further, and made in inference mode."""
+    import torch
+    if how == "python":
+        monkeypatch.setattr(mad, "_native", mad._NotBuilt)
+    x, w, logits = normal(1, 6, 40), 1 + 0.1 * normal(2, 40), normal(3, 9, 5)
+    ids, _ = mad.maddness_route(logits, 2)
+
+    def calls():
+        y, mean, rstd = mad.maddness_layer_norm(x, w, training=True)
+        return [mean, rstd, *mad.maddness_layer_norm_gradient(y, x, mean, rstd, w)[1:], *mad.maddness_balance(logits, ids)]
+
+    want = [t.clone() for t in calls()]
+    assert [(t.dtype, tuple(t.shape)) for t in want] == [(torch.float32, (6,))] * 2 + [(torch.float32, (40,))] * 2 + [(torch.float32, ()), (torch.int32, (5,)), (torch.float32, (5,))]
+    got = calls()
+    for i, t in enumerate(got):
+        assert t.is_contiguous() and not t.requires_grad and t._version == 0
+        t.add_(1)
+        assert all(torch.equal(a, b) for a, b in zip(got[i + 1:], want[i + 1:]))
+    for t, c in zip(got, want):
+        assert torch.equal(t, c + 1)
+    with torch.inference_mode():
+        assert all(torch.equal(a, b) for a, b in zip(calls(), want))
+    loss = calls()[4].requires_grad_()
+    (2 * loss).backward()
+    assert float(loss.grad) == 2
