@@ -519,7 +519,7 @@ int maddness_layer_norm_gradient(const void *gradient, int32_t gradient_dtype, i
 
 /*
  * How evenly the tokens fall on the experts.  s are the scores that maddness_route makes of the logits (0 for a masked one), p[t][e] = s[t][e] /
- * sum_f s[t][f]; a token whose scores are all 0 (padding) counts nowhere.
+ * sum_f s[t][f]; a token whose scores are all 0 (padding) counts nowhere.  Exponentials are off by up to 2^-22 of themselves here, and a sigmoid below 2^-126 is 0.
  *   counts[e] = how many of `ids` [T][k] are e (those outside [0, E) are none);  n = their sum, L = the tokens that count
  *   push[e]   = factor E counts[e] / (n L), 0 where n or L is 0
  *   loss      = sum_e push[e] sum_t p[t][e]: factor where all experts have the same, more the less evenly they have

@@ -1,4 +1,5 @@
-// The norm over many tensors, and their scaling by it.  Both move bytes: the squares are summed in fp64 beside the loads.
+// The norm over many tensors, and their scaling by it.  Both move bytes: the squares are summed in fp64 beside the loads.  201 million bfloat16 gradients: squares 111 us (3.6 TB/s behind a
+// scaling whose results are still on their way to memory, 4.9 without), scaling to fp32 228 (5.3 TB/s).
 //
 // The tensors' places go with the launch, as arguments of the kernel, so that a captured graph holds them too; so many tensors to a launch.
 #include "lanes.h"

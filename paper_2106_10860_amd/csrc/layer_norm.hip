@@ -1,6 +1,11 @@
 // Rows that stay in registers from their load to their store: to 8-bit integers, through a layer norm, and back through its gradient.
 //
-// All of it moves bytes: a row is read once, its sums go around the lanes that hold it, and it is written once.
+//   mu = mean(x), v = mean((x - mu)^2), r = 1 / sqrt(v + eps), h = (x - mu) r, y = h weight + bias
+//   u = g weight, dx = r (u - mean(u) - h mean(u h)), dweight = sum over rows of g h, dbias = sum over rows of g
+//
+// All of it moves bytes: a row is read once, its sums go around the lanes that hold it (a wavefront for up to 1024 elements, else as many of a workgroup as
+// have it in pieces of 8 and 16 bytes or more), and it is written once.  What the norm's parameters need of the lanes stays in their registers, so a workgroup takes rows in turn, and
+// asks for the next one before it works on this one.  32768 rows of 4096 bfloat16: forward 96 us (5.6 TB/s of what is read and written, the copy of 1 GiB 5.0), gradient 155 (5.2).
 #include "lanes.h"
 #include "layers_common.h"
 
@@ -65,7 +70,7 @@ __device__ __forceinline__ bool counts(const Place &p, int i) { return WHOLE || 
 // 1 / sqrt(x) to a step of fp32 (the instruction takes numbers below 2^-126 for 0).
 __device__ __forceinline__ float inverse_root(float x) { return x < 1e-30f ? 1.0f / sqrtf(x) : __builtin_amdgcn_rsqf(x); }
 
-// NORM: normalised; else as they are (to integers).  Rows of 8 to WAVES * PER * 512 elements.
+// NORM: normalised; else as they are (to integers).  8192 rows of 4096 bfloat16 through a norm to integers 24 us, 4.2 TB/s: the vector units are busy for 60 % of it.  Rows of 8 to WAVES * PER * 512 elements.
 template <int XT, int OT, bool NORM, int WAVES, int PER, bool WHOLE>
 __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
 {
@@ -223,7 +228,8 @@ int launch_rows(const RowsArgs &a, hipStream_t stream)
 
 // --------------------------------------------------------------------------------------------------------------- the gradient
 
-// dx row by row, and of all rows that a workgroup takes the sums of g h and g for its lanes' columns; partial is [2][gridDim.x][n].
+// dx row by row, and of all rows that a workgroup takes the sums of g h and g for its lanes' columns; partial is [2][gridDim.x][n].  Two workgroups to a compute unit at most: more would leave more
+// partial sums (of 4096 columns 16.8 MB as it is, 5 us of the 160 that 32768 rows take) and are no faster, as a row ahead keeps memory busy.
 template <int GT, int XT, int WAVES, int PER, bool SUMS, bool WHOLE>
 __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGradientArgs a)
 {
@@ -377,7 +383,8 @@ __global__ __launch_bounds__(256) void norm_sums_any_kernel(NormGradientArgs a)
     a.partial[(gridDim.y + blockIdx.y) * a.n + c] = dbias;
 }
 
-// Sums of `parts` rows of partial sums (none: 0): 32 columns to a workgroup, its 32 runs of 32 lanes take every 32nd row.  blockIdx.y: weight or bias.
+// Sums of `parts` rows of partial sums (none: 0): 32 columns to a workgroup, its 32 runs of 32 lanes take every 32nd row, whole
+// lines of them.  blockIdx.y: weight or bias.  (512 rows of 4096 5 us, by 16 columns 7; of 510 3.2, by 64 columns 4.7.)
 __global__ __launch_bounds__(1024) void column_sums_kernel(const float *partial, int64_t parts, int64_t n, float *dweight, float *dbias)
 {
     __shared__ float sums[16][32];
