@@ -24,8 +24,10 @@ __device__ __forceinline__ Piece load_piece(const int8_t *row, int64_t kb, int g
 
 __device__ __forceinline__ i32x4 multiply(i32x4 b, i32x4 a, i32x4 c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(b, a, c, 0, 0, 0); }
 
+// A result: every step rounded on its own, so that all kernels give the same.
 __device__ __forceinline__ float scaled(int32_t sum, float scale_a, float scale_b, const float *bias, int64_t n)
 {
+#pragma clang fp contract(off)
     const float v = (float)sum * scale_a * scale_b;
     return bias ? v + bias[n] : v;
 }
@@ -311,11 +313,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void integer_tiles_kernel(IntegerA
                 const i32x4 sum = acc[half * (MT / 2) + i][j];
                 float four[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) four[k] = (float)sum[k] * scale_a * scale_b[j][k];
-                if (p.bias) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) four[k] += p.bias[min(n0 + (wn * NT + j) * 16 + 4 * g + k, p.N - 1)];
-                }
+                for (int k = 0; k < 4; ++k) four[k] = scaled(sum[k], scale_a, scale_b[j][k], p.bias, min(n0 + (wn * NT + j) * 16 + 4 * g + k, p.N - 1));
                 store_run<OUT>(mine + (i * 16 + r16) * LINE, j * 16 + 4 * g, four);
             }
         }

@@ -70,7 +70,8 @@ __device__ __forceinline__ bool counts(const Place &p, int i) { return WHOLE || 
 // 1 / sqrt(x) to a step of fp32 (the instruction takes numbers below 2^-126 for 0).
 __device__ __forceinline__ float inverse_root(float x) { return x < 1e-30f ? 1.0f / sqrtf(x) : __builtin_amdgcn_rsqf(x); }
 
-// NORM: normalised; else as they are (to integers).  8192 rows of 4096 bfloat16 through a norm to integers 24 us, 4.2 TB/s: the vector units are busy for 60 % of it.  Rows of 8 to WAVES * PER * 512 elements.
+// NORM: normalised; else as they are (to integers).  8192 rows of 4096 bfloat16 through a norm to integers 24 us, 4.2 TB/s: the vector units are
+// busy for 60 % of it.  Rows of 8 to WAVES * PER * 512 elements.
 template <int XT, int OT, bool NORM, int WAVES, int PER, bool WHOLE>
 __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
 {
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
                 for (int i = 0; i < 8; ++i) v[p][i] -= mean;
                 if (!counts<WHOLE>(place[p])) continue;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) squares += counts<WHOLE>(place[p], i) ? v[p][i] * v[p][i] : 0.0f;
+                for (int i = 0; i < 8; ++i) squares = counts<WHOLE>(place[p], i) ? __builtin_fmaf(v[p][i], v[p][i], squares) : squares;
             }
             const float rstd = inverse_root(over_row<WAVES>(squares, sums[1], plus) * each + a.eps);
             if (a.mean && threadIdx.x % (WAVES * 64) == 0) {
@@ -126,7 +127,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
 #pragma unroll
             for (int p = 0; p < PER; ++p)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[p][i] = v[p][i] * rstd * weight[p][i] + bias[p][i];
+                for (int i = 0; i < 8; ++i) v[p][i] = __builtin_fmaf(v[p][i] * rstd, weight[p][i], bias[p][i]);      // (the same in every form of the kernel)
         }
         if constexpr (OT == kI8) {
             uint32_t top = 0;
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(1024) void rows_any_kernel(RowsArgs a)
             mean = over_row<16>(sum, sums[0], plus) / (float)a.n;
             for (int64_t c = threadIdx.x; c < a.n; c += 1024) {
                 const float d = widen_at<XT>(a.x, from + c) - mean;
-                squares += d * d;
+                squares = __builtin_fmaf(d, d, squares);
             }
             rstd = 1.0f / sqrtf(over_row<16>(squares, sums[1], plus) / (float)a.n + a.eps);
             if (a.mean && threadIdx.x == 0) {
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(1024) void rows_any_kernel(RowsArgs a)
         auto value = [&](int64_t c) INLINE_LAMBDA {
             const float x = widen_at<XT>(a.x, from + c);
             if constexpr (!NORM) return x;
-            return (x - mean) * rstd * (a.weight ? widen_at(a.weight, a.parameter_dtype, c) : 1.0f) + (a.bias ? widen_at(a.bias, a.parameter_dtype, c) : 0.0f);
+            return __builtin_fmaf((x - mean) * rstd, a.weight ? widen_at(a.weight, a.parameter_dtype, c) : 1.0f, a.bias ? widen_at(a.bias, a.parameter_dtype, c) : 0.0f);
         };
         if constexpr (OT == kI8) {
             uint32_t top = 0;

@@ -186,11 +186,12 @@ def test_results_do_not_depend_on_other_rows(lib):
     A, qa, sa = integers(lib, rng, 4200, 1030)
     B, qb, sb = integers(lib, rng, 4096, 1030)
     for dtype in DTYPES:
-        whole = lib.maddness_integer_product(A, B, out_dtype=torch_type(dtype))
+        bias = torch.from_numpy(rng.normal(size=4096).astype(np.float32) * 1e5).cuda()
+        whole = lib.maddness_integer_product(A, B, bias=bias, out_dtype=torch_type(dtype))
         kernels = {lib.maddness_last_kernel()}
         for rows in (1, 16, 32, 64, 65, 500, 1000, 2000, 2300):
             print("case rows", rows, dtype, flush=True)
-            part = lib.maddness_integer_product(lib.IntegerMatrix(A.q[:rows], A.scale[:rows]), B, out_dtype=torch_type(dtype))
+            part = lib.maddness_integer_product(lib.IntegerMatrix(A.q[:rows], A.scale[:rows]), B, bias=bias, out_dtype=torch_type(dtype))
             kernels.add(lib.maddness_last_kernel())
             assert torch.equal(part, whole[:rows]), rows
         assert len(kernels) == 7, kernels

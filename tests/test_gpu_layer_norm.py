@@ -84,6 +84,8 @@ def test_layer_norm_to_integers(mad, case, dtype):
     only = mad.maddness_layer_norm(x_d, w, b, integer=True)
     assert torch.equal(only.q, got.q) and torch.equal(only.scale, got.scale)
     want, _, _, e_y, _, _ = ref.norm(host(x_d), host(w), host(b), 1e-5, depth_of(cols))
+    again = mad.maddness_quantise_rows(y)
+    assert torch.equal(again.q, got.q) and torch.equal(again.scale, got.scale)
     q, scale = ref.quantise(host(y))
     e_scale = e_y.max(1) / 127 + 2 * ref.U * scale
     assert (np.abs(host(got.scale) - np.abs(want).max(1) / 127) <= e_scale).all()
