@@ -274,15 +274,14 @@ struct Cut {
     }
 };
 
-// Launches f with a table after the other: at least once.
+// Calls f with a table after the other: at least once.  (Only who has launched something asks for errors: an older call's may be waiting.)
 template <int N, typename F>
 int for_tables(const maddness_tensor *tensors, int64_t n, int pieces, bool outs, F f)
 {
     int64_t from = 0;
     do {
         const Table<N> t = next_table<N>(tensors, n, chunk_of(pieces), from, outs);
-        f(t);
-        const int rc = check_hip(hipGetLastError(), outs ? "launch clip_kernel" : "launch squares_kernel");
+        const int rc = f(t);
         if (rc != MADDNESS_OK) return rc;
     } while (from < n);
     return MADDNESS_OK;
@@ -295,6 +294,7 @@ int launch_squares_as(const maddness_tensor *tensors, int64_t n, double *partial
     return for_tables<N>(tensors, n, PIECES, false, [&](const Table<N> &t) {
         hipLaunchKernelGGL((squares_kernel<PIECES, N>), dim3((unsigned)parts), dim3(kThreads), 0, stream, t, partials, add);
         add = true;
+        return check_hip(hipGetLastError(), "launch squares_kernel");
     });
 }
 
@@ -302,8 +302,9 @@ template <int PIECES, int N>
 int launch_clip_as(const maddness_tensor *tensors, int64_t n, const double *partials, int parts, float *norm, bool given, float max_norm, hipStream_t stream)
 {
     return for_tables<N>(tensors, n, PIECES, true, [&](const Table<N> &t) {
-        if (t.chunks == 0 && given) return;
+        if (t.chunks == 0 && given) return (int)MADDNESS_OK;
         hipLaunchKernelGGL((clip_kernel<PIECES, N>), dim3(groups_of(t.chunks)), dim3(kThreads), 0, stream, t, partials, parts, norm, given, max_norm);
+        return check_hip(hipGetLastError(), "launch clip_kernel");
     });
 }
 
