@@ -505,7 +505,8 @@ int maddness_integer_product(const maddness_integer_matrix *A, const maddness_in
  * maddness_layer_norm_gradient: from the gradient g of y, with h = (x - mu) r and u = g weight:
  *   dx = r (u - mean(u) - h mean(u h)), rounded to x's dtype;  dweight[c] = sum over rows of g h, dbias[c] = sum over rows of g, in fp32 in an order that
  *   depends on the sizes only.
- * gradient [rows][ldg] of gradient_dtype.  mean and rstd of the call before.  dx [rows][ldd], or NULL.  dweight and dbias [cols], or both NULL.
+ * gradient [rows][ldg] of gradient_dtype.  mean and rstd of the call before.  dx [rows][ldd], or NULL.  dweight and dbias [cols], or both NULL
+ * (of up to 2^26 columns).
  * Without rows dweight and dbias are 0.
  * workspace  maddness_layer_norm_gradient_workspace(rows, cols) bytes, 16-byte aligned; not needed (NULL) without dweight and dbias.
  */
@@ -543,7 +544,7 @@ int maddness_balance_gradient(const void *logits, int32_t dtype, int64_t T, int3
  * maddness_clip_gradients: every tensor's out = data times min(1, max_norm / norm[0]), in fp32, rounded to out_dtype; out may be data itself where
  * the types agree (then nothing is written where the factor is 1), and otherwise overlaps no data or out.  A norm that is not finite leaves the factor 1: the caller sees
  * it in norm.  max_norm >= 0 (infinity: the factor is 1).  Where norm_given is 0 the norm is that of these tensors, and written to norm; else norm
- * is read (a norm over the tensors of several processes).
+ * is read (a norm over the tensors of several processes).  norm is no element of what is written, nor of a data unless it is given.
  * workspace  maddness_gradient_norm_workspace() bytes, 8-byte aligned (NULL where norm_given).
  */
 typedef struct {

@@ -64,6 +64,8 @@ int check_parameter(const void *p, int32_t dtype, const char *name)
     return MADDNESS_OK;
 }
 
+constexpr int64_t kMostSummedColumns = (int64_t)1 << 26;    // 32 of them are a workgroup's of 1024
+
 int check_norm(int64_t rows, int64_t cols)
 {
     int rc;
@@ -101,7 +103,7 @@ int check_tensors(const maddness_tensor *tensors, int64_t n, bool outs)
 }
 
 // What is written must not be read or written by another tensor's scaling: the workgroups go over the tensors in no order.
-int check_apart(const maddness_tensor *tensors, int64_t n)
+int check_apart(const maddness_tensor *tensors, int64_t n, const float *norm, bool norm_given)
 {
     struct Range {
         uintptr_t begin, end;
@@ -126,6 +128,9 @@ int check_apart(const maddness_tensor *tensors, int64_t n)
         if (!far || r.end > far->end) far = &r;
         if (r.written && (!far_written || r.end > far_written->end)) far_written = &r;
     }
+    const uintptr_t at = reinterpret_cast<uintptr_t>(norm);
+    for (const Range &r : ranges)
+        if ((r.written || !norm_given) && r.begin < at + 4 && r.end > at) return fail(MADDNESS_E_INVAL, "norm lies within tensor %lld", (long long)r.of);
     return MADDNESS_OK;
 }
 
@@ -227,6 +232,7 @@ int maddness_layer_norm_gradient(const void *gradient, int32_t gradient_dtype, i
     if (dx && (rc = check_floats(dx, dtype, rows, cols, ldd, "dx")) != MADDNESS_OK) return rc;
     if (!dweight != !dbias) return fail(MADDNESS_E_INVAL, "dweight and dbias go together");
     if (!dx && !dweight) return fail(MADDNESS_E_INVAL, "dx and dweight are both NULL");
+    if (dweight && cols > kMostSummedColumns) return fail(MADDNESS_E_UNSUPPORTED, "cols = %lld, dweight and dbias have up to 2^26", (long long)cols);
     if (!aligned(dweight, 4) || !aligned(dbias, 4)) return fail(MADDNESS_E_ALIGN, "dweight / dbias not 4-byte aligned");
     if (dweight && (rc = check_workspace(workspace, workspace_bytes, maddness_layer_norm_gradient_workspace(rows, cols), 16)) != MADDNESS_OK) return rc;
     NormGradientArgs a{};
@@ -299,7 +305,7 @@ int maddness_clip_gradients(const maddness_tensor *tensors, int64_t n, float max
     if (!aligned(norm, 4)) return fail(MADDNESS_E_ALIGN, "norm not 4-byte aligned");
     if (!norm_given && (rc = check_workspace(workspace, workspace_bytes, maddness_gradient_norm_workspace(), 8)) != MADDNESS_OK) return rc;
     try {
-        if ((rc = check_apart(tensors, n)) != MADDNESS_OK) return rc;
+        if ((rc = check_apart(tensors, n, norm, norm_given != 0)) != MADDNESS_OK) return rc;
     } catch (const std::bad_alloc &) {
         return fail(MADDNESS_E_UNSUPPORTED, "no host memory to compare %lld tensors", (long long)n);
     }

@@ -92,7 +92,8 @@ def test_layer_norm_refuses(mad):
           (dict(mean=None), "inval", "mean"), (dict(rstd=FAKE + 2), "align", "rstd"), (dict(weight=FAKE + 1), "align", "weight"), (dict(ldd=199), "inval", "dx"),
           (dict(dx=None), "inval", "both"), (dict(dw=FAKE), "inval", "together"), (dict(dw=FAKE, db=FAKE + 1), "align", "dbias"),
           (dict(dw=FAKE, db=FAKE), "unsupported", "workspace"), (dict(dw=FAKE, db=FAKE, work=FAKE + 8, size=1 << 24), "align", "workspace"),
-          (dict(dw=FAKE, db=FAKE, work=FAKE, size=need(4, 200) - 1), "unsupported", "workspace"))
+          (dict(dw=FAKE, db=FAKE, work=FAKE, size=need(4, 200) - 1), "unsupported", "workspace"),
+          (dict(cols=2**26 + 1, ldg=2**27, ldx=2**27, ldd=2**27, dw=FAKE, db=FAKE, work=FAKE, size=2**40), "unsupported", "2^26"))
     refused(mad, gradient(rows=0), mad.MADDNESS_OK)
 
 
@@ -163,5 +164,8 @@ def test_gradient_norm_and_clipping_refuse(mad):
     refused(mad, clip(dict(out=FAKE + 16)), inval, "overlap")
     refused(mad, clip(dict(out_dtype=2)), inval, "overlap")
     refused(mad, clip(dict(count=4000), dict(data=FAKE + 64, out=1 << 30), dict(data=FAKE + 40000, out=FAKE + 40000)), inval, "tensors 0 and 1")
+    # the norm within what is read or written
+    refused(mad, clip(dict(data=FAKE + 4096, out=FAKE + 8192), out=FAKE + 8192 + 396, given=1, work=None, size=0), inval, "norm lies within tensor 0")
+    refused(mad, clip(dict(data=FAKE + 4096, out=FAKE + 8192), out=FAKE + 4096), inval, "norm lies within tensor 0")
     # nothing to do
     refused(mad, clip(given=1, work=None, size=0), mad.MADDNESS_OK)
