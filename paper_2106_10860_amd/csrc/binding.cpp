@@ -723,9 +723,9 @@ at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const at::Device &d
 
 // n elements (n < 0: one, without dimensions) of a tensor's memory from the offset-th on, as a tensor of their own: results of one call that are small share an
 // allocation (each would take 0.9 us).
-at::Tensor part_of(const at::Tensor &all, int64_t offset, int64_t n, at::ScalarType type)
+at::Tensor part_of(const at::Tensor &all, int64_t offset, int64_t n)
 {
-    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), c10::scalarTypeToTypeMeta(type));
+    auto impl = c10::make_intrusive<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
     impl->set_storage_offset(offset);
     if (n < 0) impl->set_sizes_contiguous(at::IntArrayRef());
     else impl->set_sizes_contiguous({n});
@@ -906,8 +906,8 @@ PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
         else y = fresh({r.rows, r.cols}, type, x.device());
         if (training) {
             const at::Tensor both = fresh({2, r.rows}, at::kFloat, x.device());
-            mean = part_of(both, 0, r.rows, at::kFloat);
-            rstd = part_of(both, r.rows, r.rows, at::kFloat);
+            mean = part_of(both, 0, r.rows);
+            rstd = part_of(both, r.rows, r.rows);
         }
         const void *x_p = x.data_ptr();
         void *out = integer ? q.q.data_ptr() : y.data_ptr();
@@ -943,8 +943,8 @@ PyObject *layer_norm_gradient(PyObject *, PyObject *const *a, Py_ssize_t n)
         const Scratch work(parameters ? maddness_layer_norm_gradient_workspace(r.rows, r.cols) : 0);
         if (parameters) {
             const at::Tensor both = fresh({2, r.cols}, at::kFloat, x.device());
-            dweight = part_of(both, 0, r.cols, at::kFloat);
-            dbias = part_of(both, r.cols, r.cols, at::kFloat);
+            dweight = part_of(both, 0, r.cols);
+            dbias = part_of(both, r.cols, r.cols);
         }
         const void *g_p = g.data_ptr(), *x_p = x.data_ptr();
         void *dx_p = dx.data_ptr();
@@ -982,8 +982,9 @@ PyObject *balance(PyObject *, PyObject *const *a, Py_ssize_t n)
         const float factor = real(a[3]);
         void *stream = stream_on(x.device());
         const Scratch work(maddness_balance_workspace(r.rows, E));
-        const at::Tensor all = fresh({2 * E + 1}, at::kFloat, x.device());
-        at::Tensor loss = part_of(all, 0, -1, at::kFloat), counts = part_of(all, 1, E, at::kInt), push = part_of(all, 1 + E, E, at::kFloat);
+        // (memory of one type: torch.save refuses tensors that share it with two)
+        const at::Tensor all = fresh({E + 1}, at::kFloat, x.device()), counts = fresh({E}, at::kInt, x.device());
+        const at::Tensor loss = part_of(all, 0, -1), push = part_of(all, 1, E);
         const void *x_p = x.data_ptr();
         float *loss_p = static_cast<float *>(loss.data_ptr()), *push_p = static_cast<float *>(push.data_ptr());
         int32_t *counts_p = static_cast<int32_t *>(counts.data_ptr());

@@ -298,3 +298,8 @@ def test_results_are_tensors_as_any(mad, monkeypatch, how):
     loss = calls()[4].requires_grad_()
     (2 * loss).backward()
     assert float(loss.grad) == 2
+    import io
+    file = io.BytesIO()
+    torch.save(calls(), file)
+    file.seek(0)
+    assert all(torch.equal(a, b) for a, b in zip(torch.load(file, weights_only=True), want))
