@@ -276,7 +276,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGr
             for (int i = 0; i < 8; ++i) {
                 h[p][i] = (h[p][i] - mean) * r;
                 if constexpr (SUMS) {
-                    dweight[p][i] += g[p][i] * h[p][i];
+                    dweight[p][i] = __builtin_fmaf(g[p][i], h[p][i], dweight[p][i]);
                     dbias[p][i] += g[p][i];
                 }
                 g[p][i] *= weight[p][i];
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGr
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 su += counts<WHOLE>(place[p], i) ? g[p][i] : 0.0f;
-                suh += counts<WHOLE>(place[p], i) ? g[p][i] * h[p][i] : 0.0f;
+                suh = counts<WHOLE>(place[p], i) ? __builtin_fmaf(g[p][i], h[p][i], suh) : suh;
             }
         }
         if (AHEAD && row + step < a.rows) load(row + step);
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGr
 #pragma unroll
         for (int p = 0; p < PER; ++p) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) g[p][i] = r * (g[p][i] - su - h[p][i] * suh);
+            for (int i = 0; i < 8; ++i) g[p][i] = r * __builtin_fmaf(-h[p][i], suh, g[p][i] - su);
             if (place[p].skip < 8) store_run<XT>(a.dx, row * a.ldd + place[p].at, g[p]);
         }
     }
@@ -356,14 +356,14 @@ __global__ __launch_bounds__(1024) void norm_gradient_any_kernel(NormGradientArg
         for (int64_t c = threadIdx.x; c < a.n; c += 1024) {
             const float u = widen_at<GT>(a.g, row * a.ldg + c) * (a.weight ? widen_at(a.weight, a.parameter_dtype, c) : 1.0f);
             su += u;
-            suh += u * ((widen_at<XT>(a.x, row * a.ldx + c) - mean) * r);
+            suh = __builtin_fmaf(u, (widen_at<XT>(a.x, row * a.ldx + c) - mean) * r, suh);
         }
         su = over_row<16>(su, sums[0], plus) / (float)a.n;
         suh = over_row<16>(suh, sums[1], plus) / (float)a.n;
         for (int64_t c = threadIdx.x; c < a.n; c += 1024) {
             const float u = widen_at<GT>(a.g, row * a.ldg + c) * (a.weight ? widen_at(a.weight, a.parameter_dtype, c) : 1.0f);
             const float h = (widen_at<XT>(a.x, row * a.ldx + c) - mean) * r;
-            store_as<XT>(a.dx, row * a.ldd + c, r * (u - su - h * suh));
+            store_as<XT>(a.dx, row * a.ldd + c, r * __builtin_fmaf(-h, suh, u - su));
         }
     }
 }
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(256) void norm_sums_any_kernel(NormGradientArgs a)
     float dweight = 0.0f, dbias = 0.0f;
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const float g = widen_at<GT>(a.g, row * a.ldg + c);
-        dweight += g * ((widen_at<XT>(a.x, row * a.ldx + c) - a.mean[row]) * a.rstd[row]);
+        dweight = __builtin_fmaf(g, (widen_at<XT>(a.x, row * a.ldx + c) - a.mean[row]) * a.rstd[row], dweight);
         dbias += g;
     }
     a.partial[blockIdx.y * a.n + c] = dweight;
