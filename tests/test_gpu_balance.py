@@ -1,4 +1,6 @@
 """The balance of experts: counts, loss and gradient, within what fp32 scores and sums may change."""
+import math
+
 import numpy as np
 import pytest
 
@@ -157,3 +159,87 @@ def test_refusals(mad):
         mad.maddness_balance_gradient(logits, push, loss_gradient=torch.ones(2, device="cuda"))
     with pytest.raises(ValueError, match="gradient"):
         mad.maddness_balance_gradient(logits, push.clone().requires_grad_())
+
+
+LEAST = -126 * math.log(2.0)                              # a sigmoid of 2^-126, below which it is 0
+
+
+def far_logits(dtype):
+    """Every 16-bit number between -140 and -80, or a sweep of fp32 ones; none as near to LEAST as fp32 scores are off."""
+    import torch
+    if dtype == "f32":
+        x = np.linspace(-140, -80, 6001).astype(np.float32).astype(np.float64)
+    else:
+        x = host(torch.arange(-32768, 32768).to(torch.int16).cuda().view(torch_type(dtype)))
+    return x[(x >= -140) & (x <= -80) & (np.abs(x - LEAST) > 1e-4)]
+
+
+def check_sigmoid(mad, logits, ids, what):
+    """Loss, counts, push and gradient against 64 bits, in which a score below 2^-126 is 0 too; returns the scores' shares, the loss and its bound."""
+    factor, (T, E) = 0.25, logits.shape
+    x, i = host(logits), ids.cpu().numpy()
+    s, seen, rel = ref.scores(x, "sigmoid")
+    s = np.where(s < 2.0 ** -126, 0.0, s)
+    total = s.sum(1, keepdims=True)
+    p = np.divide(s, total, out=np.zeros_like(s), where=total > 0)
+    counts_w = np.bincount(i[(i >= 0) & (i < E)].ravel(), minlength=E)
+    push_w = factor * E * counts_w / (counts_w.sum() * int((total > 0).sum()))
+    want = float((push_w * p.sum(0)).sum())
+    loss, counts, push = mad.maddness_balance(logits, ids, scores="sigmoid", factor=factor)
+    assert np.array_equal(counts.cpu().numpy(), counts_w)
+    push_h = host(push)
+    assert (np.abs(push_h - push_w) <= 1.01 * U * push_w).all(), what
+    # bounds as above; shares may be so small that they lose half a step of fp32's subnormal numbers
+    rel_p = rel + rel.max(1, keepdims=True) + 24 * U
+    e_loss = 1.01 * (((rel_p * p).sum(0) * push_w).sum() + (depth_of(T, E) + 4) * U * want + 2.0 ** -149 * T * push_w.sum()) + 2.0 ** -149
+    assert abs(float(loss) - want) <= e_loss, (what, float(loss), want)
+    d = ref.balance_gradient(p, s, seen, push_h, "sigmoid")
+    dot = (p * push_h).sum(1, keepdims=True)
+    e_dot = (p * push_h * (rel_p + 26 * U)).sum(1, keepdims=True)
+    apart = np.abs(push_h - dot)
+    bound = 1.01 * p * ((1 - s) * (rel_p * apart + e_dot + 6 * U * (apart + push_h + dot)) + apart * (rel * s + U)) + 2.0 ** -148
+    for dtype in DTYPES:
+        if logits.dtype is torch_type(dtype):
+            check(mad.maddness_balance_gradient(logits, push, scores="sigmoid"), d, bound, dtype, what)
+    return s, push_w, want, e_loss
+
+
+# (tokens, experts): every split of a token's experts over lanes, by one workgroup and by many
+@pytest.mark.parametrize("size", [(2048, 8), (512, 60), (128, 200), (32, 600), (4099, 8), (4099, 60), (4099, 200), (2051, 600)], ids=lambda c: "T%d_E%d" % c)
+def test_sigmoids_that_vanish(mad, size):
+    """Finite logits whose exponential has no number in fp32: alone among ordinary ones, half of a token's, all of them (such a token counts nowhere);
+    and tokens that have only scores next to the smallest."""
+    import torch
+    T, E = size
+    print("case far sigmoids", size, flush=True)
+    for dtype in DTYPES:
+        rng = np.random.default_rng(T + E)
+        far = far_logits(dtype)
+        x = rng.normal(size=(T, E)) * 2
+        x[np.arange(0, T, 4), rng.integers(0, E, size=-(-T // 4))] = far[np.arange(-(-T // 4)) % len(far)]
+        half = x[1::4]
+        half[:] = np.where(rng.random(half.shape) < 0.5, rng.choice(far, half.shape), half)
+        x[2::4] = rng.choice(far[far < LEAST], x[2::4].shape)
+        x[3::4] = rng.choice(far[far > LEAST], x[3::4].shape)
+        logits = dev(x, dtype)
+        ids = logits.float().topk(2, -1)[1].to(torch.int32).contiguous()
+        check_sigmoid(mad, logits, ids, (size, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_sigmoids_of_every_logit(mad, dtype):
+    """All 65536 numbers of a type, each beside ordinary logits; the scores are those of the choice of experts."""
+    import torch
+    E = 8
+    print("case every sigmoid", dtype, flush=True)
+    every = torch.arange(-32768, 32768).to(torch.int16).cuda().view(torch_type(dtype))
+    logits = dev(np.random.default_rng(8).normal(size=(65536, E)), dtype)
+    logits[torch.arange(65536, device="cuda"), torch.arange(65536, device="cuda") % E] = every
+    ids, scores = mad.maddness_route(logits, E, scores="sigmoid", renormalise=False)
+    s, push, want, e_loss = check_sigmoid(mad, logits, ids[:, :2].contiguous(), dtype)
+    route = np.zeros(s.shape)
+    rows, slots = np.nonzero(ids.cpu().numpy() >= 0)
+    route[rows, ids.cpu().numpy()[rows, slots]] = host(scores)[rows, slots]
+    assert (np.abs(route - s) <= 8 * U * s + 2.0 ** -126).all()
+    loss = ((route / route.sum(1, keepdims=True)).sum(0) * push).sum()
+    assert abs(loss - want) <= e_loss

@@ -303,3 +303,23 @@ def test_results_are_tensors_as_any(mad, monkeypatch, how):
     torch.save(calls(), file)
     file.seek(0)
     assert all(torch.equal(a, b) for a, b in zip(torch.load(file, weights_only=True), want))
+
+
+def test_the_layers_balance_of_logits_that_vanish(mad):
+    """Sigmoid logits of -80 to -140 among a token's: loss and gradient are numbers, the gradient that of the choice with the balance's on top."""
+    import torch
+    from paper_2106_10860_amd.expert_layer import ExpertLayer
+    layer, x, gate, _, _, grad = problem(mad)
+    logits = x @ gate.T
+    logits[::3, 1] = torch.linspace(-140, -80, 100, device="cuda")
+    with_balance = ExpertLayer(layer.W, layer.Wt, 2, scores="sigmoid", balance=0.5)
+    _, saved = with_balance.forward(x, logits, training=True)
+    dlogits = with_balance.backward(saved, grad)[2]
+    assert bool(saved.balance_loss.isfinite()) and bool(dlogits.isfinite().all())
+    without = ExpertLayer(layer.W, layer.Wt, 2, scores="sigmoid")
+    choice = without.backward(without.forward(x, logits, training=True)[1], grad)[2]
+    want, counts, push, p, s, seen, _ = ref.balance(host(logits), saved.ids.cpu().numpy(), "sigmoid", 0.5)
+    d = ref.balance_gradient(p, s, seen, host(saved.push), "sigmoid")
+    # (shares and their products within 100 roundings, as every one of 8 experts' parts has less)
+    most = 100 * ref.U * (p * (np.abs(host(saved.push)) + (p * host(saved.push)).sum(1, keepdims=True)) + np.abs(host(choice))) + 2.0 ** -126
+    assert abs(float(saved.balance_loss) - want) <= 100 * ref.U * want and (np.abs(host(dlogits) - (host(choice) + d)) <= most).all()
