@@ -90,9 +90,9 @@ __device__ __forceinline__ uint32_t nearest_integer(float x, float s, float inv)
 {
     constexpr float kMagic = 12582912.0f;                     // 1.5 2^23: one more is one step
     const float t = __builtin_fmaf(x, inv, kMagic), q = t - kMagic;
-    const float r = __builtin_fmaf(-q, s, x), half = 0.5f * s, off = fabsf(r);
+    const float r = __builtin_fmaf(-q, s, x), twice = 2.0f * fabsf(r);        // (half of s need not be a number of fp32, where that is below 2^-125)
     uint32_t b = __float_as_uint(t);
-    const bool other = off > half || (off == half && (b & 1));
+    const bool other = twice > s || (twice == s && (b & 1));
     return b + (other ? (r > 0 ? 1u : 0xffffffffu) : 0u);
 }
 

@@ -288,3 +288,25 @@ def test_refusals(mad):
             mad.IntegerMatrix(*bad)
     with pytest.raises(mad.MaddnessError):                         # rows that do not begin at multiples of 16 bytes
         mad.maddness_integer_product(x[:, :20], mad.IntegerMatrix(torch.zeros((4, 20), dtype=torch.int8, device="cuda"), s))
+
+
+def test_rows_whose_scale_has_no_half(mad):
+    """A scale between 2^-126 and 2^-125 with a last bit has a half that is no number of fp32; quotients next to one still go to the nearest integer."""
+    import torch
+    rng = np.random.default_rng(7)
+    x = np.zeros((200, 400), np.float32)
+    for row in x:
+        row[0] = np.float32(rng.uniform(127 * 2.0 ** -126, 127 * 2.0 ** -125))
+        halves = ((np.arange(127) + 0.5) * np.float64(np.float32(row[0] / np.float32(127)))).astype(np.float32)
+        near = np.concatenate([halves, np.nextafter(halves, np.float32(0)), np.nextafter(halves, np.float32(1))])
+        near[near > row[0]] = 0
+        row[1:1 + len(near)] = near * rng.choice([-1, 1], len(near)).astype(np.float32)
+    q, scale = ref.quantise(x)
+    for wide in (1, 42):                                       # (in registers, and rows that are read again)
+        got = mad.maddness_quantise_rows(torch.from_numpy(np.tile(x[:200 // wide], (1, wide))).cuda())
+        assert np.array_equal(host(got.scale), scale[:200 // wide])
+        assert np.array_equal(got.q.cpu().numpy().astype(int), np.tile(q[:200 // wide], (1, wide)))
+    # and within the product
+    eye = mad.IntegerMatrix(torch.eye(400, dtype=torch.int8, device="cuda"), torch.ones(400, device="cuda"))
+    out = mad.maddness_integer_product(torch.from_numpy(x[:32]).cuda(), eye, out_dtype=torch.float32)
+    assert np.array_equal(out.cpu().numpy(), q[:32].astype(np.float32) * scale[:32, None].astype(np.float32))
