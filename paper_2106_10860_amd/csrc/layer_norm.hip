@@ -109,7 +109,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum += counts<WHOLE>(place[p], i) ? v[p][i] : 0.0f;
             }
-            const float mean = over_row<WAVES>(sum, sums[0], plus) * each;
+            const float mean = over_row<WAVES>(sum, sums[0], plus) / (float)n;      // (a rounded 1 / n would leave a row of one number uncentred)
             float squares = 0.0f;
 #pragma unroll
             for (int p = 0; p < PER; ++p) {
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGr
                 suh += sums[turn][1][w];
             }
         }
-        su *= each;
+        su /= (float)n;                                       // (as the mean: a gradient of one number is centred to 0)
         suh *= each;
 #pragma unroll
         for (int p = 0; p < PER; ++p) {

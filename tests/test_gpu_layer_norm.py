@@ -178,3 +178,16 @@ def test_refusals(mad):
         mad.maddness_layer_norm(x, torch.nn.Parameter(w))
     with pytest.raises(ValueError, match="gradient"):
         mad.maddness_layer_norm_gradient(y, x, mean, rstd, torch.nn.Parameter(w))
+
+
+@pytest.mark.parametrize("cols", [8, 100, 510, 700, 1000, 1023, 1500, 2049, 4096, 4095, 5000, 8191, 12345, 16384, 20000])
+def test_rows_of_one_number(mad, cols):
+    """Their sum is exact (4000 = 125 * 2^5, and sums below 2^29), so the mean is the number, the norm the bias, and a gradient of one number centres to nothing."""
+    import torch
+    x = torch.full((5, cols), 4000.0, device="cuda")
+    b = torch.linspace(-1, 1, cols, device="cuda")
+    y, mean, rstd = mad.maddness_layer_norm(x, torch.full_like(b, 3.0), b, training=True)
+    assert bool((mean == 4000).all()) and torch.equal(y, b.expand(5, cols))
+    assert bool((rstd == rstd[0]).all()) and abs(float(rstd[0]) * 1e-5 ** 0.5 - 1) < 4 * ref.U
+    dx, dw, db = mad.maddness_layer_norm_gradient(x, x, mean, rstd, parameters=True)
+    assert not dx.any() and not dw.any() and bool((db == 20000).all())
