@@ -31,6 +31,9 @@ __device__ __forceinline__ T over_row(T x, T (&slots)[WAVES], F f)
     return x;
 }
 
+__device__ __forceinline__ float fused(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
+__device__ __forceinline__ double fused(double a, double b, double c) { return __builtin_fma(a, b, c); }
+
 // Which of a row's n elements (n >= 8) a lane holds as its piece: the eight from column `at` on, of which the first `skip` are its neighbour's too.
 struct Place {
     int at, skip;
@@ -155,24 +158,26 @@ __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
     }
 }
 
-// Rows of any length, a workgroup to each, read again for every sum.
-template <int XT, int OT, bool NORM>
+// Rows of any length, a workgroup to each, read again for every sum.  A thread adds every 1024th element, one after the other: for long rows in fp64 (SUM), as there is no end to how
+// many (4096 rows of 20000 223 us, 214 in fp32; 512 of 300000 562 and 552); the one element that a thread has of a row below 8 needs none of it (2^19 rows of 7 1.55 ms, 2.31 with
+// fp64 between the lanes).
+template <int XT, int OT, bool NORM, typename SUM>
 __global__ __launch_bounds__(1024) void rows_any_kernel(RowsArgs a)
 {
-    __shared__ float sums[2][16];
+    __shared__ SUM sums[2][16];
     __shared__ uint32_t tops[16];
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const int64_t from = row * a.ldx;
         float mean = 0.0f, rstd = 1.0f;
         if constexpr (NORM) {
-            float sum = 0.0f, squares = 0.0f;
-            for (int64_t c = threadIdx.x; c < a.n; c += 1024) sum += widen_at<XT>(a.x, from + c);
-            mean = over_row<16>(sum, sums[0], plus) / (float)a.n;
+            SUM sum = 0, squares = 0;
+            for (int64_t c = threadIdx.x; c < a.n; c += 1024) sum += (SUM)widen_at<XT>(a.x, from + c);
+            mean = (float)(over_row<16>(sum, sums[0], plus) / (SUM)a.n);
             for (int64_t c = threadIdx.x; c < a.n; c += 1024) {
-                const float d = widen_at<XT>(a.x, from + c) - mean;
-                squares = __builtin_fmaf(d, d, squares);
+                const SUM d = (SUM)(widen_at<XT>(a.x, from + c) - mean);
+                squares = fused(d, d, squares);
             }
-            rstd = 1.0f / sqrtf(over_row<16>(squares, sums[1], plus) / (float)a.n + a.eps);
+            rstd = 1.0f / sqrtf((float)(over_row<16>(squares, sums[1], plus) / (SUM)a.n) + a.eps);
             if (a.mean && threadIdx.x == 0) {
                 a.mean[row] = mean;
                 a.rstd[row] = rstd;
@@ -216,7 +221,9 @@ int launch_rows(const RowsArgs &a, hipStream_t stream)
 {
     if (a.n < 8 || a.n > kLongestRow) {
         note_kernel("rows_any_kernel", __PRETTY_FUNCTION__);
-        hipLaunchKernelGGL((rows_any_kernel<XT, OT, NORM>), dim3((unsigned)std::min(a.rows, (int64_t)device_info().cus * 2)), dim3(1024), 0, stream, a);
+        const dim3 grid((unsigned)std::min(a.rows, (int64_t)device_info().cus * 2));
+        if (NORM && a.n >= 8) hipLaunchKernelGGL((rows_any_kernel<XT, OT, NORM, std::conditional_t<NORM, double, float>>), grid, dim3(1024), 0, stream, a);
+        else hipLaunchKernelGGL((rows_any_kernel<XT, OT, NORM, float>), grid, dim3(1024), 0, stream, a);
         return check_hip(hipGetLastError(), "launch rows_any_kernel");
     }
     if (a.n <= 512) return launch_rows_as<XT, OT, NORM, 1, 1>(a, stream);
@@ -345,21 +352,20 @@ __global__ __launch_bounds__(threads_of(WAVES)) void norm_gradient_kernel(NormGr
     }
 }
 
-// Rows of any length: dx, read twice.
-template <int GT, int XT>
+// Rows of any length: dx, read twice; SUM as in rows_any_kernel.
+template <int GT, int XT, typename SUM>
 __global__ __launch_bounds__(1024) void norm_gradient_any_kernel(NormGradientArgs a)
 {
-    __shared__ float sums[2][16];
+    __shared__ SUM sums[2][16];
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const float mean = a.mean[row], r = a.rstd[row];
-        float su = 0.0f, suh = 0.0f;
+        SUM all_u = 0, all_uh = 0;
         for (int64_t c = threadIdx.x; c < a.n; c += 1024) {
             const float u = widen_at<GT>(a.g, row * a.ldg + c) * (a.weight ? widen_at(a.weight, a.parameter_dtype, c) : 1.0f);
-            su += u;
-            suh = __builtin_fmaf(u, (widen_at<XT>(a.x, row * a.ldx + c) - mean) * r, suh);
+            all_u += (SUM)u;
+            all_uh = fused((SUM)u, (SUM)((widen_at<XT>(a.x, row * a.ldx + c) - mean) * r), all_uh);
         }
-        su = over_row<16>(su, sums[0], plus) / (float)a.n;
-        suh = over_row<16>(suh, sums[1], plus) / (float)a.n;
+        const float su = (float)(over_row<16>(all_u, sums[0], plus) / (SUM)a.n), suh = (float)(over_row<16>(all_uh, sums[1], plus) / (SUM)a.n);
         for (int64_t c = threadIdx.x; c < a.n; c += 1024) {
             const float u = widen_at<GT>(a.g, row * a.ldg + c) * (a.weight ? widen_at(a.weight, a.parameter_dtype, c) : 1.0f);
             const float h = (widen_at<XT>(a.x, row * a.ldx + c) - mean) * r;
@@ -368,20 +374,20 @@ __global__ __launch_bounds__(1024) void norm_gradient_any_kernel(NormGradientArg
     }
 }
 
-// Their sums over the rows that a workgroup takes, a thread to a column.
+// Their sums over the rows that a workgroup takes, a thread to a column: of long rows few workgroups share the rows, so a thread adds many, in fp64.
 template <int GT, int XT>
 __global__ __launch_bounds__(256) void norm_sums_any_kernel(NormGradientArgs a)
 {
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (c >= a.n) return;
-    float dweight = 0.0f, dbias = 0.0f;
+    double dweight = 0.0, dbias = 0.0;
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-        const float g = widen_at<GT>(a.g, row * a.ldg + c);
-        dweight = __builtin_fmaf(g, (widen_at<XT>(a.x, row * a.ldx + c) - a.mean[row]) * a.rstd[row], dweight);
+        const double g = (double)widen_at<GT>(a.g, row * a.ldg + c);
+        dweight = __builtin_fma(g, (double)((widen_at<XT>(a.x, row * a.ldx + c) - a.mean[row]) * a.rstd[row]), dweight);
         dbias += g;
     }
-    a.partial[blockIdx.y * a.n + c] = dweight;
-    a.partial[(gridDim.y + blockIdx.y) * a.n + c] = dbias;
+    a.partial[blockIdx.y * a.n + c] = (float)dweight;
+    a.partial[(gridDim.y + blockIdx.y) * a.n + c] = (float)dbias;
 }
 
 // Sums of `parts` rows of partial sums (none: 0): 32 columns to a workgroup, its 32 runs of 32 lanes take every 32nd row, whole
@@ -434,7 +440,9 @@ int launch_gradient(const NormGradientArgs &a, hipStream_t stream)
     if (a.n < 8 || a.n > kLongestRow) {
         if (a.dx) {
             note_kernel("norm_gradient_any_kernel", __PRETTY_FUNCTION__);
-            hipLaunchKernelGGL((norm_gradient_any_kernel<GT, XT>), dim3((unsigned)std::min(a.rows, (int64_t)device_info().cus * 2)), dim3(1024), 0, stream, a);
+            const dim3 grid((unsigned)std::min(a.rows, (int64_t)device_info().cus * 2));
+            if (a.n < 8) hipLaunchKernelGGL((norm_gradient_any_kernel<GT, XT, float>), grid, dim3(1024), 0, stream, a);
+            else hipLaunchKernelGGL((norm_gradient_any_kernel<GT, XT, double>), grid, dim3(1024), 0, stream, a);
         }
         if (a.dweight) {
             note_kernel("norm_sums_any_kernel", __PRETTY_FUNCTION__);

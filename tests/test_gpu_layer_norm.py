@@ -191,3 +191,54 @@ def test_rows_of_one_number(mad, cols):
     assert bool((rstd == rstd[0]).all()) and abs(float(rstd[0]) * 1e-5 ** 0.5 - 1) < 4 * ref.U
     dx, dw, db = mad.maddness_layer_norm_gradient(x, x, mean, rstd, parameters=True)
     assert not dx.any() and not dw.any() and bool((db == 20000).all())
+
+
+@pytest.mark.parametrize("size", [(1 << 21, 7), (20000, 16400), (3000, 540000)], ids=lambda c: "%dx%d" % c)
+def test_sums_over_many_rows_of_any_length(mad, size):
+    """Lengths whose sums over rows are taken a column to a thread: hundreds or thousands of rows to each, added in fp64, so that only the
+    parts' sum is left to fp32."""
+    import torch
+    rows, cols = size
+    print("case many rows", size, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, cols, generator=g, device="cuda", dtype=torch.bfloat16 if cols > 7 else torch.float32)
+    grad = torch.full((rows, cols), 1.1, device="cuda")
+    x[:, 3] = 2.5                                              # (a column whose h hardly changes: all of its terms have one sign)
+    _, mean, rstd = mad.maddness_layer_norm(x, training=True)
+    _, dw, db = mad.maddness_layer_norm_gradient(grad, x, mean, rstd, parameters=True)
+    parts = mad.lib().maddness_layer_norm_gradient_workspace(rows, cols) // (8 * cols)
+    assert rows // parts > 100
+    depth = -(-parts // 32) + 18                               # additions of a part, and its own rounding
+    keep = torch.arange(0, cols, max(1, cols // 1000), device="cuda").unique()
+    keep = torch.cat([keep, torch.tensor([3, cols - 1], device="cuda")])
+    h = (x[:, keep].double() - mean.double().unsqueeze(1)) * rstd.double().unsqueeze(1)
+    gk = grad[:, keep].double()
+    want_w, size_w, want_b = (gk * h).sum(0), (gk * h).abs().sum(0), gk.sum(0)
+    # h is rounded twice
+    assert bool(((dw[keep].double() - want_w).abs() <= 1.01 * (depth + 2) * ref.U * size_w).all())
+    assert bool(((db[keep].double() - want_b).abs() <= 1.01 * depth * ref.U * want_b).all())
+
+
+def test_sums_of_a_long_row(mad):
+    """Four million numbers: 4096 to a thread, added in fp64, so that mean and deviation are off by their last roundings only."""
+    import torch
+    cols, U = 1 << 22, ref.U
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(2, cols, generator=g, device="cuda") + 3.7
+    y, mean, rstd = mad.maddness_layer_norm(x, training=True)
+    mean_w = x.double().mean(1)
+    assert bool(((mean.double() - mean_w).abs() <= 1.01 * U * mean_w.abs()).all())
+    d = x.double() - mean.double().unsqueeze(1)
+    r = 1 / torch.sqrt((d * d).mean(1) + 1e-5)
+    # centred values are rounded (2 U in their squares), the variance and its sum with eps too: half of 4 U in the root, which is rounded, as the quotient is
+    assert bool(((rstd.double() - r).abs() <= 1.01 * 4 * U * r).all())
+    grad = 1.1 + 0.1 * torch.randn(2, cols, generator=g, device="cuda")
+    dx, _, _ = mad.maddness_layer_norm_gradient(grad, x, mean, rstd, parameters=False)
+    h = d * rstd.double().unsqueeze(1)
+    u = grad.double()
+    su, suh = u.mean(1, keepdim=True), (u * h).mean(1, keepdim=True)
+    want = rstd.double().unsqueeze(1) * (u - su - h * suh)
+    # su to one rounding; h to two, in suh (once more rounded) and beside it; u - su and the sum one each, the factor one
+    parts = u.abs() + su.abs() + (h * suh).abs()
+    most = 1.01 * rstd.double().unsqueeze(1) * U * (su.abs() + h.abs() * 3 * (u * h).abs().mean(1, keepdim=True) + 2 * (h * suh).abs() + 3 * parts)
+    assert bool(((dx.double() - want).abs() <= most + U * want.abs()).all())
