@@ -541,10 +541,10 @@ int maddness_balance_gradient(const void *logits, int32_t dtype, int64_t T, int3
  * The norm over many tensors of any of the types F32, F16 and BF16: norm[0] = sqrt(sum of squares), summed in fp64 and rounded to fp32 once.
  * `tensors` is a HOST array of n of them, read before the call returns; data and out are device pointers to `count` elements without gaps.
  *
- * maddness_clip_gradients: every tensor's out = data times min(1, max_norm / norm[0]), in fp32, rounded to out_dtype; out may be data itself where
+ * maddness_clip_gradients: every tensor's out = data times min(1, max_norm / norm), the factor rounded to fp32 once, the product in fp32, rounded to out_dtype; out may be data itself where
  * the types agree (then nothing is written where the factor is 1), and otherwise overlaps no data or out.  A norm that is not finite leaves the factor 1: the caller sees
- * it in norm.  max_norm >= 0 (infinity: the factor is 1).  Where norm_given is 0 the norm is that of these tensors, and written to norm; else norm
- * is read (a norm over the tensors of several processes).  norm is no element of what is written, nor of a data unless it is given.
+ * it in norm.  max_norm >= 0 (infinity: the factor is 1).  Where norm_given is 0 the norm is that of these tensors, as it is before its
+ * rounding, and written to norm; else norm is read (a norm over the tensors of several processes).  norm is no element of what is written, nor of a data unless it is given.
  * workspace  maddness_gradient_norm_workspace() bytes, 8-byte aligned (NULL where norm_given).
  */
 typedef struct {

@@ -123,18 +123,18 @@ __global__ __launch_bounds__(kThreads) void squares_kernel(Table<N> t, double *p
     if (threadIdx.x == 0) partials[blockIdx.x] = add ? partials[blockIdx.x] + sum : sum;
 }
 
-__device__ __forceinline__ float norm_of(const double *partials, int parts, double (&slots)[kThreads / 64])
+__device__ __forceinline__ double norm_of(const double *partials, int parts, double (&slots)[kThreads / 64])
 {
     double sum = 0.0;
     for (int i = threadIdx.x; i < parts; i += kThreads) sum += partials[i];
-    return (float)sqrt(group_sum(sum, slots));
+    return sqrt(group_sum(sum, slots));
 }
 
 __global__ __launch_bounds__(kThreads) void norm_kernel(const double *partials, int parts, float *norm)
 {
     __shared__ double slots[kThreads / 64];
-    const float all = norm_of(partials, parts, slots);
-    if (threadIdx.x == 0) *norm = all;
+    const double all = norm_of(partials, parts, slots);
+    if (threadIdx.x == 0) *norm = (float)all;
 }
 
 // Eight elements as they are in memory, of a narrow type in the first half.
@@ -202,14 +202,15 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(Table<N> t, const double
         }
     };
     if (blockIdx.x < t.chunks) turn_to(blockIdx.x);
-    float all;
+    double all;
     if (given) {
-        all = *norm;
+        all = (double)*norm;
     } else {
         all = norm_of(partials, parts, slots);
-        if (blockIdx.x == 0 && threadIdx.x == 0) *norm = all;
+        if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)all;
     }
-    const float factor = all > max_norm && all <= 3.402823466e38f ? (float)((double)max_norm / (double)all) : 1.0f;
+    // (of the norm as it was summed: rounded first it would put half a step more on every element)
+    const float factor = all > (double)max_norm && (float)all <= 3.402823466e38f ? (float)((double)max_norm / all) : 1.0f;
     for (uint32_t chunk = blockIdx.x; chunk < t.chunks;) {
         if (now.data != now.out || factor != 1.0f) {
             switch (now.types) {

@@ -174,3 +174,21 @@ def test_refusals(mad):
     with pytest.raises(ValueError, match="gradient"):
         mad.maddness_clip_gradients([torch.nn.Parameter(t)], 1.0)
     assert float(t.sum()) == 8
+
+
+def test_the_factor_is_that_of_the_whole_norm(mad):
+    """The quotient is formed before the norm is rounded to fp32: an element is off by the factor's rounding and its own."""
+    import torch
+    for seed in range(24):
+        for counts in ([5000, 77], [300000, 12, 4000] + [9] * 10):
+            ts = tensors(counts, ["f32"], seed)
+            norm = exact_norm(ts)
+            outs = [torch.empty_like(t) for t in ts]
+            mad.maddness_clip_gradients(ts, 1.0, out=outs)
+            for o, t in zip(outs, ts):
+                want = t.double() * min(1.0, 1.0 / norm)
+                assert bool(((o.double() - want).abs() <= 2.001 * ref.U * want.abs() + 2.0 ** -149).all()), (seed, counts)
+    # a norm that is given is taken as it is
+    t = torch.full((4,), 3.0, device="cuda")
+    mad.maddness_clip_gradients([t], 1.0, norm=torch.tensor(7.0, device="cuda"))
+    assert bool((t == 3 * (torch.tensor(1.0, device="cuda") / torch.tensor(7.0, device="cuda"))).all())
