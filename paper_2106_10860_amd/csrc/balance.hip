@@ -54,7 +54,14 @@ __device__ __forceinline__ float exponential(float x)
 
 // 1 / (1 + e^-x); 0 where that is below 2^-126, as the instruction gives no such numbers (so it is for all x below -88 too, which have e^88 here: a comparison of its own
 // takes 1.2 us of the 31 that 32768 tokens of 256 experts take).
-__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exponential(-x)); }
+// `other` is 1 minus that, as e^-x s: the difference itself has fewer digits the nearer s is to 1, and none from a logit of 18 on.  (Where s is 0 here so is this, and nothing that it is
+// a factor of beside s.)
+__device__ __forceinline__ float sigmoid(float x, float &other)
+{
+    const float e = exponential(-x), s = __builtin_amdgcn_rcpf(1.0f + e);
+    other = e * s;
+    return s;
+}
 
 // The four neighbours of every 4 LANES experts that a lane has: i of its R.
 template <int LANES>
@@ -84,9 +91,9 @@ __device__ __forceinline__ void load_logits(const BalanceArgs &a, bool pieces, i
     }
 }
 
-// A token's scores over LANES lanes, R to a lane, and their sum; 0 for masked ones and beyond E.
+// A token's scores over LANES lanes, R to a lane, and their sum; 0 for masked ones and beyond E.  slope: 1, or of a sigmoid 1 - s.
 template <int LANES, int R>
-__device__ __forceinline__ float scores_of(const BalanceArgs &a, int lane, float (&x)[R], float (&s)[R], uint32_t &seen)
+__device__ __forceinline__ float scores_of(const BalanceArgs &a, int lane, float (&x)[R], float (&s)[R], float (&slope)[R], uint32_t &seen)
 {
     seen = 0;
     float top = -kTop;
@@ -101,7 +108,8 @@ __device__ __forceinline__ float scores_of(const BalanceArgs &a, int lane, float
     if (a.softmax) top = over_token<LANES>(top, larger);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-        const float v = a.softmax ? exponential(x[i] - top) : sigmoid(x[i]);
+        slope[i] = 1.0f;
+        const float v = a.softmax ? exponential(x[i] - top) : sigmoid(x[i], slope[i]);
         s[i] = seen >> i & 1 ? v : 0.0f;
         sum += s[i];
     }
@@ -160,13 +168,13 @@ __global__ __launch_bounds__(kThreads) void balance_kernel(BalanceArgs a, void *
     int live = 0;
     const int64_t step = (int64_t)gridDim.x * kWaves * TOKENS;
     for (int64_t t = ((int64_t)blockIdx.x * kWaves + wave) * TOKENS + part; t < a.T; t += ONCE * step) {
-        float x[ONCE][R], s[R];
+        float x[ONCE][R], s[R], slope[R];
 #pragma unroll
         for (int u = 0; u < ONCE; ++u) load_logits<DT, LANES, R>(a, pieces, min(t + u * step, a.T - 1), lane, x[u]);
 #pragma unroll
         for (int u = 0; u < ONCE; ++u) {
             uint32_t seen;
-            const float all = scores_of<LANES, R>(a, lane, x[u], s, seen);
+            const float all = scores_of<LANES, R>(a, lane, x[u], s, slope, seen);
             const bool here = all > 0.0f && t + u * step < a.T;
             live += here;
             const float scale = here ? 1.0f / all : 0.0f;
@@ -311,9 +319,9 @@ __global__ __launch_bounds__(kGradientWaves * 64) void balance_gradient_kernel(B
 #pragma unroll
         for (int u = 0; u < ONCE; ++u) {
             const int64_t t = t0 + u * step;
-            float s[R];
+            float s[R], slope[R];
             uint32_t seen;
-            const float all = scores_of<LANES, R>(a, lane, x[u], s, seen), scale = all > 0.0f ? 1.0f / all : 0.0f;
+            const float all = scores_of<LANES, R>(a, lane, x[u], s, slope, seen), scale = all > 0.0f ? 1.0f / all : 0.0f;
             float dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < R; ++i) dot += s[i] * scale * push[i];
@@ -326,7 +334,7 @@ __global__ __launch_bounds__(kGradientWaves * 64) void balance_gradient_kernel(B
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int j = 4 * q + i;
-                    d[i] = seen >> j & 1 ? times * (s[j] * scale * (push[j] - dot) * (a.softmax ? 1.0f : 1.0f - s[j])) : 0.0f;
+                    d[i] = seen >> j & 1 ? times * (s[j] * scale * (push[j] - dot) * slope[j]) : 0.0f;
                 }
                 if (add_pieces) {
                     if (e >= a.E) continue;

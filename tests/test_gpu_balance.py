@@ -243,3 +243,28 @@ def test_sigmoids_of_every_logit(mad, dtype):
     assert (np.abs(route - s) <= 8 * U * s + 2.0 ** -126).all()
     loss = ((route / route.sum(1, keepdims=True)).sum(0) * push).sum()
     assert abs(loss - want) <= e_loss
+
+
+def test_slopes_of_large_logits(mad):
+    """A sigmoid's slope keeps its digits where the score is next to 1: 1 - s is made of the exponential, not of s."""
+    import torch
+    T, E = 2400, 8
+    rng = np.random.default_rng(12)
+    x = rng.normal(size=(T, E))
+    x[np.arange(T), np.arange(T) % E] = np.linspace(-20, 100, T)
+    x[5::50] = rng.random((T // 50, E)) * 40
+    logits = dev(x)
+    ids = logits.topk(2, -1)[1].to(torch.int32).contiguous()
+    push = host(mad.maddness_balance(logits, ids, scores="sigmoid")[2])
+    got = host(mad.maddness_balance_gradient(logits, mad.maddness_balance(logits, ids, scores="sigmoid")[2], scores="sigmoid"))
+    x = host(logits)
+    _, _, _, p, s, seen, rel = ref.balance(x, ids.cpu().numpy(), "sigmoid", 1.0)
+    slope = 1 / (1 + np.exp(x))
+    dot = (p * push).sum(1, keepdims=True)
+    rel_p = rel + rel.max(1, keepdims=True) + 24 * U
+    e_dot = (p * push * (rel_p + 26 * U)).sum(1, keepdims=True)
+    apart = np.abs(push - dot)
+    # the slope: an exponential of 4 U, a score of 8 and a product; one below 2^-126 may be 0
+    bound = 1.01 * p * slope * (rel_p * apart + e_dot + 6 * U * (apart + push + dot) + 14 * U * apart) + p * apart * 2.0 ** -126 + 2.0 ** -148
+    off = np.abs(got - p * slope * (push - dot))
+    assert (off <= bound + ref.rounding(got, "f32")).all(), float((off / bound).max())
