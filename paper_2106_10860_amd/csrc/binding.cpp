@@ -758,12 +758,13 @@ PyObject *tuple_of(const T &...t)
     return tuple;
 }
 
-// An IntegerMatrix, as its constructor checked it.
+// An IntegerMatrix: what its constructor checks, as its tensors may have been replaced since.
 maddness_integer_matrix integer_matrix(PyObject *o, const at::Device *device, at::Device *own)
 {
     Ref q_ref(PyObject_GetAttr(o, s_q)), scale_ref(PyObject_GetAttr(o, s_scale));
-    const at::Tensor &q = tensor(q_ref.p), &scale = tensor(scale_ref.p);
-    if (q.dim() != 2 || q.scalar_type() != at::kChar || (device && q.device() != *device)) throw NotUsual();
+    const at::Tensor &q = tensor(q_ref.p);
+    if (q.dim() != 2 || q.scalar_type() != at::kChar || (device && q.device() != *device) || (q.size(1) > 1 && q.stride(1) != 1)) throw NotUsual();
+    const at::Tensor &scale = flat(scale_ref.p, at::kFloat, {q.size(0)}, q.device());
     maddness_integer_matrix m{};
     m.data = q.data_ptr();
     m.dtype = MADDNESS_I8;

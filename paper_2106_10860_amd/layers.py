@@ -36,12 +36,16 @@ def _here(t) -> None:
 
 class IntegerMatrix:
     """8-bit integers ``q`` [rows, cols] of dtype int8 with unit column stride, rows 16-byte aligned, and their ``scale`` fp32 [rows]:
-    row r stands for q[r] * scale[r]."""
+    row r stands for q[r] * scale[r].  Both may be replaced; every call checks what it finds."""
 
     __slots__ = ("q", "scale")
 
     def __init__(self, q, scale):
-        torch = _m._torch or _m._torch_module()
+        self.q, self.scale = q, scale
+        self._check()
+
+    def _check(self) -> None:
+        torch, q, scale = _m._torch or _m._torch_module(), self.q, self.scale
         if not isinstance(q, torch.Tensor) or not isinstance(scale, torch.Tensor) or not q.is_cuda or not scale.is_cuda:
             raise TypeError("q and scale must be device tensors")
         if q.dtype is not torch.int8 or scale.dtype is not torch.float32:
@@ -54,7 +58,6 @@ class IntegerMatrix:
         if not scale.is_contiguous():
             raise ValueError("scale must be contiguous")
         _no_gradient(scale, "scale")
-        self.q, self.scale = q, scale
 
     @classmethod
     def _made(cls, q, scale) -> "IntegerMatrix":
@@ -79,6 +82,7 @@ class IntegerMatrix:
 
     @property
     def _struct(self):
+        self._check()
         rows, cols = self.q.shape
         ld = self.q.stride(0) if rows > 1 else _up(max(cols, self.q.stride(0)), 16)
         return _m._IntegerMatrix(self.q.data_ptr(), MADDNESS_I8, rows, cols, ld, self.scale.data_ptr())
@@ -118,6 +122,7 @@ def maddness_integer_product(A, B: IntegerMatrix, bias=None, out_dtype=None, out
     if r is not NotImplemented:
         return _m._done(r)
     torch = _m._torch or _m._torch_module()
+    b = B._struct
     if isinstance(A, IntegerMatrix):
         a, (M, K), device = A._struct, A.shape, A.device
     else:
@@ -139,7 +144,7 @@ def maddness_integer_product(A, B: IntegerMatrix, bias=None, out_dtype=None, out
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
     if workspace is not None and not workspace.is_contiguous():              # (its size in bytes is then not what it has room for)
         raise ValueError("workspace must be contiguous")
-    _m._check(L.maddness_integer_product(C.byref(a), C.byref(B._struct), bias_p, out.data_ptr(), out_code, _m._rows(out, "out")[2],
+    _m._check(L.maddness_integer_product(C.byref(a), C.byref(b), bias_p, out.data_ptr(), out_code, _m._rows(out, "out")[2],
                                          _m._ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(),
                                          _m._stream(None)))
     return out

@@ -310,3 +310,23 @@ def test_rows_whose_scale_has_no_half(mad):
     eye = mad.IntegerMatrix(torch.eye(400, dtype=torch.int8, device="cuda"), torch.ones(400, device="cuda"))
     out = mad.maddness_integer_product(torch.from_numpy(x[:32]).cuda(), eye, out_dtype=torch.float32)
     assert np.array_equal(out.cpu().numpy(), q[:32].astype(np.float32) * scale[:32, None].astype(np.float32))
+
+
+def test_replaced_tensors_are_checked(mad):
+    """A matrix whose values or scales were replaced is refused by the call as by the constructor, on either side, and taken where they fit."""
+    import torch
+    x = torch.ones((3, 32), device="cuda")
+    want = mad.maddness_integer_product(x, mad.maddness_quantise_rows(torch.ones((4, 32), device="cuda")), out_dtype=torch.float32)
+    q, s = torch.zeros((4, 32), dtype=torch.int8, device="cuda"), torch.ones(4, device="cuda")
+    bad = [("scale", s.half(), TypeError), ("scale", s.double(), TypeError), ("scale", s.cpu(), TypeError), ("scale", None, TypeError), ("scale", s[:3], ValueError), ("scale", s[:1].expand(4), ValueError),
+           ("scale", s.reshape(4, 1), ValueError), ("scale", torch.ones(8, device="cuda")[::2], ValueError), ("q", q.float(), TypeError), ("q", q.cpu(), TypeError), ("q", q[0], ValueError),
+           ("q", q[:2], ValueError), ("q", q.t(), ValueError), ("q", q[:, :1].expand(4, 32), ValueError), ("q", None, TypeError)]
+    for name, value, error in bad:
+        for side in (0, 1):
+            W = mad.maddness_quantise_rows(torch.ones((4, 32), device="cuda"))
+            setattr(W, name, value)
+            with pytest.raises(error):
+                mad.maddness_integer_product(W if side else x, W)
+    W = mad.maddness_quantise_rows(torch.zeros((4, 32), device="cuda"))
+    W.q, W.scale = torch.full((4, 32), 127, dtype=torch.int8, device="cuda"), torch.full((4,), 1 / 127, device="cuda")
+    assert torch.equal(mad.maddness_integer_product(x, W, out_dtype=torch.float32), want)

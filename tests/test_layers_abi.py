@@ -169,3 +169,13 @@ def test_gradient_norm_and_clipping_refuse(mad):
     refused(mad, clip(dict(data=FAKE + 4096, out=FAKE + 8192), out=FAKE + 4096), inval, "norm lies within tensor 0")
     # nothing to do
     refused(mad, clip(given=1, work=None, size=0), mad.MADDNESS_OK)
+
+
+def test_an_integer_matrix_is_checked_by_every_call(mad):
+    """Its tensors can be replaced: what a call finds there is refused as by the constructor."""
+    import torch
+    W = mad.IntegerMatrix._made(torch.zeros((4, 32), dtype=torch.int8), torch.ones(4))
+    with pytest.raises(TypeError, match="device tensors"):
+        W._struct
+    with pytest.raises(TypeError, match="device tensors"):
+        mad.maddness_integer_product(torch.ones((3, 32)), W)
