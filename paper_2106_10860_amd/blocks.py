@@ -91,12 +91,16 @@ def _flat(t, dtype, shape, name: str):
 
 class BlockMatrix:
     """8-bit values ``q`` [rows, cols] (or [experts, rows, cols]) of dtype float8_e4m3fn with unit column stride, and their exponents
-    ``scale``, uint8 [rows / tile, cols / 128] each rounded up, the byte b for 2^(b - 127)."""
+    ``scale``, uint8 [rows / tile, cols / 128] each rounded up, the byte b for 2^(b - 127).  All may be replaced; every call checks what it finds."""
 
     __slots__ = ("q", "scale", "tile")
 
     def __init__(self, q, scale, tile: int = 1):
-        torch = _m._torch or _m._torch_module()
+        self.q, self.scale, self.tile = q, scale, tile
+        self._check()
+
+    def _check(self) -> None:
+        torch, q, scale, tile = _m._torch or _m._torch_module(), self.q, self.scale, self.tile
         if not isinstance(q, torch.Tensor) or not isinstance(scale, torch.Tensor) or not q.is_cuda or not scale.is_cuda:
             raise TypeError("q and scale must be device tensors")
         if q.dtype is not torch.float8_e4m3fn or scale.dtype is not torch.uint8:
@@ -113,7 +117,6 @@ class BlockMatrix:
         for t, name in ((q, "q"), (scale, "scale")):
             if t.shape[-1] > 1 and t.stride(-1) != 1:
                 raise ValueError(f"{name} must have unit column stride")
-        self.q, self.scale, self.tile = q, scale, tile
 
     @classmethod
     def _made(cls, q, scale, tile: int) -> "BlockMatrix":
@@ -128,6 +131,8 @@ class BlockMatrix:
 
     @property
     def _struct(self):
+        self._check()
+
         def strides(t, unit):
             ld = t.stride(-2) if t.shape[-2] > 1 else _up(max(t.shape[-1], t.stride(-2)), unit)
             return ld, (t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else 0)
@@ -238,7 +243,9 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", so
     if r is not NotImplemented:
         return _m._done(r)
     torch = _m._torch or _m._torch_module()
+    b = B._struct
     if isinstance(A, BlockMatrix):
+        A._check()
         if len(A.shape) != 2:
             raise ValueError("A must be 2-D")
         a, a_dtype, (M, K), device = A._struct, MADDNESS_E4M3, A.shape, A.device
@@ -285,7 +292,7 @@ def maddness_block_product(A, B: BlockMatrix, offsets=None, by: str = "rows", so
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
     if workspace is not None and not workspace.is_contiguous():              # (its size in bytes is then not what it has room for)
         raise ValueError("workspace must be contiguous")
-    _m._check(L.maddness_block_product(C.byref(a), C.byref(B._struct), how, groups, offsets_p, source_p, M, repeat, out.data_ptr(), _code(out, "out"), ldo,
+    _m._check(L.maddness_block_product(C.byref(a), C.byref(b), how, groups, offsets_p, source_p, M, repeat, out.data_ptr(), _code(out, "out"), ldo,
                                        _m._ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(),
                                        _m._stream(None)))
     return out

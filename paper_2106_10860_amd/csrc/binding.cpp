@@ -378,7 +378,7 @@ T *flat_or_null(PyObject *o, at::ScalarType type, at::IntArrayRef sizes, const a
     return o == Py_None ? nullptr : static_cast<T *>(flat(o, type, sizes, device).data_ptr());
 }
 
-// A BlockMatrix, as its constructor checked it.
+// A BlockMatrix: what its constructor checks, as its parts may have been replaced since.
 maddness_block_matrix block_matrix(PyObject *o, const at::Device *device, int64_t *experts, at::Device *own = nullptr)
 {
     Ref q_ref(PyObject_GetAttr(o, s_q)), scale_ref(PyObject_GetAttr(o, s_scale)), tile(PyObject_GetAttr(o, s_tile));
@@ -391,6 +391,10 @@ maddness_block_matrix block_matrix(PyObject *o, const at::Device *device, int64_
     m.tile = narrow(whole(tile.p));
     m.rows = q.size(n - 2);
     m.cols = q.size(n - 1);
+    if ((m.tile != 1 && m.tile != MADDNESS_BLOCK) || scale.scalar_type() != at::kByte || scale.device() != q.device() || (n == 3 && scale.size(0) != q.size(0)) ||
+        scale.size(n - 2) != (m.rows + m.tile - 1) / m.tile || scale.size(n - 1) < (m.cols + MADDNESS_BLOCK - 1) / MADDNESS_BLOCK || (m.cols > 1 && q.stride(n - 1) != 1) ||
+        (scale.size(n - 1) > 1 && scale.stride(n - 1) != 1))
+        throw NotUsual();
     m.ld = m.rows > 1 ? q.stride(n - 2) : up(std::max(m.cols, q.stride(n - 2)), 16);
     m.scale = static_cast<const uint8_t *>(scale.data_ptr());
     m.lds = scale.size(n - 2) > 1 ? scale.stride(n - 2) : up(std::max(scale.size(n - 1), scale.stride(n - 2)), 4);

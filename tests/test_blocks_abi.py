@@ -154,3 +154,13 @@ def test_product_by_choice_refuses(mad):
             (dict(groups=0), inval, "groups"), (dict(groups=70000), unsupported, "groups"), (dict(out=None), inval, "out")):
         refused(mad, call(**kw), status, text)
     refused(mad, call(slots=0, source=None), mad.MADDNESS_OK)
+
+
+def test_a_block_matrix_is_checked_by_every_call(mad):
+    """Its tensors can be replaced: what a call finds there is refused as by the constructor."""
+    import torch
+    W = mad.BlockMatrix._made(torch.zeros((4, 32)).to(torch.float8_e4m3fn), torch.full((4, 4), 127, dtype=torch.uint8), 1)
+    with pytest.raises(TypeError, match="device tensors"):
+        W._struct
+    with pytest.raises(TypeError, match="device tensors"):
+        mad.maddness_block_product(torch.ones((3, 32)), W)

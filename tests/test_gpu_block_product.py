@@ -448,3 +448,33 @@ def test_a_stream_that_is_given_owns_what_the_call_makes(mad):
     ids2, weights2 = mad.maddness_route(logits, 4)
     assert torch.equal(ids, ids2) and torch.equal(weights, weights2)
     assert torch.equal(y, mad.maddness_combine(got[:40].float(), mad.maddness_order(ids2, 32)[3], weights2))
+
+
+@pytest.mark.parametrize("how", ["native", "python"])
+def test_replaced_parts_are_checked(mad, monkeypatch, how):
+    """A matrix whose values, exponents or tile were replaced is refused by the call as by the constructor, on either side, and taken where they fit."""
+    import torch
+    if how == "python":
+        monkeypatch.setattr(mad, "_native", mad._NotBuilt)
+    x = torch.ones((3, 300), device="cuda")
+    one = torch.ones((200, 300), device="cuda")
+    want = mad.maddness_block_product(x, mad.maddness_quantise_blocks(one))
+    q, s = (torch.zeros((200, 304), device="cuda").to(torch.float8_e4m3fn)[:, :300], torch.full((200, 4), 127, dtype=torch.uint8, device="cuda"))
+    bad = [("scale", s.float(), TypeError), ("scale", s.to(torch.int8), TypeError), ("scale", s.cpu(), TypeError), ("scale", None, TypeError), ("scale", s[:199], ValueError), ("scale", s[:, :2], ValueError),
+           ("scale", s[0], ValueError), ("scale", s.t().contiguous().t(), ValueError), ("q", q.float(), TypeError), ("q", q.cpu(), TypeError), ("q", q[0], ValueError), ("q", q[:150], ValueError),
+           ("q", q.as_strided((200, 300), (304, 0)), ValueError), ("q", None, TypeError), ("tile", 128, ValueError), ("tile", 7, ValueError)]
+    for name, value, error in bad:
+        for side in (0, 1):
+            W = mad.maddness_quantise_blocks(one)
+            setattr(W, name, value)
+            with pytest.raises(error):
+                mad.maddness_block_product(W if side else x, W)
+    W = mad.maddness_quantise_blocks(torch.zeros_like(one))
+    fits = mad.maddness_quantise_blocks(one)
+    W.q, W.scale = fits.q, fits.scale
+    assert torch.equal(mad.maddness_block_product(x, W), want)
+    stack = mad.maddness_quantise_blocks(torch.ones((3, 200, 300), device="cuda"))
+    stack.scale = stack.scale[:2]
+    ids = torch.zeros(3, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        mad.maddness_block_product(x, stack, by="choice", source=ids)
