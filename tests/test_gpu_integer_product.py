@@ -330,3 +330,24 @@ def test_replaced_tensors_are_checked(mad):
     W = mad.maddness_quantise_rows(torch.zeros((4, 32), device="cuda"))
     W.q, W.scale = torch.full((4, 32), 127, dtype=torch.int8, device="cuda"), torch.full((4,), 1 / 127, device="cuda")
     assert torch.equal(mad.maddness_integer_product(x, W, out_dtype=torch.float32), want)
+
+
+@pytest.mark.parametrize("size", [(16384, 1024, 1024), (4000, 510, 4096), (300, 1000, 510), (1, 512, 1024)], ids=lambda c: "%dx%dx%d" % c)
+def test_bfloat16_rows_to_the_bit(mad, size):
+    """Each step of the definition on its own (the quotient's rounding, the exact sum, two products and the result's rounding): the very bits, in tiles of every size.  An
+    element of half its row's largest is 63.5 steps, or just below, as the scale's own rounding has it."""
+    import torch
+    M, N, K = size
+    print("case to the bit", size, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    x = (torch.randn(M, K, generator=g, device="cuda") * torch.exp(0.5 * torch.randn(M, 1, generator=g, device="cuda"))).bfloat16()
+    x[:, 3], x[:, 5] = 16 * x[:, 7], 8 * x[:, 7]
+    W = mad.maddness_quantise_rows(torch.randn(N, K, generator=g, device="cuda") / K ** 0.5)
+    top = x.double().abs().amax(1, keepdim=True)
+    scale = (top / torch.full_like(top, 127.0)).float()        # (a 64-bit quotient is never so near to half an fp32 step that this rounds twice)
+    q = torch.round(x.double() / scale.double())
+    assert bool((q.abs().amax(1) == 127).all())
+    sums = torch.mm(q, W.q.double().T.contiguous())            # (whole numbers below 2^53)
+    want = (sums.float() * scale * W.scale).bfloat16()
+    assert torch.equal(mad.maddness_integer_product(x, W), want)
+    assert torch.equal(mad.maddness_integer_product(mad.maddness_quantise_rows(x), W), want)

@@ -323,3 +323,30 @@ def test_the_layers_balance_of_logits_that_vanish(mad):
     # (shares and their products within 100 roundings, as every one of 8 experts' parts has less)
     most = 100 * ref.U * (p * (np.abs(host(saved.push)) + (p * host(saved.push)).sum(1, keepdims=True)) + np.abs(host(choice))) + 2.0 ** -126
     assert abs(float(saved.balance_loss) - want) <= 100 * ref.U * want and (np.abs(host(dlogits) - (host(choice) + d)) <= most).all()
+
+
+def test_the_example_without_its_options_is_the_plain_loop(mad):
+    """The steps of a loop of choice, layer and updates alone, written out: the same losses to the bit."""
+    import torch
+    from paper_2106_10860_amd.expert_layer import ExpertLayer, train_example
+    steps, T, K, N, E, k = 4, 300, 128, 96, 4, 2
+    g = torch.Generator(device="cuda").manual_seed(0)
+
+    def randn(*shape):
+        return torch.randn(*shape, generator=g, device="cuda")
+
+    kinds, truth = randn(E, K), randn(E, N, K) / K ** 0.5
+    weight, gate = randn(E, N, K) * (0.3 / K ** 0.5), 0.3 * randn(E, K)
+    losses = []
+    for _ in range(steps):
+        kind = torch.randint(E, (T,), generator=g, device="cuda")
+        x = kinds[kind] + 0.5 * randn(T, K)
+        off = ExpertLayer.from_weights(weight, k)
+        out, saved = off.forward(x, x @ gate.T, training=True)
+        error = out - torch.bmm(truth[kind], x.unsqueeze(2)).squeeze(2)
+        losses.append(float((error ** 2).mean()))
+        assert saved.balance_loss is None and saved.counts is None and saved.push is None
+        _, dW, dlogits = off.backward(saved, 2 * error / error.numel())
+        weight -= 4.0 * dW
+        gate -= 0.05 * (dlogits.T @ x)
+    assert train_example(steps=steps, tokens=T, inputs=K, outputs=N, experts=E) == losses
