@@ -494,8 +494,8 @@ int maddness_integer_product(const maddness_integer_matrix *A, const maddness_in
                              int64_t ldo, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * The layer norm of every row: mu = mean(x), v = mean((x - mu)^2), r = 1 / sqrt(v + eps), y = (x - mu) r weight + bias; all in fp32, the
- * variance of the centred values.
+ * The layer norm of every row: mu = mean(x), v = mean((x - mu)^2), r = 1 / sqrt(v + eps), y = (x - mu) r weight + bias; all in fp32 (sums of rows beyond
+ * 16384 elements in fp64), the variance of the centred values.  mu is a number of fp32: half a step of it or more is left in the centred values.
  * x       [rows][ldx] of `dtype`; weight, bias [cols] of parameter_dtype, or NULL (1 and 0).  Types: F32, F16 or BF16.
  * out     [rows][ldo] of out_dtype: y rounded once, scale NULL.  Or MADDNESS_I8: y as an integer matrix with `scale` [rows], as
  *         maddness_quantise_rows makes of the fp32 y.
@@ -503,8 +503,8 @@ int maddness_integer_product(const maddness_integer_matrix *A, const maddness_in
  * cols >= 1; eps >= 0 and finite.
  *
  * maddness_layer_norm_gradient: from the gradient g of y, with h = (x - mu) r and u = g weight:
- *   dx = r (u - mean(u) - h mean(u h)), rounded to x's dtype;  dweight[c] = sum over rows of g h, dbias[c] = sum over rows of g, in fp32 in an order that
- *   depends on the sizes only.
+ *   dx = r (u - mean(u) - h mean(u h)), rounded to x's dtype;  dweight[c] = sum over rows of g h, dbias[c] = sum over rows of g, in fp32 (a thread's part
+ *   of rows below 8 or beyond 16384 elements in fp64) in an order that depends on the sizes only.
  * gradient [rows][ldg] of gradient_dtype.  mean and rstd of the call before.  dx [rows][ldd], or NULL.  dweight and dbias [cols], or both NULL
  * (of up to 2^26 columns).
  * Without rows dweight and dbias are 0.

@@ -130,7 +130,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void rows_kernel(RowsArgs a)
 #pragma unroll
             for (int p = 0; p < PER; ++p)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[p][i] = __builtin_fmaf(v[p][i] * rstd, weight[p][i], bias[p][i]);      // (the same in every form of the kernel)
+                for (int i = 0; i < 8; ++i) v[p][i] = __builtin_fmaf(v[p][i] * rstd, weight[p][i], bias[p][i]);      // (written out, so that all of this kernel's forms round alike)
         }
         if constexpr (OT == kI8) {
             uint32_t top = 0;
