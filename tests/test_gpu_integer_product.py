@@ -332,7 +332,7 @@ def test_replaced_tensors_are_checked(mad):
     assert torch.equal(mad.maddness_integer_product(x, W, out_dtype=torch.float32), want)
 
 
-@pytest.mark.parametrize("size", [(16384, 1024, 1024), (4000, 510, 4096), (300, 1000, 510), (1, 512, 1024)], ids=lambda c: "%dx%dx%d" % c)
+@pytest.mark.parametrize("size", [(16384, 1024, 1024), (8192, 1024, 1024), (8192, 1024, 512), (4000, 510, 4096), (300, 1000, 510), (1, 512, 1024)], ids=lambda c: "%dx%dx%d" % c)
 def test_bfloat16_rows_to_the_bit(mad, size):
     """Each step of the definition on its own (the quotient's rounding, the exact sum, two products and the result's rounding): the very bits, in tiles of every size.  An
     element of half its row's largest is 63.5 steps, or just below, as the scale's own rounding has it."""
